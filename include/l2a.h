@@ -44,7 +44,7 @@
 extern "C" {
 #endif
 
-enum { L2A_BF16 = 0, L2A_FP32 = 1 };
+enum { L2A_BF16 = 0, L2A_FP32 = 1, L2A_FP8 = 2 /* elements of an l2a_cache only, see there */ };
 
 enum {
     L2A_FLAG_DENSE = 1,       /* every token is routed (d = 1 everywhere): the in-house dense causal
@@ -232,6 +232,82 @@ size_t l2a_decode_workspace_bytes(const l2a_params* p);
 int l2a_attn_decode(const l2a_params* p, const void* q, const void* k_cache, const void* v_cache,
                     const int32_t* pos, const uint8_t* mask, void* O, float* lse_local, float* lse_global,
                     void* S_opt, void* A_opt, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Serving on a paged KV cache (Sec. 3.4): new tokens of many sequences at once, packed one sequence behind the other -- chunks of
+ * prompts, drafts of a few tokens, single tokens, in any mixture.  A step is
+ *     l2a_router_decide (B = 1, T = packed tokens)  ->  l2a_cache_write  ->  l2a_attn_extend
+ * and l2a_cache_read hands cached rows back (a prefix for l2a_attn_fwd, a sequence that is moved).  bf16, D = 128.
+ *
+ * The cache is a pool of pages of page_size tokens; row r of sequence b is row r mod page_size of page table[b][r / page_size].
+ *   k, v              [pages, Hkv, page_size, D] elements: the rows of a KV head in a page lie one behind the other
+ *   L2A_BF16          bf16 elements
+ *   L2A_FP8           e4m3 elements (OCP: no infinities, largest 448) in blocks of 32 channels, each with a power of two of its own:
+ *                     k_scale, v_scale [pages, Hkv, page_size, D / 32] uint8 hold its exponent plus 127, and an
+ *                     element stands for e4m3 * 2^(byte - 127), which is a bf16 number.  The exponent of a block whose largest
+ *                     magnitude is m is the least integer e with m <= 448 * 2^e, clamped into -118..119; elements are rounded to
+ *                     nearest, ties to even (magnitudes above 448 * 2^119 become that).  A NaN stays a NaN, an infinity becomes one.  A row takes 132 bytes instead of 256.
+ *   table             [B, max_pages] int32, device memory.  Entries of pages that a call has no use for may hold anything.
+ * The struct is host memory and is read during the call; what it points to is device memory owned by the caller.
+ *
+ * In all three calls p->B is the number of sequences and p->T the number of packed tokens.
+ *   seq_start   [B + 1] int32, device memory, ascending: sequence b has packed tokens seq_start[b] .. seq_start[b + 1] - 1,
+ *               none where the two are equal.  Packed tokens before the first and behind the last sequence belong to nobody: what
+ *               they hold is not read, and outputs are left as they were there.
+ *   pos         [B] int32, device memory: position of the sequence's first new token (the tokens cached before it)
+ * Values in device memory cannot be validated on the host.  Values out of range (starts that do not ascend, positions outside
+ * the table, page numbers outside the pool) never lead to an access outside the tensors: l2a_cache_write and l2a_cache_read
+ * skip such rows, l2a_attn_extend clamps them into range.
+ *
+ * Errors of the three calls: L2A_ERR_NULL, L2A_ERR_ALIGN as everywhere (all tensors 16-byte aligned, table and index arrays 4-byte);
+ * L2A_ERR_SHAPE for page_size not a power of two in 16..1024, pages or max_pages < 1, more than 2^30 tokens per
+ * sequence, max_new < 1; L2A_ERR_UNSUPPORTED for p->dtype other than L2A_BF16, D other than 128, an unknown cache dtype,
+ * L2A_FLAG_SCALAR, L2A_FLAG_RING_CACHE.
+ */
+typedef struct l2a_cache {
+    void *k, *v;
+    void *k_scale, *v_scale; /* L2A_FP8 only */
+    const int32_t* table;
+    int32_t pages;           /* of the pool */
+    int32_t page_size;       /* tokens of a page */
+    int32_t max_pages;       /* entries of a sequence in the table */
+    int32_t dtype;           /* L2A_BF16 | L2A_FP8 */
+} l2a_cache;
+
+/*
+ * Cache rows of the packed tokens: written from (l2a_cache_write) or to (l2a_cache_read) k, v [T, Hkv, D] bf16.  Writing rounds
+ * an L2A_FP8 cache's elements as above, reading is exact.  Of p: B, T, Hkv, D and dtype count (the other fields must still be
+ * valid).  Two packed tokens with the same place in the pool (two sequences that share a page they both write): either one's row.
+ */
+int l2a_cache_write(const l2a_params* p, const l2a_cache* c, const void* k, const void* v, const int32_t* seq_start,
+                    const int32_t* pos, void* stream);
+int l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* seq_start, const int32_t* pos, void* k, void* v,
+                   void* stream);
+
+/*
+ * Attention of the packed new tokens over their sequences' pages (Sec. 3.1 Eqs. 2, 4, 5 with the keys in the cache): the token at
+ * position t takes Local attention over rows t-W..t and, where its decision is 1, Global attention over rows 0..t; o = s + d a.
+ * The new tokens' own rows have to be in the cache already (l2a_cache_write).  Both branches read the same q and cache (for
+ * separate Local and Global modules call twice with L2A_FLAG_SKIP_GLOBAL / L2A_FLAG_SKIP_LOCAL and a cache each).  The keys of
+ * a routed row's window are read and multiplied once for both branches.  Rows that no token of the call has in reach are not
+ * read: with L2A_FLAG_SKIP_GLOBAL (or where no token is routed) a sequence's pages before its first new token's window may
+ * have been given back, and their table entries hold anything; rows behind a sequence's last new token are not read either.
+ *
+ *   q           in  [T,Hq,D]
+ *   mask        in  [mask_heads,T] uint8, device memory: the new tokens' decisions (l2a_router_decide writes [1,1,T]; NULL
+ *                   allowed with L2A_FLAG_DENSE: all routed, or L2A_FLAG_SKIP_GLOBAL)
+ *   max_new     most new tokens that a sequence of this call has (device data beyond it is cut off)
+ *   O           out [T,Hq,D]
+ *   lse_local, lse_global  out optional [Hq,T]; lse_global is -inf where d = 0
+ *   S_opt, A_opt  out optional [T,Hq,D]; A is zero where d = 0
+ *   workspace   l2a_extend_workspace_bytes(p, c, max_new) bytes, 16-byte aligned; as everywhere not preserved, and calls that share one (captured
+ *               graphs of them, too) must be ordered
+ * How a row's keys are shared out, and so the last bits of its results, depends on the whole call.
+ */
+size_t l2a_extend_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_new);
+int l2a_attn_extend(const l2a_params* p, const l2a_cache* c, const void* q, const int32_t* seq_start, const int32_t* pos,
+                    const uint8_t* mask, int32_t max_new, void* O, float* lse_local, float* lse_global, void* S_opt,
+                    void* A_opt, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Backward (Sec. 3.2: gradients only for the active queries, reusing the saved log-sum-exp

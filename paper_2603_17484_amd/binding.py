@@ -16,7 +16,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libl2a.so")
 
-L2A_BF16, L2A_FP32 = 0, 1
+L2A_BF16, L2A_FP32, L2A_FP8 = 0, 1, 2
 L2A_FLAG_DENSE, L2A_FLAG_SKIP_LOCAL, L2A_FLAG_SKIP_GLOBAL = 1, 2, 4
 L2A_FLAG_SEQUENTIAL = 8
 L2A_FLAG_RING_CACHE = 16
@@ -25,6 +25,7 @@ L2A_FLAG_SCALAR = 1 << 16
 EXPORTS = ("l2a_version", "l2a_strerror", "l2a_route_workspace_bytes", "l2a_attn_workspace_bytes",
            "l2a_kblk_entries", "l2a_route_compact", "l2a_route_compact_static", "l2a_router_decide", "l2a_attn_fwd", "l2a_attn_bwd",
            "l2a_decode_workspace_bytes", "l2a_attn_decode",
+           "l2a_cache_write", "l2a_cache_read", "l2a_extend_workspace_bytes", "l2a_attn_extend",
            "l2a_profile_enable", "l2a_profile_read")
 
 
@@ -32,6 +33,13 @@ class l2a_params(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("W", ctypes.c_int32), ("mask_heads", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class l2a_cache(ctypes.Structure):
+    """A paged KV cache (make_cache fills one from tensors and keeps them alive)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 class L2AError(RuntimeError):
@@ -71,6 +79,14 @@ def lib() -> ctypes.CDLL:
         L.l2a_decode_workspace_bytes.argtypes = [pp]
         L.l2a_attn_decode.restype = ctypes.c_int
         L.l2a_attn_decode.argtypes = [pp] + [vp] * 10 + [vp, ctypes.c_size_t, vp]
+        cp = ctypes.POINTER(l2a_cache)
+        for f in (L.l2a_cache_write, L.l2a_cache_read):
+            f.restype = ctypes.c_int
+            f.argtypes = [pp, cp] + [vp] * 4 + [vp]
+        L.l2a_extend_workspace_bytes.restype = ctypes.c_size_t
+        L.l2a_extend_workspace_bytes.argtypes = [pp, cp, ctypes.c_int32]
+        L.l2a_attn_extend.restype = ctypes.c_int
+        L.l2a_attn_extend.argtypes = [pp, cp] + [vp] * 4 + [ctypes.c_int32] + [vp] * 5 + [vp, ctypes.c_size_t, vp]
         L.l2a_attn_fwd.restype = ctypes.c_int
         L.l2a_attn_fwd.argtypes = [pp] + [vp] * 6 + [i32p] * 3 + [vp] * 5 + [vp, ctypes.c_size_t, vp]
         L.l2a_attn_bwd.restype = ctypes.c_int
@@ -146,6 +162,73 @@ def l2a_attn_decode(p: l2a_params, q, k_cache, v_cache, pos, mask, O, lse_local=
         raise L2AError(rc, "l2a_attn_decode")
 
 
+def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+               v_scale: Optional[torch.Tensor] = None) -> l2a_cache:
+    """k, v [pages, Hkv, page_size, 128]: bfloat16, or float8_e4m3fn with k_scale, v_scale [pages, Hkv, page_size, 4] uint8;
+    table [B, max_pages] int32."""
+    fp8 = k.dtype == torch.float8_e4m3fn
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or not (fp8 or k.dtype == torch.bfloat16):
+        raise ValueError("k and v must be [pages, Hkv, page_size, 128], both bfloat16 or both float8_e4m3fn")
+    for s in (k_scale, v_scale):
+        if (s is None) == fp8 or (fp8 and (s.dtype != torch.uint8 or tuple(s.shape) != tuple(k.shape[:3]) + (k.shape[3] // 32,))):
+            raise ValueError("float8_e4m3fn caches have k_scale and v_scale [pages, Hkv, page_size, 4] uint8, bfloat16 ones have none")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("table must be [B, max_pages] int32")
+    if len({t.device for t in (k, v, table, k_scale, v_scale) if t is not None}) > 1:
+        raise ValueError("a cache's tensors must be on one device")
+    c = l2a_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), k.shape[0], k.shape[2], table.shape[1],
+                  L2A_FP8 if fp8 else L2A_BF16)
+    c.tensors = (k, v, k_scale, v_scale, table)
+    return c
+
+
+def _check_packed(p: l2a_params, c: l2a_cache, seq_start, pos, rows, mask=None, stats=()) -> None:
+    """The sizes and types that the C ABI cannot see.  rows: [T, heads, D] bf16 tensors with their numbers of heads."""
+    k, table = c.tensors[0], c.tensors[4]
+    if k.shape[1] != p.Hkv or k.shape[3] != p.D or table.shape[0] != p.B:
+        raise ValueError(f"the cache has {k.shape[1]} KV heads of {k.shape[3]} channels and a table of {table.shape[0]} sequences")
+    if seq_start.dtype != torch.int32 or pos.dtype != torch.int32 or seq_start.numel() != p.B + 1 or pos.numel() != p.B:
+        raise ValueError("seq_start and pos must be int32 of B + 1 and B entries")
+    for t, heads in rows:
+        if t is not None and (t.dtype != torch.bfloat16 or t.numel() != p.T * heads * p.D):
+            raise ValueError(f"packed rows must be bfloat16 [T, {heads}, {p.D}]")
+    if mask is not None and (mask.element_size() != 1 or mask.numel() != p.mask_heads * p.T):
+        raise ValueError("mask must be [mask_heads, T] bytes")
+    for t in stats:
+        if t is not None and (t.dtype != torch.float32 or t.numel() != p.Hq * p.T):
+            raise ValueError("log-sum-exps must be float32 [Hq, T]")
+    here = torch.cuda.current_device()
+    for t in (k, seq_start, pos, mask, *(r for r, _ in rows), *stats):
+        if t is not None and t.device.index != here:
+            raise ValueError("tensors must be on the current device, whose stream the call is enqueued on")
+
+
+def l2a_cache_write(p: l2a_params, c: l2a_cache, k, v, seq_start, pos) -> None:
+    _check_packed(p, c, seq_start, pos, ((k, p.Hkv), (v, p.Hkv)))
+    rc = lib().l2a_cache_write(ctypes.byref(p), ctypes.byref(c), _ptr(k), _ptr(v), _ptr(seq_start), _ptr(pos), _stream())
+    if rc != 0:
+        raise L2AError(rc, "l2a_cache_write")
+
+
+def l2a_cache_read(p: l2a_params, c: l2a_cache, seq_start, pos, k, v) -> None:
+    _check_packed(p, c, seq_start, pos, ((k, p.Hkv), (v, p.Hkv)))
+    rc = lib().l2a_cache_read(ctypes.byref(p), ctypes.byref(c), _ptr(seq_start), _ptr(pos), _ptr(k), _ptr(v), _stream())
+    if rc != 0:
+        raise L2AError(rc, "l2a_cache_read")
+
+
+def l2a_attn_extend(p: l2a_params, c: l2a_cache, q, seq_start, pos, mask, max_new: int, O, lse_local=None, lse_global=None,
+                    S_opt=None, A_opt=None, workspace=None) -> None:
+    _check_packed(p, c, seq_start, pos, ((q, p.Hq), (O, p.Hq), (S_opt, p.Hq), (A_opt, p.Hq)), mask, (lse_local, lse_global))
+    if workspace is None:
+        workspace = alloc_extend_workspace(p, c, max_new)
+    rc = lib().l2a_attn_extend(ctypes.byref(p), ctypes.byref(c), _ptr(q), _ptr(seq_start), _ptr(pos), _ptr(mask), max_new, _ptr(O),
+                               _ptr(lse_local), _ptr(lse_global), _ptr(S_opt), _ptr(A_opt), _ptr(workspace),
+                               workspace.numel() if workspace is not None else 0, _stream())
+    if rc != 0:
+        raise L2AError(rc, "l2a_attn_extend")
+
+
 def l2a_attn_fwd(p: l2a_params, q_loc, k_loc, v_loc, q_glb, k_glb, v_glb, row_idx, count, kblk_first_row, O,
                  lse_local, lse_global, S_opt=None, A_opt=None, workspace=None) -> None:
     rc = lib().l2a_attn_fwd(ctypes.byref(p), _ptr(q_loc), _ptr(k_loc), _ptr(v_loc), _ptr(q_glb), _ptr(k_glb),
@@ -216,6 +299,19 @@ def alloc_fwd(p: l2a_params, device="cuda", branches=True, alloc=None):
 
 def alloc_fwd_workspace(p: l2a_params, device="cuda", alloc=None):
     return _ws(lib().l2a_attn_workspace_bytes(ctypes.byref(p), 0), device, alloc)
+
+
+def alloc_extend_workspace(p: l2a_params, c: l2a_cache, max_new: int, alloc=None):
+    return _ws(lib().l2a_extend_workspace_bytes(ctypes.byref(p), ctypes.byref(c), max_new), c.tensors[0].device, alloc)
+
+
+def alloc_cache(p: l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", alloc=None) -> l2a_cache:
+    """A pool of pages and an empty table (all entries -1)."""
+    e = alloc or torch.empty
+    shape = (pages, p.Hkv, page_size, p.D)
+    k, v = (e(shape, dtype=torch.float8_e4m3fn if fp8 else torch.bfloat16, device=device) for _ in range(2))
+    ks, vs = (e(shape[:3] + (p.D // 32,), dtype=torch.uint8, device=device) if fp8 else None for _ in range(2))
+    return make_cache(k, v, e((p.B, max_pages), dtype=torch.int32, device=device).fill_(-1), ks, vs)
 
 
 def alloc_bwd(p: l2a_params, device="cuda", alloc=None):

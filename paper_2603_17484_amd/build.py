@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libl2a.so")
 
 SOURCES = ["l2a_api.hip", "route_compact.hip", "attn_fp32.hip", "attn_simple.hip", "util.hip", "attn_fwd_bf16.hip",
            "attn_bwd_dq_bf16.hip", "attn_bwd_dkdv_bf16.hip", "pack.hip", "router.hip", "attn_decode_bf16.hip",
-           "profile.hip"]
+           "attn_extend_bf16.hip", "cache.hip", "profile.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -137,6 +137,14 @@ int mfma_decode(const Geom& g, const void* q, const void* k, const void* v, cons
                 int mask_heads, int do_local, int do_global, int ring, float* part, void* O, void* S, void* A, float* lse_l,
                 float* lse_g, hipStream_t st);
 
+// ---- cache.hip, attn_extend_bf16.hip : a paged KV cache (paged.hpp) and the attention of new tokens over it
+struct Pages;
+int cache_rows(const Geom& g, const Pages& c, bool read, void* k, void* v, const int32_t* seq_start, const int32_t* pos, hipStream_t st);
+size_t extend_workspace(const Geom& g, int max_new);
+int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq_start, const int32_t* pos, const uint8_t* mask,
+                int mask_heads, int max_new, int do_local, int do_global, void* O, float* lse_l, float* lse_g, void* S, void* A,
+                void* workspace, hipStream_t st);
+
 // ---- pack.hip : layout pre-passes (token-minor copies for the matrix-core kernels)
 struct Fill {  // n 32-bit words of one value
     uint32_t* p;

@@ -1,6 +1,6 @@
 // C ABI of the L2A layer: argument checks and the launch sequence of each call.
 // Every step of the layer runs in the kernels of this library; nothing here computes.
-#include "common.hpp"
+#include "paged.hpp"
 
 #include <cmath>
 
@@ -28,6 +28,7 @@ int check_params(const l2a_params* p) {
 }
 
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
 Geom make_geom(const l2a_params& p) {
     Geom g;
@@ -93,6 +94,33 @@ size_t dkdv_part_bytes(const l2a_params& p) {
 size_t bwd_workspace_bytes(const l2a_params& p) {
     if (fp32_parts(p)) return 3 * delta_bytes(p) + fp32_dq_shared_bytes(make_geom(p));
     return 2 * delta_bytes(p) + (use_mfma(p) ? 2 * packed_set_bytes(p) + dkdv_part_bytes(p) : 0);
+}
+
+// What the calls on a paged cache have in common: the cache's description, and sizes the kernels are built for.
+int check_cache(const l2a_params* p, const l2a_cache* c) {
+    const int rc = check_params(p);
+    if (rc != L2A_OK) return rc;
+    if (!use_mfma(*p) || (p->flags & L2A_FLAG_RING_CACHE)) return L2A_ERR_UNSUPPORTED;
+    if (!c || !c->k || !c->v || !c->table) return L2A_ERR_NULL;
+    if (c->dtype != L2A_BF16 && c->dtype != L2A_FP8) return L2A_ERR_UNSUPPORTED;
+    if (c->dtype == L2A_FP8 && (!c->k_scale || !c->v_scale)) return L2A_ERR_NULL;
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return L2A_ERR_SHAPE;
+    if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 30)) return L2A_ERR_SHAPE;
+    if (misaligned(c->k) || misaligned(c->v) || (c->dtype == L2A_FP8 && (misaligned(c->k_scale) || misaligned(c->v_scale)))) return L2A_ERR_ALIGN;
+    if (misaligned4(c->table)) return L2A_ERR_ALIGN;
+    return L2A_OK;
+}
+Pages make_pages(const l2a_cache& c) {
+    int log2 = 0;
+    while ((1 << log2) < c.page_size) ++log2;
+    const bool fp8 = c.dtype == L2A_FP8;
+    return Pages{(char*)c.k, (char*)c.v, fp8 ? (unsigned char*)c.k_scale : nullptr, fp8 ? (unsigned char*)c.v_scale : nullptr, c.table,
+                 c.pages, log2, c.max_pages, fp8};
+}
+Geom packed_geom(const l2a_params& p, const Pages& c) {
+    Geom g = make_geom(p);
+    g.W = p.W < c.capacity() ? p.W : c.capacity();  // (p.T is no sequence's length)
+    return g;
 }
 
 }  // namespace
@@ -297,6 +325,51 @@ int l2a_attn_fwd(const l2a_params* p, const void* q_loc, const void* k_loc, cons
         if ((r = fwd_branch(rs, q_glb, k_glb, v_glb, vt_glb, out)) != L2A_OK) return r;
     }
     return L2A_OK;
+}
+
+int l2a_cache_write(const l2a_params* p, const l2a_cache* c, const void* k, const void* v, const int32_t* seq_start,
+                    const int32_t* pos, void* stream) {
+    const int rc = check_cache(p, c);
+    if (rc != L2A_OK) return rc;
+    if (!k || !v || !seq_start || !pos) return L2A_ERR_NULL;
+    if (misaligned(k) || misaligned(v) || misaligned4(seq_start) || misaligned4(pos)) return L2A_ERR_ALIGN;
+    return cache_rows(make_geom(*p), make_pages(*c), false, (void*)k, (void*)v, seq_start, pos, (hipStream_t)stream);
+}
+
+int l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* seq_start, const int32_t* pos, void* k, void* v,
+                   void* stream) {
+    const int rc = check_cache(p, c);
+    if (rc != L2A_OK) return rc;
+    if (!k || !v || !seq_start || !pos) return L2A_ERR_NULL;
+    if (misaligned(k) || misaligned(v) || misaligned4(seq_start) || misaligned4(pos)) return L2A_ERR_ALIGN;
+    return cache_rows(make_geom(*p), make_pages(*c), true, k, v, seq_start, pos, (hipStream_t)stream);
+}
+
+size_t l2a_extend_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_new) {
+    if (check_cache(p, c) != L2A_OK || max_new < 1) return 0;
+    return extend_workspace(packed_geom(*p, make_pages(*c)), max_new);
+}
+
+int l2a_attn_extend(const l2a_params* p, const l2a_cache* c, const void* q, const int32_t* seq_start, const int32_t* pos,
+                    const uint8_t* mask, int32_t max_new, void* O, float* lse_local, float* lse_global, void* S_opt,
+                    void* A_opt, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_cache(p, c);
+    if (rc != L2A_OK) return rc;
+    if (max_new < 1) return L2A_ERR_SHAPE;
+    const bool dense = p->flags & L2A_FLAG_DENSE, do_local = !(p->flags & L2A_FLAG_SKIP_LOCAL), do_global = !(p->flags & L2A_FLAG_SKIP_GLOBAL);
+    if (!q || !seq_start || !pos || !O || (do_global && !dense && !mask)) return L2A_ERR_NULL;
+    const void* ptrs[] = {q, O, S_opt, A_opt};
+    for (const void* x : ptrs)
+        if (x && misaligned(x)) return L2A_ERR_ALIGN;
+    const void* words[] = {seq_start, pos, lse_local, lse_global};
+    for (const void* x : words)
+        if (x && misaligned4(x)) return L2A_ERR_ALIGN;
+    const Pages pages = make_pages(*c);
+    const Geom g = packed_geom(*p, pages);
+    if (!workspace || workspace_bytes < extend_workspace(g, max_new)) return L2A_ERR_WORKSPACE;
+    if (misaligned(workspace)) return L2A_ERR_ALIGN;
+    return mfma_extend(g, pages, q, seq_start, pos, dense ? nullptr : mask, p->mask_heads, max_new, do_local, do_global, O, lse_local,
+                       lse_global, S_opt, A_opt, workspace, (hipStream_t)stream);
 }
 
 int l2a_attn_bwd(const l2a_params* p, const void* dO, const void* q_loc, const void* k_loc,

@@ -1,0 +1,184 @@
+"""The operators on a paged KV cache against plain 64-bit forms: rows written (bits) and read back, and the attention of new tokens
+over the pages -- single tokens, drafts, chunks, mixtures -- at the sizes, masks and pages where it can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_17484_amd import binding as B
+from paper_2603_17484_amd.runner import GuardedAllocator, to_host
+from tests.paged_helpers import D, E4M3, SENTINEL, Step, bits, cache_on_gpu, check_extend, dequantise, quantise, up
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------
+# rows written and read back
+# ------------------------------------------------------------------------------------------
+ROWS = [  # new, cached, KV heads, page, fp8, tokens before the first and behind the last sequence
+    ([1], [0], 1, 16, False, 0, 0), ([1], [0], 1, 16, True, 0, 0), ([5, 0, 1, 33], [15, 7, 16, 0], 4, 16, False, 2, 3),
+    ([5, 0, 1, 33], [15, 7, 16, 0], 4, 16, True, 2, 3), ([300], [77], 8, 64, True, 0, 5), ([300], [77], 3, 32, False, 7, 0),
+    ([1] * 70, [3 * i for i in range(70)], 2, 16, True, 0, 0), ([0, 0, 3, 0], [0, 0, 1022, 0], 2, 1024, True, 0, 0)]
+
+
+@pytest.mark.parametrize("new,cached,Hkv,page,fp8,lead,tail", ROWS)
+def test_rows_are_written_and_read_back(new, cached, Hkv, page, fp8, lead, tail):
+    s = Step(new, cached, Hkv, Hkv, 4, page, fp8, seed=len(new) + page, lead=lead, tail=tail)
+    alloc = GuardedAllocator()
+    none = [0] * s.B
+    p, c = cache_on_gpu(s, alloc, s.pool(s.k, [None] * s.B, none), s.pool(s.v, [None] * s.B, none))
+    packed = []
+    for rows in (s.k, s.v):
+        x = np.full((s.N, Hkv, D), np.nan)
+        for b in range(s.B):
+            x[s.start[b]:s.start[b + 1]] = rows[b][cached[b]:]
+        packed.append(x)
+    start, pos = up(s.start), up(np.array(cached, np.int32))
+    B.l2a_cache_write(p, c, *(up(x, torch.bfloat16) for x in packed), start, pos)
+    torch.cuda.synchronize()
+    alloc.check()
+    # the new rows and nothing else
+    for rows, pool, scale in ((s.k, c.tensors[0], c.tensors[2]), (s.v, c.tensors[1], c.tensors[3])):
+        x, e = s.pool(rows, [None] * s.B, none)
+        for b in range(s.B):
+            for t in range(cached[b], cached[b] + new[b]):
+                page_, at = s.place(b, t)
+                if fp8:
+                    x[page_, :, at], e[page_, :, at] = quantise(rows[b][t])
+                else:
+                    x[page_, :, at] = bits(rows[b][t])
+        assert np.array_equal(pool.view(torch.uint8).cpu().numpy(), x.view(np.uint8).reshape(*x.shape[:-1], -1))
+        if fp8:
+            assert np.array_equal(scale.cpu().numpy(), e)
+    # read back, with rows of nobody left alone
+    back = [alloc((s.N, Hkv, D), torch.bfloat16).fill_(SENTINEL) for _ in range(2)]
+    B.l2a_cache_read(p, c, start, pos, *back)
+    torch.cuda.synchronize()
+    alloc.check()
+    for got, want in zip(back, packed):
+        got = to_host(got)
+        want = dequantise(*quantise(np.nan_to_num(want))) if fp8 else want
+        assert np.array_equal(got[lead:s.N - tail], want[lead:s.N - tail])
+        assert (got[:lead] == SENTINEL).all() and (got[s.N - tail:] == SENTINEL).all()
+
+
+def write_fp8(x):
+    """x [N, 128] through a cache of one head and pages of 16: (bytes, exponents, values read back)."""
+    n = len(x)
+    p = B.make_params(1, n, 1, 1, D, 4)
+    pages = -(-n // 16)
+    c = B.alloc_cache(p, pages, 16, pages, True)
+    c.tensors[4].copy_(torch.arange(pages, dtype=torch.int32))
+    t = torch.from_numpy(x).bfloat16().cuda().view(n, 1, D)
+    start, pos = torch.tensor([0, n], dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32).cuda()
+    B.l2a_cache_write(p, c, t, t.clone(), start, pos)
+    k, v = torch.empty_like(t), torch.empty_like(t)
+    B.l2a_cache_read(p, c, start, pos, k, v)
+    code, code_v = (x.view(torch.uint8).cpu().numpy().reshape(-1, D)[:n] for x in c.tensors[:2])
+    assert np.array_equal(code, code_v) and torch.equal(k.view(torch.int16), v.view(torch.int16))
+    return code, c.tensors[2].cpu().numpy().reshape(-1, 4)[:n], to_host(k).reshape(n, D)
+
+
+def test_every_finite_bf16_number_is_rounded_to_nearest():
+    """All of them beside block maxima that give them every place on the e4m3 grid: itself, and 1, 1.75, 1.7578125 times 2^j."""
+    every = (np.arange(0x7F80, dtype=np.uint32) << 16).view(np.float32).astype(np.float64)
+    assert np.isfinite(every).all()
+    rows = []
+    for top in (0.0, 1.0, 448.0, 450.0, 1.7578125 * 2.0 ** 20, 2.0 ** -110, 2.0 ** 127):
+        x = every[every <= top] if top else every
+        x = x[-31 * 4 * 800:] if top else x
+        x = np.concatenate([x, np.zeros((-len(x)) % 31)]).reshape(-1, 31)
+        x = np.concatenate([x, np.full((len(x), 1), top)], 1) * np.where(np.arange(32) % 2, -1, 1)
+        rows.append(x)
+    x = np.concatenate(rows)
+    x = np.concatenate([x, np.zeros(((-len(x)) % 4, 32))]).reshape(-1, D)
+    code, e, back = write_fp8(x)
+    want, we = quantise(x)
+    assert np.array_equal(e, we)
+    assert np.array_equal(code, want), np.argwhere(code != want)[:5]
+    assert np.array_equal(back, dequantise(want, we))
+
+
+def test_nan_and_infinity_become_nan_and_stay_in_their_places():
+    x = np.ones((2, D))
+    x[0, 5], x[0, 40], x[1, 100] = np.nan, np.inf, -np.inf
+    code, e, back = write_fp8(x)
+    for r, c in ((0, 5), (0, 40), (1, 100)):
+        assert (code[r, c] & 127) == 127 and np.isnan(back[r, c])
+    assert np.isnan(E4M3[code]).sum() == 3
+    assert (back[0, :5] == 1).all() and (back[0, 64:] == 1).all()  # a NaN does not count as its block's largest
+
+
+def test_rows_outside_the_table_or_the_pool_are_skipped():
+    s = Step([20, 4, 6], [30, 0, 5], 2, 2, 4, 16, seed=3)
+    s.table[1, 0], s.table[2, 0] = -5, s.pages
+    alloc = GuardedAllocator()
+    p, c = cache_on_gpu(s, alloc, s.pool(s.k[:1], [None], [0]), s.pool(s.v[:1], [None], [0]))
+    before = [t.clone() for t in c.tensors[:2]]
+    x = torch.ones(s.N, 2, D, dtype=torch.bfloat16, device="cuda")
+    out = [alloc((s.N, 2, D), torch.bfloat16).fill_(SENTINEL) for _ in range(2)]
+    cap = s.max_pages * s.page
+    for pos in ([cap - 3, 0, 0], [-19, 0, 0], [2 ** 31 - 1, -2 ** 31, 0]):
+        pos_t = torch.tensor(pos, dtype=torch.int32, device="cuda")
+        s.table[0, :] = -1
+        s.table[0, 0] = 0
+        c.tensors[4].copy_(up(s.table))
+        B.l2a_cache_write(p, c, x, x, up(s.start), pos_t)
+        B.l2a_cache_read(p, c, up(s.start), pos_t, *out)
+    torch.cuda.synchronize()
+    alloc.check()
+    got = c.tensors[0].float()
+    # token 19 of sequence 0 at position 0 is the only one with a place
+    changed = (c.tensors[0].view(torch.int16) != before[0].view(torch.int16)).flatten(1).any(1).nonzero().flatten().tolist()
+    assert changed == [0] and bool((got[0, :, 0] == 1).all())
+    assert bool((out[0][19] == 1).all()) and bool((out[0][:19] == SENTINEL).all()) and bool((out[0][20:] == SENTINEL).all())
+    for bad in ([5, 3, 1, 0], [-9, 2 ** 31 - 1, -4, 7], [24, 24, 24, 24]):  # starts that do not ascend, or lie outside
+        B.l2a_cache_write(p, c, x, x, up(np.array(bad, np.int32)), up(np.array([0, 0, 0], np.int32)))
+    torch.cuda.synchronize()
+    alloc.check()
+
+
+# ------------------------------------------------------------------------------------------
+# attention of new tokens over the pages
+# ------------------------------------------------------------------------------------------
+EXTEND = {
+    "first token": dict(new=[1], cached=[0], Hq=4, Hkv=2, W=100, f=1.0),
+    "one token": dict(new=[1], cached=[700], Hq=28, Hkv=4, W=100, f=1.0),
+    "one token, not routed": dict(new=[1], cached=[700], Hq=28, Hkv=4, W=100, f=0.0),
+    "single tokens": dict(new=[1] * 9, cached=[0, 1, 15, 16, 63, 64, 65, 500, 1300], Hq=16, Hkv=2, W=64, f=0.5),
+    "single tokens, decisions per head": dict(new=[1] * 7, cached=[5, 100, 200, 300, 401, 502, 900], Hq=14, Hkv=2, W=130, f=0.5, Hm=14),
+    "single tokens, fp8": dict(new=[1] * 6, cached=[0, 31, 127, 128, 700, 900], Hq=32, Hkv=8, W=100, f=0.6, fp8=True, page=64),
+    "many sequences": dict(new=[1] * 300, cached=[(i * 37) % 90 for i in range(300)], Hq=4, Hkv=2, W=20, f=0.4),
+    "drafts": dict(new=[5, 3, 0, 8], cached=[100, 333, 50, 0], Hq=28, Hkv=4, W=64, f=0.5),
+    "drafts, fp8": dict(new=[5, 3, 0, 8], cached=[100, 333, 50, 0], Hq=28, Hkv=4, W=64, f=0.5, fp8=True, page=32, Hm=4),
+    "first chunk": dict(new=[333], cached=[0], Hq=4, Hkv=2, W=50, f=0.3),
+    "chunk": dict(new=[300], cached=[600], Hq=4, Hkv=1, W=200, f=0.3),
+    "chunk, fp8": dict(new=[300], cached=[600], Hq=4, Hkv=1, W=200, f=0.3, fp8=True, page=128),
+    "chunk, decisions per head": dict(new=[200], cached=[150], Hq=8, Hkv=2, W=100, f=0.4, Hm=8, page=32),
+    "chunks and tokens": dict(new=[1, 129, 1, 0, 64, 1], cached=[400, 77, 0, 9, 64, 1023], Hq=6, Hkv=2, W=90, f=0.3, lead=3, tail=2),
+    "chunks and tokens, fp8": dict(new=[1, 129, 1, 0, 64, 1], cached=[400, 77, 0, 9, 64, 1023], Hq=6, Hkv=2, W=90, f=0.3, lead=3, tail=2, fp8=True),
+    "window of one key": dict(new=[70, 1], cached=[130, 99], Hq=4, Hkv=2, W=0, f=0.3),
+    "window spans all": dict(new=[70, 1], cached=[130, 99], Hq=4, Hkv=2, W=4096, f=0.4),
+    "window begins inside the chunk": dict(new=[150], cached=[20], Hq=4, Hkv=2, W=63, f=0.4),
+    "all routed": dict(new=[90], cached=[200], Hq=4, Hkv=2, W=64, f=1.0),
+    "none routed": dict(new=[90], cached=[200], Hq=4, Hkv=2, W=64, f=0.0),
+    "one group of sixteen": dict(new=[20, 1], cached=[200, 77], Hq=16, Hkv=1, W=64, f=0.4),
+    "as many heads": dict(new=[40, 1], cached=[100, 77], Hq=3, Hkv=3, W=64, f=0.4, Hm=3),
+    "large scores": dict(new=[60], cached=[200], Hq=4, Hkv=2, W=64, f=0.5, scale=6.0),
+}
+
+
+@pytest.mark.parametrize("name", EXTEND)
+def test_extend(name):
+    check_extend(Step(**EXTEND[name], seed=len(name)))
+
+
+@pytest.mark.parametrize("flags", [B.L2A_FLAG_DENSE, B.L2A_FLAG_SKIP_GLOBAL, B.L2A_FLAG_SKIP_LOCAL, B.L2A_FLAG_SKIP_LOCAL | B.L2A_FLAG_DENSE,
+                                   B.L2A_FLAG_SKIP_GLOBAL | B.L2A_FLAG_DENSE])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_flags(flags, fp8):
+    check_extend(Step([40, 1, 9], [100, 77, 0], 8, 2, 50, 16, fp8, 8, 0.4, seed=flags), flags)
+
+
+def test_only_the_output_is_wanted_and_a_scale_of_its_own():
+    check_extend(Step([40, 1], [100, 300], 8, 2, 50, seed=1), optional=False)
+    check_extend(Step([40, 1], [100, 300], 8, 2, 50, seed=2), scale=0.3)
