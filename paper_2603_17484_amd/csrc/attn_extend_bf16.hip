@@ -26,12 +26,14 @@ using plan::Seq;
 
 constexpr int kPart = kD + 4;  // floats of a row's sums: maximum (log2 units), sum, 2 unused, O[128]
 
-struct Tile {
+struct Tile {  // 64 bytes
     long long start;  // on the line
     int blocks;
-    int pair, kind;   // b * Hkv + KV head; plan::kWindow or kPrefix
+    int b, hk, kind;  // plan::kWindow or kPrefix
     int first, rows;  // of the sequence's rows, or of its list
     int lo, hi;       // keys
+    int pos0, pos1;   // positions of the first and last row
+    Seq s;
     int pad;
 };
 struct Head {
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                 const int pair = p0 + lo, b = pair / gm.Hkv, hk = pair - b * gm.Hkv;
                 const Seq s = seq_of(a, b);
                 const int windows = window_tiles(a, s), within = i - (lo ? ends[lo - 1] : 0), rows = s.n * G;
-                t.pair = pair;
+                t.b = b, t.hk = hk, t.s = s;
                 t.kind = within < windows ? plan::kWindow : plan::kPrefix;
                 t.first = (t.kind == plan::kWindow ? within : within - windows) * a.tile_rows;
                 t.rows = min(a.tile_rows, (t.kind == plan::kWindow ? rows : min(a.listed[pair], rows)) - t.first);
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                     const int32_t* list = list_of(a, a.list, s, hk);
                     c0 = plan::clamp(list[c0], 0, rows - 1), c1 = plan::clamp(list[c1], 0, rows - 1);
                 }
-                const Range k = plan::tile_keys(t.kind, s.pos + c0 / G, s.pos + c1 / G, gm.W);
+                t.pos0 = s.pos + c0 / G, t.pos1 = s.pos + c1 / G;
+                const Range k = plan::tile_keys(t.kind, t.pos0, t.pos1, gm.W);
                 t.lo = k.lo, t.hi = k.hi;
                 t.blocks = plan::tile_blocks(k);
             }
@@ -201,13 +204,59 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     }
 }
 
-__device__ __forceinline__ void dma16_at(const void* lane_src, unsigned lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(lane_src) : "memory");
+// Blocks of keys in shared memory: 4 rows of 256 bytes, the keys of one load instruction, are 1024 bytes; the next 4 follow kFour
+// further on.  Within them the 16-byte chunk c of row r lies at 256 (c / 4) + 64 r + 16 (c mod 4).  Both ways of reading, K's rows 16 bytes
+// a lane and V's columns through the transposing read, touch every bank once, and an operand's place is one lane's number
+// plus constants: they are the instructions' offsets.  (With the chunks of a row permuted by an exclusive or instead, a block's operands took 16
+// registers and as many additions.)
+constexpr int kFour = 1024 + 16;
+constexpr int kBlockBytes = kKeys / 4 * kFour;
+__device__ __forceinline__ constexpr int chunk_at(int row, int c) { return (row >> 2) * kFour + (row & 3) * 64 + (c >> 2) * 256 + (c & 3) * 16; }
+// this lane's part of the places, and the operands: 16 channels 16 ks .. of rows 32 half .. ; 32 channels 32 d .. of rows 16 step ..
+__device__ __forceinline__ unsigned k_lane(int lane) { return chunk_at(lane & 31, lane >> 5); }
+__device__ __forceinline__ unsigned v_lane(int lane) {
+    const int i = lane & 15;
+    return (lane >> 5) * kFour + (i >> 2) * 64 + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+}
+__device__ __forceinline__ bf16x8 k_operand(lds_cptr at, int ks, int half) {
+    return *(const __attribute__((address_space(3))) bf16x8*)(at + half * 8 * kFour + (ks >> 1) * 256 + (ks & 1) * 32);
+}
+__device__ __forceinline__ bf16x8 v_operand(lds_cptr at, int d, int step) {
+    typedef s16x4 __attribute__((address_space(3)))* lds_ptr;
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + d * 256 + step * 4 * kFour));
+    const s16x4 v2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + d * 256 + (step * 4 + 2) * kFour));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// The row and the 16 bytes of it that a lane loads, of the 4 (e4m3: 8) rows of an instruction.  e4m3: so that a lane's 16 elements become
+// two chunks whose stores, eight lanes at a time, touch every bank once.
+template <bool FP8>
+__device__ __forceinline__ int load_row(int lane) { return FP8 ? ((lane >> 1) & 3) + 4 * (lane >> 5) : (lane >> 2) & 3; }
+template <bool FP8>
+__device__ __forceinline__ int load_chunk(int lane) { return FP8 ? (lane & 1) + 2 * ((lane >> 3) & 3) : (lane >> 4) * 4 + (lane & 3); }
+// e4m3: a lane's 16 elements of `row`, with the exponents of the row, become bf16
+__device__ __forceinline__ void store_converted(const u32x4& x, uint32_t exponents, char* block, int row, int lane) {
+    const int c = load_chunk<true>(lane);
+    u32x4 y[2];
+    dequantise16(x, exponent_value((exponents >> (8 * (c >> 1))) & 0xffu), y);
+    u32x4* const at = reinterpret_cast<u32x4*>(block + chunk_at(row, 2 * c));
+    at[0] = y[0], at[1] = y[1];
 }
 
-struct ExtendLds {
-    __bf16 k[2][kKeys * 128];
-    __bf16 v[2][kKeys * 128];
+// Shared memory.  A stage holds K of one block, V of another; blocks are loaded three walks of the loop ahead of their use.
+constexpr int kWaves = 8;  // of a workgroup: up to 32 rows each
+template <bool FP8>
+struct ExtendLds;
+template <>
+struct ExtendLds<false> {
+    static constexpr int kK = 5, kV = 4;
+    char k[kK][kBlockBytes], v[kV][kBlockBytes];
+};
+template <>
+struct ExtendLds<true> {  // e4m3 as loaded, each wavefront's pieces its own, and the bf16 blocks made of them
+    static constexpr int kK = 3, kV = 2, kRaw = 3;
+    char k[kK][kBlockBytes], v[kV][kBlockBytes];
+    char raw_k[kRaw][kWaves][1024], raw_v[kRaw][kWaves][1024];
+    uint32_t raw_ks[kRaw][kWaves][64], raw_vs[kRaw][kWaves][64];
 };
 
 // A row's result: s (x), a (y), their log-sum-exps, four channels a lane
@@ -223,194 +272,561 @@ __device__ __forceinline__ void store_row(const ExtendArgs& a, int token, int he
     }
 }
 
-template <bool FP8, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void extend_kernel(ExtendArgs a) {
-    __shared__ __attribute__((aligned(1024))) ExtendLds lds;
-    const Geom& gm = a.gm;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 31, h = lane >> 5, G = gm.G;
-    // workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring stretches
-    const int w = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);
-    const Head line = *a.head;
-    if ((long long)w * line.per >= line.total) return;
-    const long long x1 = (long long)(w + 1) * line.per;
+#define FENCE() __builtin_amdgcn_sched_barrier(0)
+#define scalar __attribute__((address_space(4)))  // read through the scalar cache: the same for all lanes, written by earlier launches
 
-    for (int T = a.first_tile[w]; T < line.tiles; ++T) {
-        const Tile t = a.tiles[T];
-        if (t.start >= x1) break;
-        const plan::Piece piece = plan::piece(Place{t.start, t.blocks}, line.per, w);
-        if (piece.from == piece.to) continue;
-        const int b = t.pair / gm.Hkv, hk = t.pair - b * gm.Hkv;
-        const Seq s = seq_of(a, b);
-        const int32_t* table = a.c.table + (size_t)b * a.c.max_pages;
-
-        // ---- this lane's row (rows past the end repeat the last one: computed, never written)
-        const int r = wave * 32 + n;
-        const bool valid = r < t.rows, wave_on = wave * 32 < t.rows;
-        int code = t.first + min(r, t.rows - 1);
-        if (t.kind == plan::kPrefix) code = plan::clamp(list_of(a, a.list, s, hk)[code], 0, s.n * G - 1);
-        const int local_tok = code / G, g = code - local_tok * G, head = hk * G + g, token = s.start + local_tok, pos = s.pos + local_tok;
-        const Range keys = plan::row_keys(t.kind, pos, gm.W);
-        const int first_lo = __builtin_amdgcn_readlane(keys.lo, 0), last_lo = __builtin_amdgcn_readlane(keys.lo, 31);
-        const int first_hi = __builtin_amdgcn_readlane(keys.hi, 0), last_hi = __builtin_amdgcn_readlane(keys.hi, 31);
-        bf16x8 qreg[8];
-        const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
+template <typename X>
+__device__ __forceinline__ X uniform(const X* p) {
+    struct Words {
+        int w[sizeof(X) / 4];
+    } x;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+    for (unsigned i = 0; i < sizeof(X) / 4; ++i) x.w[i] = ((const scalar int*)(uintptr_t)p)[i];
+    return __builtin_bit_cast(X, x);
+}
 
-        // ---- loads.  Keys out of the tile's range (before its first row's window: their pages may have been given back; behind its
-        // last row: not written yet) repeat the nearest one in it: always masked, and what lies in such rows must not meet a zero weight
-        const int jb0 = t.lo / kKeys + piece.from, jb1 = t.lo / kKeys + piece.to;  // blocks jb0 .. jb1 - 1
-        auto row_at = [&](int key) __attribute__((always_inline)) {
-            key = plan::clamp(key, t.lo, t.hi);
-            const int page = plan::clamp(table[key >> a.c.page_log2], 0, a.c.pages - 1);
-            return pool_row(a.c, gm.Hkv, page, hk, key);
-        };
-        constexpr int NL = 16 / NW;  // bf16: instructions of a wavefront per K or V block, 4 rows each
-        constexpr int NR = 8 / NW;   // e4m3: the same, 8 rows each
-        u32x4 kx[NR], vx[NR];
-        uint32_t kse[NR], vse[NR];
-        auto load = [&](int jb, int buf) __attribute__((always_inline)) {
+// A number that wraps around
+__device__ __forceinline__ int next(int i, int n) { return i + 1 == n ? 0 : i + 1; }
+
+// The blocks of a piece on their way to LDS.  Block i + 1 of K and block i of V go together (group i): a block's scores are computed
+// before the block ahead of it is multiplied with V.
+template <bool FP8>
+struct Loader {
+    typedef ExtendLds<FP8> Lds;
+    // one instruction of a wavefront loads 1024 bytes, rows that lie in one page: 4 of bf16, 8 of e4m3
+    static constexpr int kRows = FP8 ? 8 : 4, kEach = kKeys / (kRows * kWaves);
+    static constexpr int kGroup = 4;  // instructions of a group: K and V, two each (e4m3: elements and exponents)
+    static_assert(kEach * (FP8 ? 2 : 1) == 2, "the group's instructions");
+    const ExtendArgs& a;
+    Lds& lds;
+    const scalar int32_t* table;
+    int hk, lo, hi, jb0, blocks;  // keys lo .. hi may be read; blocks jb0 .. jb0 + blocks - 1
+    int wave, lane;
+    int issued, k_to, v_to;       // last group issued; where the next K and V go
+    size_t row_k[kEach], row_v[kEach];  // rows of the pool where the instructions of the next group's K and V begin
+
+    // Keys out of lo .. hi (before the first row's window: their pages may have been given back; behind the last row: not written yet)
+    // repeat the nearest key inside: always masked, and what lies in such rows must not meet a zero weight.
+    __device__ __forceinline__ int tile_row(int e) const { return (e * kWaves + wave) * kRows; }
+    __device__ __forceinline__ int first_key(int block, int e) const {
+        return plan::clamp((jb0 + block) * kKeys + tile_row(e), lo & -kRows, hi & -kRows);
+    }
+    __device__ __forceinline__ void find(int block) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int key = first_key(block, e);
+            row_k[e] = pool_row(a.c, a.gm.Hkv, plan::clamp(table[key >> a.c.page_log2], 0, a.c.pages - 1), hk, key);
+        }
+    }
+    __device__ __forceinline__ void issue_half(const char* pool, const unsigned char* scales, int block, const size_t* rows, char* tile, uint32_t* tile_scales) {
+        const int k0 = (jb0 + block) * kKeys;
+        const bool inside = k0 >= lo && k0 + kKeys - 1 <= hi;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int mine = load_row<FP8>(lane), row = tile_row(e) + mine;
+            unsigned off = mine;  // rows behind the instruction's first
+            if (!inside) off = plan::clamp(k0 + row, lo, hi) - first_key(block, e);
+            const unsigned to = __builtin_amdgcn_readfirstlane(lds_offset(tile)) + (e * kWaves + wave) * (FP8 ? 1024 : kFour);
             if constexpr (!FP8) {
-#pragma unroll
-                for (int i = 0; i < NL; ++i) {
-                    const int row = (i * NW + wave) * 4 + (lane >> 4);
-                    const size_t off = row_at(jb * kKeys + row) * (kD * 2) + (((lane & 15) ^ rm_tr_swizzle(row)) * 16);
-                    dma16_at(a.c.k + off, __builtin_amdgcn_readfirstlane(lds_offset(&lds.k[buf][0])) + (i * NW + wave) * 1024);
-                    dma16_at(a.c.v + off, __builtin_amdgcn_readfirstlane(lds_offset(&lds.v[buf][0])) + (i * NW + wave) * 1024);
-                }
+                dma16_so(pool + rows[e] * (kD * 2), off * (kD * 2) + load_chunk<FP8>(lane) * 16, to);
             } else {
-#pragma unroll
-                for (int i = 0; i < NR; ++i) {
-                    const size_t at = row_at(jb * kKeys + (i * NW + wave) * 8 + (lane >> 3));
-                    kx[i] = *reinterpret_cast<const u32x4*>(a.c.k + at * kD + (lane & 7) * 16);
-                    vx[i] = *reinterpret_cast<const u32x4*>(a.c.v + at * kD + (lane & 7) * 16);
-                    kse[i] = *reinterpret_cast<const uint32_t*>(a.c.ks + at * kRowScales);
-                    vse[i] = *reinterpret_cast<const uint32_t*>(a.c.vs + at * kRowScales);
-                }
+                dma16_so(pool + rows[e] * kD, off * kD + load_chunk<FP8>(lane) * 16, to);
+                dma4_so(scales + rows[e] * kRowScales, off * kRowScales, __builtin_amdgcn_readfirstlane(lds_offset(tile_scales)) + wave * 256);
             }
-        };
-        auto commit = [&](int buf) __attribute__((always_inline)) {  // e4m3: what was loaded becomes bf16 in LDS
-            if constexpr (FP8) {
+        }
+    }
+    __device__ __forceinline__ void issue() {  // the next group, as far as there is one
+        const int i = ++issued;
+        if (i + 1 < blocks) {
+            if constexpr (!FP8) issue_half(a.c.k, nullptr, i + 1, row_k, lds.k[k_to], nullptr);
+            else issue_half(a.c.k, a.c.ks, i + 1, row_k, lds.raw_k[k_to][0], lds.raw_ks[k_to][0]);
+        }
+        if (i >= 0 && i < blocks) {
+            if constexpr (!FP8) issue_half(a.c.v, nullptr, i, row_v, lds.v[v_to], nullptr);
+            else issue_half(a.c.v, a.c.vs, i, row_v, lds.raw_v[v_to][0], lds.raw_vs[v_to][0]);
+        }
+        k_to = next(k_to, FP8 ? ExtendLds<true>::kRaw : Lds::kK);
+        if (i >= 0) v_to = next(v_to, FP8 ? ExtendLds<true>::kRaw : Lds::kV);
 #pragma unroll
-                for (int i = 0; i < NR; ++i) {
-                    const int row = (i * NW + wave) * 8 + (lane >> 3), c = 2 * (lane & 7), sh = 8 * ((lane & 7) >> 1);
-                    auto put = [&](const u32x4& x, uint32_t e, __bf16* tile) __attribute__((always_inline)) {
-                        u32x4 y[2];
-                        dequantise16(x, exponent_value((e >> sh) & 0xffu), y);
-                        *reinterpret_cast<u32x4*>(tile + row * 128 + ((c ^ rm_tr_swizzle(row)) * 8)) = y[0];
-                        *reinterpret_cast<u32x4*>(tile + row * 128 + (((c + 1) ^ rm_tr_swizzle(row)) * 8)) = y[1];
-                    };
-                    put(kx[i], kse[i], &lds.k[buf][0]);
-                    put(vx[i], vse[i], &lds.v[buf][0]);
-                }
-            }
-        };
+        for (int e = 0; e < kEach; ++e) row_v[e] = row_k[e];
+        find(min(i + 2, blocks - 1));
+    }
+    // Waits until at most the two last groups are on their way; those at the end have half their loads or none.
+    __device__ __forceinline__ void wait() const {
+        constexpr int half = kGroup / 2;
+        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * half) : "memory");
+        else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * half) : "memory");
+        else if (issued == blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(half) : "memory");
+        else dma_wait();
+    }
+    // e4m3: this wavefront's pieces of a group become bf16.
+    __device__ __forceinline__ void convert(const char* raw, const uint32_t* scales, char* block) const {
+        if constexpr (FP8)
+            store_converted(*reinterpret_cast<const u32x4*>(raw + wave * 1024 + lane * 16), scales[wave * 64 + lane], block,
+                            wave * 8 + load_row<true>(lane), lane);
+    }
+};
 
-        f32x16 oacc[4];
-        float m = -INFINITY, l = 0.f;
+// What a row has so far.  The maximum is one that some score had, not the largest: it moves when a score passes it by more than 2^kSlack
+// (weights have the same 8 bits at any size), so that the two lanes of a row compare only then, and sums are rarely scaled.
+constexpr float kSlack = 8.f;
+constexpr float kNone = -3.0e38f;  // no key seen yet
+struct RowSums {
+    f32x16 o[4];
+    float m = kNone, l = 0.f;
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[d][e] = 0.f;
-        const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-
-        __syncthreads();  // the buffers are free
-        load(jb0, 0);
-        if constexpr (FP8) {
-            commit(0);
-            if (jb0 + 1 < jb1) load(jb0 + 1, 0);
+            for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+        m = kNone, l = 0.f;
+    }
+    __device__ __forceinline__ void scale(float by) {
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] *= by;
+    }
+    // mx: the largest score of this lane's keys, in log2 units
+    __device__ __forceinline__ void look(float mx) {
+        if (__any(mx > m + kSlack)) {
+            const float mnew = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+            scale(fast_exp2(m - mnew));
+            m = mnew;
         }
-        for (int jb = jb0; jb < jb1; ++jb) {
-            const int cur = (jb - jb0) & 1;
-            if constexpr (!FP8) dma_wait();
-            __syncthreads();  // this block is there, and every wavefront is done with the other buffer
-            if constexpr (FP8) {
-                if (jb + 1 < jb1) commit(cur ^ 1);
-                if (jb + 2 < jb1) load(jb + 2, 0);
+    }
+};
+__device__ __forceinline__ float largest(const f32x16& s) {
+    float m[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) m[i] = fmaxf(fmaxf(s[3 * i], s[3 * i + 1]), s[3 * i + 2]);
+    return fmaxf(fmaxf(fmaxf(m[0], m[1]), m[2]), fmaxf(fmaxf(m[3], m[4]), s[15]));
+}
+
+// A tile of up to 32 rows, as decoding has them: bound by its loads.  Every wavefront takes 32 keys at a time, every eighth of the piece's,
+// through shared memory of its own and with sums of its own, so that none waits for another before the end, where the eight sums are joined.
+// (All wavefronts loading blocks of 64 keys for two of them to compute: 217 us for 64 sequences of 8K tokens in e4m3, 1.5 us a block.)
+constexpr int kSub = 32;
+template <bool FP8>
+__device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& lds, const Tile& t, const plan::Piece& piece, int w) {
+    const Geom& gm = a.gm;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, h = lane >> 5, G = gm.G, hk = t.hk;
+    const float c2 = gm.scale_log2;
+    const scalar int32_t* const table = (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages);
+    // row r of the tile: its code, and from it the token
+    auto code_of = [&](int r) __attribute__((always_inline)) {
+        const int at = t.first + min(r, t.rows - 1);
+        return t.kind == plan::kWindow ? at : plan::clamp(list_of(a, a.list, t.s, hk)[at], 0, t.s.n * G - 1);
+    };
+    const int jb0 = t.lo / kKeys + piece.from, jb1 = t.lo / kKeys + piece.to;
+    const int sb1 = min(2 * jb1, t.hi / kSub + 1), sb0 = max(2 * jb0, t.lo / kSub) + wave;  // sub-blocks sb0, sb0 + 8, .. below sb1
+
+    __syncthreads();  // LDS is free
+    constexpr int kSubBytes = kSub / 4 * kFour;
+    static_assert(sizeof(ExtendLds<FP8>) >= kWaves * 2 * kSubBytes, "room for every wavefront's keys");
+    char *const kt = reinterpret_cast<char*>(&lds) + wave * 2 * kSubBytes, *const vt = kt + kSubBytes;
+    const lds_cptr k_at = (lds_cptr)(uintptr_t)(lds_offset(kt) + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(lds_offset(vt) + v_lane(lane));
+    const unsigned k_to = __builtin_amdgcn_readfirstlane(lds_offset(kt)), v_to = __builtin_amdgcn_readfirstlane(lds_offset(vt));
+    constexpr int kRows = FP8 ? 8 : 4, kEach = kSub / kRows;  // rows of an instruction, which lie in one page; instructions
+    const int mine = load_row<FP8>(lane);
+    u32x4 kx[FP8 ? kEach : 1], vx[FP8 ? kEach : 1];
+    uint32_t kse[FP8 ? kEach : 1], vse[FP8 ? kEach : 1];
+    size_t rows[kEach];   // where the instructions' rows begin in the pool, and how far behind that this lane's row is
+    unsigned off[kEach];
+    // keys out of the tile's repeat the nearest one in it (see Loader)
+    auto find = [&](int sb) __attribute__((always_inline)) {
+        const int k0 = sb * kSub;
+        if (k0 >= t.lo && k0 + kSub - 1 <= t.hi) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const size_t row = pool_row(a.c, gm.Hkv, plan::clamp(table[(k0 + 16 * p) >> a.c.page_log2], 0, a.c.pages - 1), hk, k0 + 16 * p);
+#pragma unroll
+                for (int e = 0; e < kEach / 2; ++e) rows[p * (kEach / 2) + e] = row + e * kRows, off[p * (kEach / 2) + e] = mine;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int first = plan::clamp(k0 + e * kRows, t.lo & -kRows, t.hi & -kRows);
+                rows[e] = pool_row(a.c, gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), hk, first);
+                off[e] = plan::clamp(k0 + e * kRows + mine, t.lo, t.hi) - first;
+            }
+        }
+    };
+    auto load = [&](const char* pool, const unsigned char* scales, u32x4* x, uint32_t* se, unsigned to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            if constexpr (!FP8) {
+                dma16_so(pool + rows[e] * (kD * 2), off[e] * (kD * 2) + load_chunk<FP8>(lane) * 16, to + e * kFour);
             } else {
-                if (jb + 1 < jb1) load(jb + 1, cur ^ 1);
-            }
-            const int k0 = jb * kKeys;
-            if (!wave_on || k0 > last_hi || k0 + kKeys - 1 < first_lo) continue;
-            const bool masked = k0 + kKeys - 1 > first_hi || k0 < last_lo;
-            const __bf16 *kt = &lds.k[cur][0], *vt = &lds.v[cur][0];
-            f32x16 sc[2];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) sc[kb] = mfma32(rm_tr_row_operand(kt, kb * 32 + n, ks, h), qreg[ks], ks == 0 ? zero16 : sc[kb]);
-            if (masked) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int key = k0 + kb * 32 + c_row(e, h);
-                        sc[kb][e] = key >= keys.lo && key <= keys.hi ? sc[kb][e] : -INFINITY;
-                    }
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float mnew = fmaxf(m, mx * gm.scale_log2);
-            if (__any(mnew > m)) {
-                const float alpha = mnew > m ? fast_exp2(m - mnew) : 1.f;
-                l *= alpha;
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) oacc[d][e] *= alpha;
-                m = mnew;
-            }
-            const float negm = m == -INFINITY ? 0.f : -m;  // no key seen yet
-            const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                u32x4 p[2];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    f32x2 f = {fast_exp2(fmaf(sc[kb][e], gm.scale_log2, negm)), fast_exp2(fmaf(sc[kb][e + 1], gm.scale_log2, negm))};
-                    const bf16x2 pb = __builtin_convertvector(f, bf16x2);
-                    // the sum of the weights as the matrix cores see them, rounded to bf16: what they are divided by is exact for them
-                    l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, l, false);
-                    p[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pb);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        oacc[d] = mfma32(rm_tr_col_operand(vt, d, 2 * kb + i, lane), __builtin_bit_cast(bf16x8, p[i]), oacc[d]);
+                x[e] = *reinterpret_cast<const u32x4*>(pool + rows[e] * kD + off[e] * kD + load_chunk<FP8>(lane) * 16);
+                se[e] = *reinterpret_cast<const uint32_t*>(scales + rows[e] * kRowScales + off[e] * kRowScales);
             }
         }
+    };
+    auto convert = [&](const u32x4* x, const uint32_t* se, char* block) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) store_converted(x[e], se[e], block, e * kRows + mine, lane);
+    };
+    if (sb0 < sb1) {
+        find(sb0);
+        load(a.c.k, a.c.ks, kx, kse, k_to);
+        load(a.c.v, a.c.vs, vx, vse, v_to);
+    }
+    const int code = code_of(n), local_tok = code / G;
+    const Range keys = plan::row_keys(t.kind, t.s.pos + local_tok, gm.W);
+    bf16x8 qreg[8];
+    const __bf16* qp = a.q + ((size_t)(t.s.start + local_tok) * gm.Hq + hk * G + code - local_tok * G) * kD + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
+    const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+    RowSums row;
+    row.clear();
+    for (int sb = sb0; sb < sb1; sb += kWaves) {
+        const bool more = sb + kWaves < sb1;
+        if (more) find(sb + kWaves);
+        if constexpr (FP8) convert(kx, kse, kt);
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
+        bf16x8 op[8];
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) op[ks] = k_operand(k_at, ks, 0);
+        if constexpr (FP8) {
+            if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
+        }
+        FENCE();
+        f32x16 sc;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) sc = mfma32(op[ks], qreg[ks], ks == 0 ? zero16 : sc);
+        if constexpr (!FP8) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of K have returned
+            if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
+            else dma_wait();
+        } else {
+            convert(vx, vse, vt);
+            if (more) load(a.c.v, a.c.vs, vx, vse, v_to);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) op[i] = v_operand(v_at, i & 3, i >> 2);
+        FENCE();
+        const int k0 = sb * kSub;
+        if (k0 < lo_max || k0 + kSub - 1 > hi_min) {
+            const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
+        }
+        row.look(largest(sc) * c2);
+        u32x4 p[2];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            f32x2 f = {fast_exp2(fmaf(sc[e], c2, -row.m)), fast_exp2(fmaf(sc[e + 1], c2, -row.m))};
+            const bf16x2 pb = __builtin_convertvector(f, bf16x2);
+            row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
+            p[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pb);
+        }
+        if constexpr (!FP8) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of V have returned
+            if (more) load(a.c.v, a.c.vs, vx, vse, v_to);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(op[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
+    }
 
-        // ---- out
-        if (!valid) continue;
-        const float lt = l + __shfl_xor(l, 32);
-        const bool whole = piece.first && piece.last;
-        if (whole && t.kind == plan::kWindow && !(pos > gm.W && token_routed(a, token, head))) {
-            const bool routed = token_routed(a, token, head);  // its window is all there is: a = s
-            const float inv = 1.f / lt, lse = (m + __builtin_amdgcn_logf(lt)) * kLn2;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const f32x4 x = {oacc[d][e] * inv, oacc[d][e + 1] * inv, oacc[d][e + 2] * inv, oacc[d][e + 3] * inv};
-                    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                    store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
-                }
-            continue;
-        }
-        float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                           : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-        if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{m, lt};
+    // ---- the eight wavefronts' sums, joined: 16 threads per row, eight channels each
+    row.l += __shfl_xor(row.l, 32);
+    float* const sums = reinterpret_cast<float*>(&lds);  // [wave][row][kPart]
+    static_assert(sizeof(ExtendLds<FP8>) >= kWaves * 32 * kPart * sizeof(float), "room for the wavefronts' sums");
+    __syncthreads();  // every wavefront is done with its part of LDS
+    {
+        float* const at = sums + (wave * 32 + n) * kPart;
+        if (h == 0) *reinterpret_cast<f32x2*>(at) = f32x2{row.m, row.l};
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{oacc[d][e], oacc[d][e + 1], oacc[d][e + 2], oacc[d][e + 3]};
+                *reinterpret_cast<f32x4*>(at + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 4, c8 = (threadIdx.x & 15) * 8;
+    if (r >= t.rows) return;
+    float m = kNone, l = 0.f;
+    f32x2 ml[kWaves];
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+        ml[v] = *reinterpret_cast<const f32x2*>(sums + (v * 32 + r) * kPart);
+        m = fmaxf(m, ml[v][0]);
+    }
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+        const float by = fast_exp2(ml[v][0] - m);
+        const f32x4* const at = reinterpret_cast<const f32x4*>(sums + (v * 32 + r) * kPart + 4 + c8);
+        l = fmaf(ml[v][1], by, l);
+        x += at[0] * by, y += at[1] * by;
+    }
+    const int my_code = code_of(r), my_tok = my_code / G, head = hk * G + my_code - my_tok * G, token = t.s.start + my_tok;
+    const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
+    if (whole && t.kind == plan::kWindow && !(t.s.pos + my_tok > gm.W && routed)) {
+        const float inv = 1.f / l, lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
+        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+        x *= inv, y *= inv;
+        store_row(a, token, head, c8, x, routed ? x : z, lse, routed ? lse : -INFINITY);
+        store_row(a, token, head, c8 + 4, y, routed ? y : z, lse, routed ? lse : -INFINITY);
+    } else {
+        float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
+                           : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+        if (c8 == 0) *reinterpret_cast<f32x2*>(out) = f32x2{m, l};
+        *reinterpret_cast<f32x4*>(out + 4 + c8) = x;
+        *reinterpret_cast<f32x4*>(out + 4 + c8 + 4) = y;
+    }
+}
+
+template <bool FP8>
+__global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
+    __shared__ __attribute__((aligned(1024))) ExtendLds<FP8> lds;
+    const Geom& gm = a.gm;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, h = lane >> 5, G = gm.G;
+    const float c2 = gm.scale_log2;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+    // workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring stretches
+    const int w = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);
+    const Head line = uniform(a.head);
+    if ((long long)w * line.per >= line.total) return;
+    const long long x1 = (long long)(w + 1) * line.per;
+
+    for (int T = uniform(a.first_tile + w); T < line.tiles; ++T) {
+        const Tile t = uniform(a.tiles + T);
+        if (t.start >= x1) break;
+        const plan::Piece piece = plan::piece(Place{t.start, t.blocks}, line.per, w);
+        if (piece.from == piece.to) continue;
+        const int b = t.b, hk = t.hk;
+        const Seq s = t.s;
+        if (t.rows <= 32) {
+            few_rows<FP8>(a, lds, t, piece, w);
+            continue;
+        }
+
+        const int jb0 = t.lo / kKeys + piece.from, blocks = piece.to - piece.from;
+        __syncthreads();  // LDS is free
+        Loader<FP8> load{a, lds, (const scalar int32_t*)(a.c.table + (size_t)b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane, -2, 0, 0};
+        load.find(0);
+        load.issue();
+        load.issue();
+        load.issue();
+
+        // ---- this lane's row (rows past the end repeat the last one: computed, never written).  Up to 128 rows: wavefronts 4 .. 7 take
+        // the second half of the keys of every block for the rows of wavefronts 0 .. 3.
+        const bool halves = t.rows <= 32 * kWaves / 2;
+        const int r = (halves ? wave & 3 : wave) * 32 + n;
+        const bool valid = r < t.rows, wave_on = r - n < t.rows;
+        int code = t.first + min(r, t.rows - 1);
+        if (t.kind == plan::kPrefix) code = plan::clamp(list_of(a, a.list, s, hk)[code], 0, s.n * G - 1);
+        const int local_tok = code / G, g = code - local_tok * G, head = hk * G + g, token = s.start + local_tok, pos = s.pos + local_tok;
+        const Range keys = plan::row_keys(t.kind, pos, gm.W);
+        bf16x8 qreg[8];
+        const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
+        // blocks that every row of the tile sees whole: from `whole0` to `whole1` - 1
+        const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
+        const int whole0 = (lo_max + kKeys - 1) / kKeys, whole1 = (hi_min + 1) / kKeys;
+        // scores of 32 keys from k0 on, those out of the row's reach taken out
+        auto mask = [&](f32x16& sc, int k0) __attribute__((always_inline)) {
+            const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
+        };
+        auto masked = [&](int jb) __attribute__((always_inline)) { return jb < whole0 || jb >= whole1; };
+
+        RowSums row;
+        row.clear();
+        int kb = 0, vb = 0;  // buffers of block j
+        int raw = 0;
+        if constexpr (FP8) {
+            load.wait();
+            load.convert(lds.raw_k[0][0], lds.raw_ks[0][0], lds.k[0]);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load.issue();
+            load.wait();
+            if (blocks > 1) load.convert(lds.raw_k[1][0], lds.raw_ks[1][0], lds.k[1]);
+            load.convert(lds.raw_v[0][0], lds.raw_vs[0][0], lds.v[0]);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load.issue();
+            raw = 2;
+        } else {
+            load.issue();
+            load.wait();
+        }
+        __syncthreads();
+        // begins a block's work: more on its way, and e4m3 of the next group made bf16
+        auto begin = [&](int j) __attribute__((always_inline)) {
+            if constexpr (FP8) {
+                if (j + 1 < blocks) {
+                    load.wait();
+                    if (j + 2 < blocks) load.convert(lds.raw_k[raw][0], lds.raw_ks[raw][0], lds.k[kb == 0 ? 2 : kb - 1]);
+                    const int rv = raw == 0 ? 2 : raw - 1;  // V of a group lies one place behind its K
+                    load.convert(lds.raw_v[rv][0], lds.raw_vs[rv][0], lds.v[vb ^ 1]);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    raw = next(raw, 3);
+                }
+            }
+            load.issue();
+        };
+        auto end = [&](int j) __attribute__((always_inline)) {
+            if constexpr (!FP8) load.wait();
+            __syncthreads();
+            kb = next(kb, ExtendLds<FP8>::kK), vb = next(vb, ExtendLds<FP8>::kV);
+        };
+
+        const unsigned k_mine = k_lane(lane), v_mine = v_lane(lane);
+        auto k_block = [&](int buf) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(lds_offset(lds.k[buf]) + k_mine); };
+        auto v_block = [&](int buf) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(lds_offset(lds.v[buf]) + v_mine); };
+        // Weights of a pair of scores, rounded to bf16; the sum is that of the weights as the matrix cores see them, so that what
+        // they are divided by is exact for them.
+        auto weigh = [&](const f32x16& sc, int e) __attribute__((always_inline)) {
+            f32x2 f = {fast_exp2(fmaf(sc[e], c2, -row.m)), fast_exp2(fmaf(sc[e + 1], c2, -row.m))};
+            const bf16x2 pb = __builtin_convertvector(f, bf16x2);
+            row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
+            return __builtin_bit_cast(uint32_t, pb);
+        };
+        if (halves) {
+            // One half of 32 keys per wavefront and block, all operands read ahead; short of rows, the loads set the pace.
+            const int half = wave >> 2;
+            for (int j = 0; j < blocks; ++j) {
+                begin(j);
+                if (wave_on) {
+                    const lds_cptr ka = k_block(kb) + half * 8 * kFour, va = v_block(vb) + half * 8 * kFour;
+                    bf16x8 kop[8], vop[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) kop[i] = k_operand(ka, i, 0);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) vop[i] = v_operand(va, i & 3, i >> 2);
+                    FENCE();
+                    f32x16 sc;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) sc = mfma32(kop[ks], qreg[ks], ks == 0 ? zero16 : sc);
+                    if (masked(jb0 + j)) mask(sc, (jb0 + j) * kKeys + half * 32);
+                    row.look(largest(sc) * c2);
+                    u32x4 p[2];
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) p[e >> 3][(e & 7) >> 1] = weigh(sc, e);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(vop[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
+                }
+                end(j);
+            }
+        } else {
+            // All keys for 32 rows a wavefront.  While the weights of 32 keys are found on the vector units, the matrix cores compute the
+            // scores of the 32 keys after them, and then the product of these weights with V (slots of one matrix instruction each;
+            // operands are read kAhead slots before their use).
+            constexpr int kAhead = 2;
+            f32x16 sa, sb;
+            float mx;
+            auto half_block = [&](auto half_tag, f32x16& cur, f32x16& nxt, lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
+                constexpr int H = decltype(half_tag)::value;  // nxt: the block's second half, or the next block's first
+                row.look(mx);
+                bf16x8 op[16 + kAhead];
+                u32x4 p[2];
+                auto read = [&](auto oc) __attribute__((always_inline)) {
+                    constexpr int o = decltype(oc)::value;
+                    if constexpr (o < 8) op[o] = k_operand(ka, o, 1 - H);
+                    else if constexpr (o < 16) op[o] = v_operand(va, o & 3, 2 * H + ((o - 8) >> 2));
+                };
+                static_for<0, kAhead>([&](auto oc) { read(oc); });
+                FENCE();
+                static_for<0, 16>([&](auto sc_) __attribute__((always_inline)) {
+                    constexpr int slot = decltype(sc_)::value;
+                    if constexpr (slot < 8) nxt = mfma32(op[slot], qreg[slot], slot == 0 ? zero16 : nxt);
+                    else row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, p[(slot - 8) >> 2]), row.o[slot & 3]);
+                    read(std::integral_constant<int, slot + kAhead>{});
+                    static_for<0, 8>([&](auto qc) __attribute__((always_inline)) {
+                        constexpr int q = decltype(qc)::value;
+                        if constexpr ((3 * q) / 2 == slot) p[q >> 2][q & 3] = weigh(cur, 2 * q);
+                    });
+                    if constexpr (slot == 12) {
+                        if (masked_next) mask(nxt, k0_next);
+                        mx = largest(nxt) * c2;
+                    }
+                    FENCE();
+                });
+            };
+            {
+                const lds_cptr ka = k_block(kb);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) sa = mfma32(k_operand(ka, ks, 0), qreg[ks], ks == 0 ? zero16 : sa);
+            }
+            if (masked(jb0)) mask(sa, jb0 * kKeys);
+            mx = largest(sa) * c2;
+            for (int j = 0; j < blocks; ++j) {
+                begin(j);
+                const int jb = jb0 + j;
+                const lds_cptr va = v_block(vb);
+                half_block(std::integral_constant<int, 0>{}, sa, sb, k_block(kb), va, jb * kKeys + 32, masked(jb));
+                half_block(std::integral_constant<int, 1>{}, sb, sa, k_block(next(kb, ExtendLds<FP8>::kK)), va, (jb + 1) * kKeys, masked(jb + 1));
+                end(j);
+            }
+        }
+
+        // ---- out
+        row.l += __shfl_xor(row.l, 32);
+        if (halves) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
+            f32x4* const there = reinterpret_cast<f32x4*>(&lds) + (wave & 3) * (17 * 64) + lane;
+            if (wave_on && wave >= 4) {
+                there[0] = f32x4{row.m, row.l, 0.f, 0.f};
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) there[(1 + d * 4 + e / 4) * 64] = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
+            }
+            __syncthreads();
+            if (wave_on && wave < 4) {
+                const f32x4 ml = there[0];
+                const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew);
+                row.scale(fast_exp2(row.m - mnew));
+                row.m = mnew;
+                row.l = fmaf(ml[1], by, row.l);
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const f32x4 x = there[(1 + d * 4 + e / 4) * 64];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) row.o[d][e + i] = fmaf(x[i], by, row.o[d][e + i]);
+                    }
+            }
+        }
+        if (valid && (!halves || wave < 4)) {
+            const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
+            if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
+                const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
+                        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                        store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
+                    }
+            } else {
+                float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
+                                   : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+                if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4)
+                        *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
+            }
+        }
     }
 }
 
@@ -453,7 +869,21 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
         const Place p{a.tiles[T].start, a.tiles[T].blocks};
         const int f = plan::first_of(p, per), l = plan::last_of(p, per);
         if (f >= l) return false;
-        for (int w = f; w <= l; ++w) sums.join(a.slots + ((size_t)plan::slot(w, w == f) * a.tile_rows + r) * kPart, c4);
+        constexpr int kAhead = 8;  // loads of this many pieces on their way together (past the end the first is read again, for nobody)
+        for (int w0 = f; w0 <= l; w0 += kAhead) {
+            f32x2 ml[kAhead];
+            f32x4 x[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int w = w0 + i <= l ? w0 + i : w0;
+                const float* part = a.slots + ((size_t)plan::slot(w, w == f) * a.tile_rows + r) * kPart;
+                ml[i] = *reinterpret_cast<const f32x2*>(part);
+                x[i] = *reinterpret_cast<const f32x4*>(part + 4 + c4);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (w0 + i <= l) sums.join(ml[i][0], ml[i][1], x[i]);
+        }
         return true;
     };
     const f32x4 z = {0.f, 0.f, 0.f, 0.f};
@@ -474,7 +904,6 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
     store_row(a, token, head, c4, x, routed ? sums.value() : z, lse_l, routed ? sums.lse() : -INFINITY);
 }
 
-constexpr int kTileWaves = 8;
 constexpr int kWorkgroups = 256;  // one per CU
 
 // The workspace: sub-buffers at multiples of 256 bytes.
@@ -487,7 +916,7 @@ size_t lay_out(ExtendArgs& a, char* base) {
     };
     const size_t rows = (size_t)g.T * g.G, pairs = (size_t)g.B * g.Hkv;
     a.workgroups = kWorkgroups;
-    a.tile_rows = 32 * kTileWaves;
+    a.tile_rows = 32 * kWaves;
     a.most_tiles = (int)(2 * g.Hkv * (rows / a.tile_rows + g.B));
     take(a.head, 1);
     take(a.tiles, a.most_tiles);
@@ -536,8 +965,8 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     }
     {
         KernelTimer kt("extend", st);
-        if (c.fp8) hipLaunchKernelGGL((extend_kernel<true, kTileWaves>), dim3(a.workgroups), dim3(64 * kTileWaves), 0, st, a);
-        else hipLaunchKernelGGL((extend_kernel<false, kTileWaves>), dim3(a.workgroups), dim3(64 * kTileWaves), 0, st, a);
+        if (c.fp8) hipLaunchKernelGGL(extend_kernel<true>, dim3(a.workgroups), dim3(64 * kWaves), 0, st, a);
+        else hipLaunchKernelGGL(extend_kernel<false>, dim3(a.workgroups), dim3(64 * kWaves), 0, st, a);
     }
     {
         KernelTimer kt("extend_combine", st);
