@@ -28,17 +28,21 @@ constexpr int kPart = kD + 4;  // floats of a row's sums: maximum (log2 units), 
 
 struct Tile {  // 64 bytes
     long long start;  // on the line
-    int blocks;
+    int blocks, skip;  // there; blocks before these, which are segments
     int b, hk, kind;  // plan::kWindow or kPrefix
     int first, rows;  // of the sequence's rows, or of its list
     int lo, hi;       // keys
     int pos0, pos1;   // positions of the first and last row
     Seq s;
-    int pad;
+};
+struct Pair {  // a KV head of a sequence
+    int first_tile, listed;      // its first tile, windows first; rows with keys before the window
+    int segments, first_segment; // of each of its tiles of keys before the window; the first of them
 };
 struct Head {
-    long long total;
-    int per, tiles;
+    long long total;     // length of the line
+    int per, tiles;      // its stretches; tiles on it
+    int segments, blocks;  // workgroups that have a segment, and its blocks
 };
 
 struct ExtendArgs {
@@ -53,13 +57,13 @@ struct ExtendArgs {
     // workspace
     Head* head;
     Tile* tiles;
-    int most_tiles, workgroups, tile_rows;
-    int32_t* first_tile;  // [workgroups]
-    int32_t* pair_tile;   // [B * Hkv] index of the pair's first tile
-    int32_t* listed;      // [B * Hkv] rows with keys before the window
-    int32_t* list;        // [Hkv][T G], a sequence's from its first row on: row codes
+    int most_tiles, workgroups, tile_rows, few;  // few: no sequence has more than 32 rows per KV head, and no lists are made
+    int32_t* first_tile;  // [workgroups] of a stretch
+    int2* segment;        // [workgroups] tile and number
+    Pair* pairs;          // [B * Hkv]
+    int32_t* list;        // [Hkv][T G], a sequence's from its first row on: codes of the rows with keys before the window, ascending
     int32_t* rank;        // [Hkv][T G] place of a row in its list
-    int32_t* token_seq;   // [T]
+    int32_t* token_seq;   // [T] (few)
     float* slots;         // [2 * workgroups][tile_rows][kPart]
     float* parts[2];      // [T * Hq][kPart]: rows of whole tiles, by kind
 };
@@ -78,6 +82,24 @@ __device__ __forceinline__ int32_t* list_of(const ExtendArgs& a, int32_t* x, con
     return x + (size_t)hk * a.gm.T * a.gm.G + (size_t)s.start * a.gm.G;
 }
 
+// The code (token in the sequence, head in the group) of row i of a tile's kind.
+__device__ __forceinline__ int row_code(const ExtendArgs& a, const Tile& t, int i) {
+    if (a.few || t.kind == plan::kWindow) return i;
+    return plan::clamp(list_of(a, a.list, t.s, t.hk)[i], 0, t.s.n * a.gm.G - 1);
+}
+// A row's result: s (x), a (y), their log-sum-exps, four channels a lane
+__device__ __forceinline__ void store_row(const ExtendArgs& a, int token, int head, int c4, const f32x4& x, const f32x4& y, float lse_l, float lse_g) {
+    const size_t off = ((size_t)token * a.gm.Hq + head) * kD + c4;
+    *reinterpret_cast<bf16x4*>(a.O + off) = __builtin_convertvector(x + y, bf16x4);
+    if (a.S) *reinterpret_cast<bf16x4*>(a.S + off) = __builtin_convertvector(x, bf16x4);
+    if (a.A) *reinterpret_cast<bf16x4*>(a.A + off) = __builtin_convertvector(y, bf16x4);
+    if (c4 == 0) {
+        const size_t so = (size_t)head * a.gm.T + token;
+        if (a.lse_l) a.lse_l[so] = lse_l;
+        if (a.lse_g) a.lse_g[so] = lse_g;
+    }
+}
+
 // Every thread takes consecutive tokens: their decisions counted, the counts summed over the workgroup, the rows written.
 constexpr int kListThreads = 1024;
 __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a) {
@@ -85,8 +107,6 @@ __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a)
     const Geom& gm = a.gm;
     const int b = blockIdx.x / gm.Hkv, hk = blockIdx.x - b * gm.Hkv, G = gm.G;
     const Seq s = seq_of(a, b);
-    if (hk == 0)
-        for (int i = threadIdx.x; i < s.n; i += kListThreads) a.token_seq[s.start + i] = b;
     const int skip = plan::rows_without_prefix(s, G, gm.W) / G, n = s.n - skip;
     const int each = (n + kListThreads - 1) / kListThreads;
     const int t0 = min(skip + (int)threadIdx.x * each, s.n), t1 = min(t0 + each, s.n);
@@ -106,7 +126,7 @@ __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a)
         if (w < wave) at += sums[w];
         total += sums[w];
     }
-    if (threadIdx.x == 0) a.listed[blockIdx.x] = total;
+    if (threadIdx.x == 0) a.pairs[blockIdx.x].listed = total;
     int32_t *list = list_of(a, a.list, s, hk), *rank = list_of(a, a.rank, s, hk);
     for (int t = t0; t < t1; ++t)
         for (int g = 0; g < G; ++g)
@@ -114,15 +134,19 @@ __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a)
                 rank[t * G + g] = at;
                 list[at++] = t * G + g;
             }
+    if (a.do_local) return;
+    const f32x4 z = {0.f, 0.f, 0.f, 0.f};  // without windows, rows that are not routed have no tile
+    for (int r = threadIdx.x >> 5; r < s.n * G; r += kListThreads / 32)
+        if (!token_routed(a, s.start + r / G, hk * G + r % G)) store_row(a, s.start + r / G, hk * G + r % G, (threadIdx.x & 31) * 4, z, z, -INFINITY, -INFINITY);
 }
 
 // Sum over the threads before this one, and over all of them.
 constexpr int kPlanThreads = 1024;
-__device__ __forceinline__ void scan(long long x, long long* sums, long long& before, long long& total) {
+__device__ __forceinline__ void scan(int x, int* sums, int& before, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    long long upto = x;
+    int upto = x;
     for (int o = 1; o < 64; o <<= 1) {
-        const long long below = __shfl_up(upto, o);
+        const int below = __shfl_up(upto, o);
         if (lane >= o) upto += below;
     }
     __syncthreads();
@@ -134,30 +158,44 @@ __device__ __forceinline__ void scan(long long x, long long* sums, long long& be
         total += sums[w];
     }
 }
+// A thread per KV head of a sequence, then one per tile, then one per stretch's beginning.
+template <bool FEW>
 __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a) {
-    __shared__ long long sums[kPlanThreads / 64];
+    __shared__ int sums[kPlanThreads / 64];
     __shared__ int ends[kPlanThreads];  // tiles up to and with a pair, of the pairs at hand
     const Geom& gm = a.gm;
     const int pairs = gm.B * gm.Hkv, G = gm.G;
-    int tiles = 0;       // of the pairs before
-    long long line = 0;  // where the next tile begins
+    int tiles = 0;        // of the pairs before
+    long long line = 0;   // where the next tile begins
     for (int p0 = 0; p0 < pairs; p0 += kPlanThreads) {
         const int mine = p0 + (int)threadIdx.x;
-        int count = 0;
+        int count = 0, windows = 0, listed = 0;
+        Seq s{};
         if (mine < pairs) {
-            const Seq s = seq_of(a, mine / gm.Hkv);
-            count = window_tiles(a, s) + (a.listed[mine] + a.tile_rows - 1) / a.tile_rows;
+            const int b = mine / gm.Hkv, hk = mine - b * gm.Hkv;
+            s = seq_of(a, b);
+            windows = window_tiles(a, s);
+            if constexpr (FEW) {  // one tile of all the sequence's rows, if one of them is routed and has keys before the window
+                bool any = false;
+                for (int r = plan::rows_without_prefix(s, G, gm.W); r < s.n * G; ++r) any |= token_routed(a, s.start + r / G, hk * G + r % G);
+                listed = any ? s.n * G : 0;
+                if (hk == 0)
+                    for (int i = 0; i < s.n; ++i) a.token_seq[s.start + i] = b;
+            } else {
+                listed = min(a.pairs[mine].listed, s.n * G);
+            }
+            count = windows + (listed + a.tile_rows - 1) / a.tile_rows;
         }
-        long long before, here;
+        int before, here;
         scan(count, sums, before, here);
-        if (mine < pairs) a.pair_tile[mine] = tiles + (int)before;
-        ends[threadIdx.x] = (int)before + count;
+        if (mine < pairs) a.pairs[mine] = Pair{tiles + before, listed, 0, 0};
+        ends[threadIdx.x] = before + count;
         __syncthreads();
         const int of = min(pairs - p0, kPlanThreads);
-        for (int i0 = 0; i0 < (int)here; i0 += kPlanThreads) {
+        for (int i0 = 0; i0 < here; i0 += kPlanThreads) {
             const int i = i0 + (int)threadIdx.x;
             Tile t{};
-            const bool on = i < (int)here && tiles + i < a.most_tiles;
+            const bool on = i < here && tiles + i < a.most_tiles;
             if (on) {
                 int lo = 0, hi = of - 1;  // the first pair that ends behind tile i
                 while (lo < hi) {
@@ -165,24 +203,18 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                     if (ends[mid] > i) hi = mid;
                     else lo = mid + 1;
                 }
-                const int pair = p0 + lo, b = pair / gm.Hkv, hk = pair - b * gm.Hkv;
-                const Seq s = seq_of(a, b);
-                const int windows = window_tiles(a, s), within = i - (lo ? ends[lo - 1] : 0), rows = s.n * G;
-                t.b = b, t.hk = hk, t.s = s;
-                t.kind = within < windows ? plan::kWindow : plan::kPrefix;
-                t.first = (t.kind == plan::kWindow ? within : within - windows) * a.tile_rows;
-                t.rows = min(a.tile_rows, (t.kind == plan::kWindow ? rows : min(a.listed[pair], rows)) - t.first);
-                int c0 = t.first, c1 = t.first + t.rows - 1;
-                if (t.kind == plan::kPrefix) {
-                    const int32_t* list = list_of(a, a.list, s, hk);
-                    c0 = plan::clamp(list[c0], 0, rows - 1), c1 = plan::clamp(list[c1], 0, rows - 1);
-                }
-                t.pos0 = s.pos + c0 / G, t.pos1 = s.pos + c1 / G;
+                t.b = (p0 + lo) / gm.Hkv, t.hk = p0 + lo - t.b * gm.Hkv;
+                t.s = seq_of(a, t.b);
+                const int w = window_tiles(a, t.s), within = i - (lo ? ends[lo - 1] : 0), rows = t.s.n * G;
+                t.kind = within < w ? plan::kWindow : plan::kPrefix;
+                t.first = (t.kind == plan::kWindow ? within : within - w) * a.tile_rows;
+                t.rows = min(a.tile_rows, (t.kind == plan::kWindow || FEW ? rows : min(a.pairs[p0 + lo].listed, rows)) - t.first);
+                t.pos0 = t.s.pos + row_code(a, t, t.first) / G, t.pos1 = t.s.pos + row_code(a, t, t.first + t.rows - 1) / G;
                 const Range k = plan::tile_keys(t.kind, t.pos0, t.pos1, gm.W);
                 t.lo = k.lo, t.hi = k.hi;
                 t.blocks = plan::tile_blocks(k);
             }
-            long long at, sum;
+            int at, sum;
             scan(on ? t.blocks + plan::kStart : 0, sums, at, sum);
             if (on) {
                 t.start = line + at;
@@ -190,12 +222,58 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
             }
             line += sum;
         }
-        tiles += (int)here;
+        tiles += here;
         __syncthreads();
     }
     tiles = min(tiles, a.most_tiles);
-    const int per = max(plan::stretch(line, a.workgroups), 1);
-    if (threadIdx.x == 0) *a.head = Head{line, per, tiles};
+    int per = max(plan::stretch(line, a.workgroups), 1), segments = 0, segment_blocks = per;
+    if (!FEW && a.do_global && per >= plan::kSegmentLeast) {
+        for (int p0 = 0; p0 < pairs; p0 += kPlanThreads) {  // how many each pair has
+            const int mine = p0 + (int)threadIdx.x;
+            int each = 0, of = 0;
+            if (mine < pairs) {
+                const Pair p = a.pairs[mine];
+                const int first = p.first_tile + window_tiles(a, seq_of(a, mine / gm.Hkv));
+                of = (p.listed + a.tile_rows - 1) / a.tile_rows;
+                if (of && first + of <= tiles) each = plan::segments(a.tiles[first].blocks, per);
+            }
+            int before, here;
+            scan(each * of, sums, before, here);
+            if (mine < pairs) a.pairs[mine].segments = each, a.pairs[mine].first_segment = segments + before;
+            segments += here;
+        }
+        __syncthreads();
+        if (segments >= a.workgroups) {  // (only lists that others wrote over could say so: sequences that overlap)
+            for (int i = threadIdx.x; i < pairs; i += kPlanThreads) a.pairs[i].segments = 0;
+            segments = 0;
+            __syncthreads();
+        }
+        line = 0;
+        for (int i0 = 0; i0 < tiles; i0 += kPlanThreads) {  // which they are, and the line without them
+            const int i = i0 + (int)threadIdx.x;
+            int blocks = 0, skip = 0;
+            if (i < tiles) {
+                const Tile& t = a.tiles[i];
+                blocks = t.blocks;
+                const Pair p = a.pairs[t.b * gm.Hkv + t.hk];
+                if (t.kind == plan::kPrefix && p.segments) {
+                    skip = p.segments * per;
+                    blocks = max(blocks - skip, 0);
+                    const int of = (p.listed + a.tile_rows - 1) / a.tile_rows;
+                    for (int k = 0; k < p.segments; ++k) {
+                        const int w = p.first_segment + k * of + t.first / a.tile_rows;
+                        if (w < a.workgroups) a.segment[w] = int2{i, k};
+                    }
+                }
+            }
+            int at, sum;
+            scan(i < tiles ? blocks + plan::kStart : 0, sums, at, sum);
+            if (i < tiles) a.tiles[i].start = line + at, a.tiles[i].blocks = blocks, a.tiles[i].skip = skip;
+            line += sum;
+        }
+        per = max(plan::stretch(line, max(a.workgroups - segments, 1)), 1);
+    }
+    if (threadIdx.x == 0) *a.head = Head{line, per, tiles, segments, segment_blocks};
     __syncthreads();
     // the tile each stretch begins in
     for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
@@ -234,42 +312,32 @@ __device__ __forceinline__ int load_row(int lane) { return FP8 ? ((lane >> 1) & 
 template <bool FP8>
 __device__ __forceinline__ int load_chunk(int lane) { return FP8 ? (lane & 1) + 2 * ((lane >> 3) & 3) : (lane >> 4) * 4 + (lane & 3); }
 // e4m3: a lane's 16 elements of `row`, with the exponents of the row, become bf16
-__device__ __forceinline__ void store_converted(const u32x4& x, uint32_t exponents, char* block, int row, int lane) {
+typedef __attribute__((address_space(3))) char* lds_ptr;
+__device__ __forceinline__ void store_converted(const u32x4& x, uint32_t exponents, lds_ptr block, int row, int lane) {
     const int c = load_chunk<true>(lane);
     u32x4 y[2];
     dequantise16(x, exponent_value((exponents >> (8 * (c >> 1))) & 0xffu), y);
-    u32x4* const at = reinterpret_cast<u32x4*>(block + chunk_at(row, 2 * c));
+    __attribute__((address_space(3))) u32x4* const at = (__attribute__((address_space(3))) u32x4*)(block + chunk_at(row, 2 * c));
     at[0] = y[0], at[1] = y[1];
 }
 
-// Shared memory.  A stage holds K of one block, V of another; blocks are loaded three walks of the loop ahead of their use.
+// Shared memory of a workgroup, in bytes from its beginning: rings of blocks of K and of V; e4m3: rings of what was loaded (K, V, their
+// exponents: every wavefront's pieces its own, which it alone converts) and of the bf16 blocks made of it.  Blocks are loaded two
+// walks of the loop ahead of their use.
 constexpr int kWaves = 8;  // of a workgroup: up to 32 rows each
 template <bool FP8>
-struct ExtendLds;
-template <>
-struct ExtendLds<false> {
-    static constexpr int kK = 5, kV = 4;
-    char k[kK][kBlockBytes], v[kV][kBlockBytes];
+struct Lds {
+    static constexpr int kK = FP8 ? 3 : 4, kV = FP8 ? 3 : 4, kRaw = 2;
+    static constexpr unsigned k = 0, v = k + kK * kBlockBytes, raw_k = v + kV * kBlockBytes;
+    static constexpr unsigned kRawBlock = kWaves * 1024, kRawScales = kWaves * 256;
+    static constexpr unsigned raw_v = raw_k + kRaw * kRawBlock, raw_ks = raw_v + kRaw * kRawBlock, raw_vs = raw_ks + kRaw * kRawScales;
+    static constexpr unsigned used = FP8 ? raw_vs + kRaw * kRawScales : raw_k, sums = kWaves * 32 * kPart * 4;  // (sums: few_rows)
+    static constexpr unsigned bytes = used > sums ? used : sums;
 };
-template <>
-struct ExtendLds<true> {  // e4m3 as loaded, each wavefront's pieces its own, and the bf16 blocks made of them
-    static constexpr int kK = 3, kV = 2, kRaw = 3;
-    char k[kK][kBlockBytes], v[kV][kBlockBytes];
-    char raw_k[kRaw][kWaves][1024], raw_v[kRaw][kWaves][1024];
-    uint32_t raw_ks[kRaw][kWaves][64], raw_vs[kRaw][kWaves][64];
-};
-
-// A row's result: s (x), a (y), their log-sum-exps, four channels a lane
-__device__ __forceinline__ void store_row(const ExtendArgs& a, int token, int head, int c4, const f32x4& x, const f32x4& y, float lse_l, float lse_g) {
-    const size_t off = ((size_t)token * a.gm.Hq + head) * kD + c4;
-    *reinterpret_cast<bf16x4*>(a.O + off) = __builtin_convertvector(x + y, bf16x4);
-    if (a.S) *reinterpret_cast<bf16x4*>(a.S + off) = __builtin_convertvector(x, bf16x4);
-    if (a.A) *reinterpret_cast<bf16x4*>(a.A + off) = __builtin_convertvector(y, bf16x4);
-    if (c4 == 0) {
-        const size_t so = (size_t)head * a.gm.T + token;
-        if (a.lse_l) a.lse_l[so] = lse_l;
-        if (a.lse_g) a.lse_g[so] = lse_g;
-    }
+// A place in a ring of `of` blocks of `each` bytes that begins at `first`, moved on.
+__device__ __forceinline__ unsigned next(unsigned at, unsigned first, unsigned each, int of) {
+    at += each;
+    return at == first + of * each ? first : at;
 }
 
 #define FENCE() __builtin_amdgcn_sched_barrier(0)
@@ -285,85 +353,75 @@ __device__ __forceinline__ X uniform(const X* p) {
     return __builtin_bit_cast(X, x);
 }
 
-// A number that wraps around
-__device__ __forceinline__ int next(int i, int n) { return i + 1 == n ? 0 : i + 1; }
-
 // The blocks of a piece on their way to LDS.  Block i + 1 of K and block i of V go together (group i): a block's scores are computed
-// before the block ahead of it is multiplied with V.
+// before the block ahead of it is multiplied with V.  A wavefront loads 8 rows of every block, which lie in one page.
 template <bool FP8>
 struct Loader {
-    typedef ExtendLds<FP8> Lds;
-    // one instruction of a wavefront loads 1024 bytes, rows that lie in one page: 4 of bf16, 8 of e4m3
-    static constexpr int kRows = FP8 ? 8 : 4, kEach = kKeys / (kRows * kWaves);
+    typedef Lds<FP8> L;
+    static constexpr int kRowBytes = FP8 ? kD : kD * 2;
     static constexpr int kGroup = 4;  // instructions of a group: K and V, two each (e4m3: elements and exponents)
-    static_assert(kEach * (FP8 ? 2 : 1) == 2, "the group's instructions");
     const ExtendArgs& a;
-    Lds& lds;
     const scalar int32_t* table;
     int hk, lo, hi, jb0, blocks;  // keys lo .. hi may be read; blocks jb0 .. jb0 + blocks - 1
     int wave, lane;
-    int issued, k_to, v_to;       // last group issued; where the next K and V go
-    size_t row_k[kEach], row_v[kEach];  // rows of the pool where the instructions of the next group's K and V begin
+    int issued;                   // last group issued
+    unsigned k_to, v_to, ks_to, vs_to;  // where the next K and V go
+    // the next group's K and V: the row of the pool where this wavefront's begin, and how many bytes behind that this lane's are
+    size_t row_k, row_v;
+    unsigned off_k[2], off_v[2];
 
+    __device__ __forceinline__ void start() {
+        issued = -2;
+        k_to = FP8 ? L::raw_k + wave * 1024 : L::k + wave * 2 * kFour, v_to = FP8 ? L::raw_v + wave * 1024 : L::v + wave * 2 * kFour;
+        ks_to = L::raw_ks + wave * 256, vs_to = L::raw_vs + wave * 256;
+        find(0);
+    }
     // Keys out of lo .. hi (before the first row's window: their pages may have been given back; behind the last row: not written yet)
     // repeat the nearest key inside: always masked, and what lies in such rows must not meet a zero weight.
-    __device__ __forceinline__ int tile_row(int e) const { return (e * kWaves + wave) * kRows; }
-    __device__ __forceinline__ int first_key(int block, int e) const {
-        return plan::clamp((jb0 + block) * kKeys + tile_row(e), lo & -kRows, hi & -kRows);
-    }
     __device__ __forceinline__ void find(int block) {
+        const int k0 = (jb0 + block) * kKeys + wave * 8, first = plan::clamp(k0, lo & -8, hi & -8);
+        row_k = pool_row(a.c, a.gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), hk, first);
+        int mine[2] = {load_row<FP8>(lane), load_row<FP8>(lane) + 4};  // rows behind the first
+        if (k0 < lo || k0 + 7 > hi) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int key = first_key(block, e);
-            row_k[e] = pool_row(a.c, a.gm.Hkv, plan::clamp(table[key >> a.c.page_log2], 0, a.c.pages - 1), hk, key);
+            for (int e = 0; e < 2; ++e) mine[e] = plan::clamp(k0 + mine[e], lo, hi) - first;
         }
-    }
-    __device__ __forceinline__ void issue_half(const char* pool, const unsigned char* scales, int block, const size_t* rows, char* tile, uint32_t* tile_scales) {
-        const int k0 = (jb0 + block) * kKeys;
-        const bool inside = k0 >= lo && k0 + kKeys - 1 <= hi;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int mine = load_row<FP8>(lane), row = tile_row(e) + mine;
-            unsigned off = mine;  // rows behind the instruction's first
-            if (!inside) off = plan::clamp(k0 + row, lo, hi) - first_key(block, e);
-            const unsigned to = __builtin_amdgcn_readfirstlane(lds_offset(tile)) + (e * kWaves + wave) * (FP8 ? 1024 : kFour);
-            if constexpr (!FP8) {
-                dma16_so(pool + rows[e] * (kD * 2), off * (kD * 2) + load_chunk<FP8>(lane) * 16, to);
-            } else {
-                dma16_so(pool + rows[e] * kD, off * kD + load_chunk<FP8>(lane) * 16, to);
-                dma4_so(scales + rows[e] * kRowScales, off * kRowScales, __builtin_amdgcn_readfirstlane(lds_offset(tile_scales)) + wave * 256);
-            }
-        }
+        off_k[0] = mine[0] * kRowBytes + load_chunk<FP8>(lane) * 16;
+        off_k[1] = FP8 ? mine[0] * kRowScales : mine[1] * kRowBytes + load_chunk<FP8>(lane) * 16;
     }
     __device__ __forceinline__ void issue() {  // the next group, as far as there is one
         const int i = ++issued;
         if (i + 1 < blocks) {
-            if constexpr (!FP8) issue_half(a.c.k, nullptr, i + 1, row_k, lds.k[k_to], nullptr);
-            else issue_half(a.c.k, a.c.ks, i + 1, row_k, lds.raw_k[k_to][0], lds.raw_ks[k_to][0]);
+            dma16_so(a.c.k + row_k * kRowBytes, off_k[0], k_to);
+            if constexpr (FP8) dma4_so(a.c.ks + row_k * kRowScales, off_k[1], ks_to);
+            else dma16_so(a.c.k + row_k * kRowBytes, off_k[1], k_to + kFour);
         }
-        if (i >= 0 && i < blocks) {
-            if constexpr (!FP8) issue_half(a.c.v, nullptr, i, row_v, lds.v[v_to], nullptr);
-            else issue_half(a.c.v, a.c.vs, i, row_v, lds.raw_v[v_to][0], lds.raw_vs[v_to][0]);
+        if (i >= 0) {
+            if (i < blocks) {
+                dma16_so(a.c.v + row_v * kRowBytes, off_v[0], v_to);
+                if constexpr (FP8) dma4_so(a.c.vs + row_v * kRowScales, off_v[1], vs_to);
+                else dma16_so(a.c.v + row_v * kRowBytes, off_v[1], v_to + kFour);
+            }
+            v_to = FP8 ? next(v_to, L::raw_v + wave * 1024, L::kRawBlock, L::kRaw) : next(v_to, L::v + wave * 2 * kFour, kBlockBytes, L::kV);
+            if (FP8) vs_to = next(vs_to, L::raw_vs + wave * 256, L::kRawScales, L::kRaw);
         }
-        k_to = next(k_to, FP8 ? ExtendLds<true>::kRaw : Lds::kK);
-        if (i >= 0) v_to = next(v_to, FP8 ? ExtendLds<true>::kRaw : Lds::kV);
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) row_v[e] = row_k[e];
+        k_to = FP8 ? next(k_to, L::raw_k + wave * 1024, L::kRawBlock, L::kRaw) : next(k_to, L::k + wave * 2 * kFour, kBlockBytes, L::kK);
+        if (FP8) ks_to = next(ks_to, L::raw_ks + wave * 256, L::kRawScales, L::kRaw);
+        row_v = row_k, off_v[0] = off_k[0], off_v[1] = off_k[1];
         find(min(i + 2, blocks - 1));
     }
-    // Waits until at most the two last groups are on their way; those at the end have half their loads or none.
+    // Waits until at most the last group is on its way; those at the end have half their loads or none.
     __device__ __forceinline__ void wait() const {
         constexpr int half = kGroup / 2;
-        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * half) : "memory");
-        else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * half) : "memory");
-        else if (issued == blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(half) : "memory");
+        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * half) : "memory");
+        else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(half) : "memory");
         else dma_wait();
     }
-    // e4m3: this wavefront's pieces of a group become bf16.
-    __device__ __forceinline__ void convert(const char* raw, const uint32_t* scales, char* block) const {
-        if constexpr (FP8)
-            store_converted(*reinterpret_cast<const u32x4*>(raw + wave * 1024 + lane * 16), scales[wave * 64 + lane], block,
-                            wave * 8 + load_row<true>(lane), lane);
+    // e4m3: this wavefront's pieces of a loaded block (the raw-th of the ring) become bf16.
+    __device__ __forceinline__ void convert(unsigned raw, unsigned raw_scales, int slot, unsigned block) const {
+        const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(raw + slot * L::kRawBlock + wave * 1024 + lane * 16);
+        const uint32_t e = *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)(raw_scales + slot * L::kRawScales + wave * 256 + lane * 4);
+        store_converted(x, e, (lds_ptr)(uintptr_t)block, wave * 8 + load_row<true>(lane), lane);
     }
 };
 
@@ -382,19 +440,20 @@ struct RowSums {
         m = kNone, l = 0.f;
     }
     __device__ __forceinline__ void scale(float by) {
-        l *= by;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[d][e] *= by;
     }
-    // mx: the largest score of this lane's keys, in log2 units
+    // mx: the largest score of this lane's keys, in log2 units.  Moves the maximum and the sum, returns what o is to be scaled by.
+    __device__ __forceinline__ float move(float mx) {
+        const float mnew = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32))), by = fast_exp2(m - mnew);
+        m = mnew;
+        l *= by;
+        return by;
+    }
     __device__ __forceinline__ void look(float mx) {
-        if (__any(mx > m + kSlack)) {
-            const float mnew = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
-            scale(fast_exp2(m - mnew));
-            m = mnew;
-        }
+        if (__any(mx > m + kSlack)) scale(move(mx));
     }
 };
 __device__ __forceinline__ float largest(const f32x16& s) {
@@ -409,26 +468,22 @@ __device__ __forceinline__ float largest(const f32x16& s) {
 // (All wavefronts loading blocks of 64 keys for two of them to compute: 217 us for 64 sequences of 8K tokens in e4m3, 1.5 us a block.)
 constexpr int kSub = 32;
 template <bool FP8>
-__device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& lds, const Tile& t, const plan::Piece& piece, int w) {
+__device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5, G = gm.G, hk = t.hk;
     const float c2 = gm.scale_log2;
     const scalar int32_t* const table = (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages);
     // row r of the tile: its code, and from it the token
-    auto code_of = [&](int r) __attribute__((always_inline)) {
-        const int at = t.first + min(r, t.rows - 1);
-        return t.kind == plan::kWindow ? at : plan::clamp(list_of(a, a.list, t.s, hk)[at], 0, t.s.n * G - 1);
-    };
-    const int jb0 = t.lo / kKeys + piece.from, jb1 = t.lo / kKeys + piece.to;
+    auto code_of = [&](int r) __attribute__((always_inline)) { return row_code(a, t, t.first + min(r, t.rows - 1)); };
+    const int jb0 = t.lo / kKeys + t.skip + piece.from, jb1 = t.lo / kKeys + t.skip + piece.to;
     const int sb1 = min(2 * jb1, t.hi / kSub + 1), sb0 = max(2 * jb0, t.lo / kSub) + wave;  // sub-blocks sb0, sb0 + 8, .. below sb1
 
     __syncthreads();  // LDS is free
     constexpr int kSubBytes = kSub / 4 * kFour;
-    static_assert(sizeof(ExtendLds<FP8>) >= kWaves * 2 * kSubBytes, "room for every wavefront's keys");
-    char *const kt = reinterpret_cast<char*>(&lds) + wave * 2 * kSubBytes, *const vt = kt + kSubBytes;
-    const lds_cptr k_at = (lds_cptr)(uintptr_t)(lds_offset(kt) + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(lds_offset(vt) + v_lane(lane));
-    const unsigned k_to = __builtin_amdgcn_readfirstlane(lds_offset(kt)), v_to = __builtin_amdgcn_readfirstlane(lds_offset(vt));
+    static_assert(Lds<FP8>::bytes >= kWaves * 2 * kSubBytes, "room for every wavefront's keys");
+    const unsigned k_to = wave * 2 * kSubBytes, v_to = k_to + kSubBytes;
+    const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
     constexpr int kRows = FP8 ? 8 : 4, kEach = kSub / kRows;  // rows of an instruction, which lie in one page; instructions
     const int mine = load_row<FP8>(lane);
     u32x4 kx[FP8 ? kEach : 1], vx[FP8 ? kEach : 1];
@@ -465,9 +520,9 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& ld
             }
         }
     };
-    auto convert = [&](const u32x4* x, const uint32_t* se, char* block) __attribute__((always_inline)) {
+    auto convert = [&](const u32x4* x, const uint32_t* se, unsigned block) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) store_converted(x[e], se[e], block, e * kRows + mine, lane);
+        for (int e = 0; e < kEach; ++e) store_converted(x[e], se[e], (lds_ptr)(uintptr_t)block, e * kRows + mine, lane);
     };
     if (sb0 < sb1) {
         find(sb0);
@@ -490,7 +545,7 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& ld
     for (int sb = sb0; sb < sb1; sb += kWaves) {
         const bool more = sb + kWaves < sb1;
         if (more) find(sb + kWaves);
-        if constexpr (FP8) convert(kx, kse, kt);
+        if constexpr (FP8) convert(kx, kse, k_to);
         else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
         bf16x8 op[8];
 #pragma unroll
@@ -508,7 +563,7 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& ld
             if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
             else dma_wait();
         } else {
-            convert(vx, vse, vt);
+            convert(vx, vse, v_to);
             if (more) load(a.c.v, a.c.vs, vx, vse, v_to);
         }
 #pragma unroll
@@ -539,8 +594,8 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& ld
 
     // ---- the eight wavefronts' sums, joined: 16 threads per row, eight channels each
     row.l += __shfl_xor(row.l, 32);
-    float* const sums = reinterpret_cast<float*>(&lds);  // [wave][row][kPart]
-    static_assert(sizeof(ExtendLds<FP8>) >= kWaves * 32 * kPart * sizeof(float), "room for the wavefronts' sums");
+    float* const sums = reinterpret_cast<float*>(lds);  // [wave][row][kPart]
+    static_assert(Lds<FP8>::bytes >= kWaves * 32 * kPart * sizeof(float), "room for the wavefronts' sums");
     __syncthreads();  // every wavefront is done with its part of LDS
     {
         float* const at = sums + (wave * 32 + n) * kPart;
@@ -588,24 +643,34 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, ExtendLds<FP8>& ld
 
 template <bool FP8>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
-    __shared__ __attribute__((aligned(1024))) ExtendLds<FP8> lds;
+    typedef Lds<FP8> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::bytes];  // all there is: places in it are its addresses
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5, G = gm.G;
     const float c2 = gm.scale_log2;
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+    asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory");  // (it is written and read by address)
     // workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring stretches
     const int w = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);
     const Head line = uniform(a.head);
-    if ((long long)w * line.per >= line.total) return;
-    const long long x1 = (long long)(w + 1) * line.per;
+    const bool segment = w < line.segments;  // all it does; the others share the line
+    const int stretch = w - line.segments;
+    if (!segment && (long long)stretch * line.per >= line.total) return;
+    const int2 mine = segment ? uniform(a.segment + w) : int2{uniform(a.first_tile + stretch), 0};
+    const long long x1 = (long long)(stretch + 1) * line.per;
 
-    for (int T = uniform(a.first_tile + w); T < line.tiles; ++T) {
+    for (int T = mine.x; T < line.tiles; ++T) {
         const Tile t = uniform(a.tiles + T);
-        if (t.start >= x1) break;
-        const plan::Piece piece = plan::piece(Place{t.start, t.blocks}, line.per, w);
-        if (piece.from == piece.to) continue;
+        plan::Piece piece{mine.y * line.blocks - t.skip, (mine.y + 1) * line.blocks - t.skip, 0, 0};
+        if (!segment) {
+            if (t.start >= x1) break;
+            piece = plan::piece(Place{t.start, t.blocks}, line.per, stretch);
+            if (piece.from == piece.to) continue;
+        } else if (T != mine.x) {
+            break;
+        }
         const int b = t.b, hk = t.hk;
         const Seq s = t.s;
         if (t.rows <= 32) {
@@ -613,11 +678,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             continue;
         }
 
-        const int jb0 = t.lo / kKeys + piece.from, blocks = piece.to - piece.from;
+        const int jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
         __syncthreads();  // LDS is free
-        Loader<FP8> load{a, lds, (const scalar int32_t*)(a.c.table + (size_t)b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane, -2, 0, 0};
-        load.find(0);
-        load.issue();
+        Loader<FP8> load{a, (const scalar int32_t*)(a.c.table + (size_t)b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
+        load.start();
         load.issue();
         load.issue();
 
@@ -626,8 +690,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         const bool halves = t.rows <= 32 * kWaves / 2;
         const int r = (halves ? wave & 3 : wave) * 32 + n;
         const bool valid = r < t.rows, wave_on = r - n < t.rows;
-        int code = t.first + min(r, t.rows - 1);
-        if (t.kind == plan::kPrefix) code = plan::clamp(list_of(a, a.list, s, hk)[code], 0, s.n * G - 1);
+        const int code = row_code(a, t, t.first + min(r, t.rows - 1));
         const int local_tok = code / G, g = code - local_tok * G, head = hk * G + g, token = s.start + local_tok, pos = s.pos + local_tok;
         const Range keys = plan::row_keys(t.kind, pos, gm.W);
         bf16x8 qreg[8];
@@ -649,19 +712,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
 
         RowSums row;
         row.clear();
-        int kb = 0, vb = 0;  // buffers of block j
-        int raw = 0;
+        unsigned kb = L::k, vb = L::v;  // block j
+        auto next_k = [&]() __attribute__((always_inline)) { return next(kb, L::k, kBlockBytes, L::kK); };
+        auto next_v = [&]() __attribute__((always_inline)) { return next(vb, L::v, kBlockBytes, L::kV); };
         if constexpr (FP8) {
             load.wait();
-            load.convert(lds.raw_k[0][0], lds.raw_ks[0][0], lds.k[0]);
+            load.convert(L::raw_k, L::raw_ks, 0, L::k);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             load.issue();
             load.wait();
-            if (blocks > 1) load.convert(lds.raw_k[1][0], lds.raw_ks[1][0], lds.k[1]);
-            load.convert(lds.raw_v[0][0], lds.raw_vs[0][0], lds.v[0]);
+            if (blocks > 1) load.convert(L::raw_k, L::raw_ks, 1, L::k + kBlockBytes);
+            load.convert(L::raw_v, L::raw_vs, 0, L::v);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             load.issue();
-            raw = 2;
         } else {
             load.issue();
             load.wait();
@@ -672,11 +735,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             if constexpr (FP8) {
                 if (j + 1 < blocks) {
                     load.wait();
-                    if (j + 2 < blocks) load.convert(lds.raw_k[raw][0], lds.raw_ks[raw][0], lds.k[kb == 0 ? 2 : kb - 1]);
-                    const int rv = raw == 0 ? 2 : raw - 1;  // V of a group lies one place behind its K
-                    load.convert(lds.raw_v[rv][0], lds.raw_vs[rv][0], lds.v[vb ^ 1]);
+                    if (j + 2 < blocks) load.convert(L::raw_k, L::raw_ks, j & 1, next(next_k(), L::k, kBlockBytes, L::kK));
+                    load.convert(L::raw_v, L::raw_vs, (j + 1) & 1, next_v());
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    raw = next(raw, 3);
                 }
             }
             load.issue();
@@ -684,12 +745,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         auto end = [&](int j) __attribute__((always_inline)) {
             if constexpr (!FP8) load.wait();
             __syncthreads();
-            kb = next(kb, ExtendLds<FP8>::kK), vb = next(vb, ExtendLds<FP8>::kV);
+            kb = next_k(), vb = next_v();
         };
-
         const unsigned k_mine = k_lane(lane), v_mine = v_lane(lane);
-        auto k_block = [&](int buf) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(lds_offset(lds.k[buf]) + k_mine); };
-        auto v_block = [&](int buf) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(lds_offset(lds.v[buf]) + v_mine); };
+        auto k_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + k_mine); };
+        auto v_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + v_mine); };
         // Weights of a pair of scores, rounded to bf16; the sum is that of the weights as the matrix cores see them, so that what
         // they are divided by is exact for them.
         auto weigh = [&](const f32x16& sc, int e) __attribute__((always_inline)) {
@@ -725,40 +785,44 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
                 end(j);
             }
         } else {
-            // All keys for 32 rows a wavefront.  While the weights of 32 keys are found on the vector units, the matrix cores compute the
-            // scores of the 32 keys after them, and then the product of these weights with V (slots of one matrix instruction each;
-            // operands are read kAhead slots before their use).
+            // All keys for 32 rows a wavefront, in steps of 32.  While the vector units find the weights of a step's keys, the matrix
+            // cores compute the scores of the next step's and the product of the step before with V, neither of which waits for these
+            // weights: 16 matrix instructions, a slot each; operands are read kAhead slots before their use.  (With the product of the
+            // same step in the second half of the slots the weights had to be found in the first ones: 1721 us at 4096 tokens behind 126976.)
             constexpr int kAhead = 2;
             f32x16 sa, sb;
+            u32x4 pa[2], pb[2];
             float mx;
-            auto half_block = [&](auto half_tag, f32x16& cur, f32x16& nxt, lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
+            auto step = [&](auto half_tag, auto first_tag, const f32x16& cur, f32x16& nxt, const u32x4 (&before)[2], u32x4 (&p)[2], lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
                 constexpr int H = decltype(half_tag)::value;  // nxt: the block's second half, or the next block's first
-                row.look(mx);
+                constexpr bool FIRST = decltype(first_tag)::value;  // nothing before
+                float by = 1.f;
+                const bool grew = __any(mx > row.m + kSlack);
+                if (grew) by = row.move(mx);
                 bf16x8 op[16 + kAhead];
-                u32x4 p[2];
                 auto read = [&](auto oc) __attribute__((always_inline)) {
                     constexpr int o = decltype(oc)::value;
                     if constexpr (o < 8) op[o] = k_operand(ka, o, 1 - H);
-                    else if constexpr (o < 16) op[o] = v_operand(va, o & 3, 2 * H + ((o - 8) >> 2));
+                    else if constexpr (o < 16 && !FIRST) op[o] = v_operand(va, o & 3, 2 * (1 - H) + ((o - 8) >> 2));
                 };
                 static_for<0, kAhead>([&](auto oc) { read(oc); });
                 FENCE();
                 static_for<0, 16>([&](auto sc_) __attribute__((always_inline)) {
                     constexpr int slot = decltype(sc_)::value;
                     if constexpr (slot < 8) nxt = mfma32(op[slot], qreg[slot], slot == 0 ? zero16 : nxt);
-                    else row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, p[(slot - 8) >> 2]), row.o[slot & 3]);
+                    else if constexpr (!FIRST) row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, before[(slot - 8) >> 2]), row.o[slot & 3]);
                     read(std::integral_constant<int, slot + kAhead>{});
-                    static_for<0, 8>([&](auto qc) __attribute__((always_inline)) {
-                        constexpr int q = decltype(qc)::value;
-                        if constexpr ((3 * q) / 2 == slot) p[q >> 2][q & 3] = weigh(cur, 2 * q);
-                    });
-                    if constexpr (slot == 12) {
+                    if constexpr (slot % 2 == 0) p[slot >> 3][(slot >> 1) & 3] = weigh(cur, slot);
+                    if constexpr (slot == 13) {
                         if (masked_next) mask(nxt, k0_next);
                         mx = largest(nxt) * c2;
                     }
                     FENCE();
                 });
+                if (grew) row.scale(by);
             };
+            typedef std::integral_constant<int, 0> H0;
+            typedef std::integral_constant<int, 1> H1;
             {
                 const lds_cptr ka = k_block(kb);
 #pragma unroll
@@ -766,20 +830,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             }
             if (masked(jb0)) mask(sa, jb0 * kKeys);
             mx = largest(sa) * c2;
+            lds_cptr va = v_block(vb);
             for (int j = 0; j < blocks; ++j) {
                 begin(j);
                 const int jb = jb0 + j;
-                const lds_cptr va = v_block(vb);
-                half_block(std::integral_constant<int, 0>{}, sa, sb, k_block(kb), va, jb * kKeys + 32, masked(jb));
-                half_block(std::integral_constant<int, 1>{}, sb, sa, k_block(next(kb, ExtendLds<FP8>::kK)), va, (jb + 1) * kKeys, masked(jb + 1));
+                if (j == 0) step(H0{}, std::true_type{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
+                else step(H0{}, std::false_type{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
+                va = v_block(vb);
+                step(H1{}, std::false_type{}, sb, sa, pa, pb, k_block(next_k()), va, (jb + 1) * kKeys, masked(jb + 1));
                 end(j);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(v_operand(va, i & 3, 2 + (i >> 2)), __builtin_bit_cast(bf16x8, pb[i >> 2]), row.o[i & 3]);
         }
 
         // ---- out
         row.l += __shfl_xor(row.l, 32);
         if (halves) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
-            f32x4* const there = reinterpret_cast<f32x4*>(&lds) + (wave & 3) * (17 * 64) + lane;
+            f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & 3) * (17 * 64) + lane;
             if (wave_on && wave >= 4) {
                 there[0] = f32x4{row.m, row.l, 0.f, 0.f};
 #pragma unroll
@@ -791,9 +859,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             if (wave_on && wave < 4) {
                 const f32x4 ml = there[0];
                 const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew);
-                row.scale(fast_exp2(row.m - mnew));
+                const float mine = fast_exp2(row.m - mnew);
+                row.scale(mine);
                 row.m = mnew;
-                row.l = fmaf(ml[1], by, row.l);
+                row.l = fmaf(ml[1], by, row.l * mine);
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -832,76 +901,131 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
 
 // Thirty-two lanes per row, four channels each.
 struct Sums {
-    float m = -INFINITY, l = 0.f;
+    float m = kNone, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     __device__ __forceinline__ void join(float m2, float l2, const f32x4& o2) {
-        const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
-        const float s0 = fast_exp2(m - ref), s1 = fast_exp2(m2 - ref);
+        const float mn = fmaxf(m, m2), s0 = fast_exp2(m - mn), s1 = fast_exp2(m2 - mn);
         l = fmaf(l, s0, l2 * s1);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], s0, o2[e] * s1);
         m = mn;
     }
-    __device__ __forceinline__ void join(const float* part, int c4) {
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(part);
-        join(ml[0], ml[1], *reinterpret_cast<const f32x4*>(part + 4 + c4));
-    }
     __device__ __forceinline__ f32x4 value() const { return o / l; }
     __device__ __forceinline__ float lse() const { return (m + __builtin_amdgcn_logf(l)) * kLn2; }
 };
+// The sums that row r of a tile has in pieces: its segments' and those of its stretch of the line.
+struct Pieces {
+    int segments, first_segment, of;  // segment k: workgroup first_segment + k * of
+    int first, last, line;            // workgroups on the line, of which the first is workgroup number `line`
+    __device__ __forceinline__ Pieces(const Place& p, const Head& head) : segments(0), first_segment(0), of(0) {
+        first = plan::first_of(p, head.per), last = plan::last_of(p, head.per), line = head.segments;
+    }
+    __device__ __forceinline__ bool whole() const { return first >= last; }
+    // every `step`-th of them from the `from`-th on; row_parts: where the line's sums are if it is whole
+    __device__ __forceinline__ void join(const ExtendArgs& a, Sums& sums, int r, const float* row_parts, int c4, int from, int step) const {
+        constexpr int kAhead = 8;  // loads of this many on their way together (past the end the first is read again, for nobody)
+        const int n = segments + (whole() ? 1 : last - first + 1);
+        for (int i0 = from; i0 < n; i0 += kAhead * step) {
+            f32x2 ml[kAhead];
+            f32x4 x[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int i = i0 + j * step < n ? i0 + j * step : i0, k = i - segments;
+                const float* part = a.slots + ((size_t)(i < segments ? plan::slot(first_segment + i * of, 0) : plan::slot(line + first + k, k == 0)) * a.tile_rows + r) * kPart;
+                if (i >= segments && whole()) part = row_parts;
+                ml[j] = *reinterpret_cast<const f32x2*>(part);
+                x[j] = *reinterpret_cast<const f32x4*>(part + 4 + c4);
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (i0 + j * step < n) sums.join(ml[j][0], ml[j][1], x[j]);
+        }
+    }
+};
+__device__ __forceinline__ const float* row_part(const ExtendArgs& a, int kind, int token, int head) {
+    return a.parts[kind] + ((size_t)token * a.gm.Hq + head) * kPart;
+}
+// Rows of tiles of many: 32 rows of a tile per workgroup, eight at a time.  Rows of whole tiles that have no keys before their window were
+// written by the kernel before.
+constexpr int kCombineRows = 32;
 __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) {
     const Geom& gm = a.gm;
-    const int c4 = (threadIdx.x & 31) * 4, G = gm.G;
-    const long long row = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (row >= (long long)gm.T * gm.Hq) return;
-    const int token = (int)(row / gm.Hq), head = (int)(row - (long long)token * gm.Hq), hk = head / G, g = head - hk * G;
+    const Head head_ = uniform(a.head);
+    if ((int)blockIdx.x >= head_.tiles) return;
+    const Tile t = uniform(a.tiles + blockIdx.x);
+    const int c4 = (threadIdx.x & 31) * 4, G = gm.G, r0 = blockIdx.y * kCombineRows;
+    if (r0 >= t.rows || (a.do_local && t.kind != plan::kWindow)) return;
+    const Pieces own(Place{t.start, t.blocks}, head_);
+    const Pair pair = uniform(a.pairs + t.b * gm.Hkv + t.hk);
+    const int first_prefix = pair.first_tile + window_tiles(a, t.s), prefix_tiles = (pair.listed + a.tile_rows - 1) / a.tile_rows;
+    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    for (int r = r0 + (threadIdx.x >> 5); r < min(r0 + kCombineRows, t.rows); r += kThreads / 32) {
+        const int code = row_code(a, t, t.first + r), tok = code / G, head = t.hk * G + code - tok * G, token = t.s.start + tok;
+        const bool routed = token_routed(a, token, head), prefix = routed && t.s.pos + tok > gm.W;
+        if (a.do_local && own.whole() && !prefix) continue;
+        Sums sums;
+        f32x4 x = z;
+        float lse_l = -INFINITY;
+        if (a.do_local) {
+            own.join(a, sums, r, row_part(a, plan::kWindow, token, head), c4, 0, 1);
+            x = sums.value(), lse_l = sums.lse();
+        }
+        if (prefix) {
+            const int i = plan::clamp(list_of(a, a.rank, t.s, t.hk)[code], 0, max(pair.listed - 1, 0)), j = i / a.tile_rows;
+            const Tile& pt = a.tiles[min(first_prefix + j, head_.tiles - 1)];
+            Pieces p(Place{pt.start, pt.blocks}, head_);
+            p.segments = pair.segments, p.first_segment = pair.first_segment + j, p.of = prefix_tiles;
+            p.join(a, sums, i - j * a.tile_rows, row_part(a, plan::kPrefix, token, head), c4, 0, 1);
+        }
+        store_row(a, token, head, c4, x, routed ? sums.value() : z, lse_l, routed ? sums.lse() : -INFINITY);
+    }
+}
+// Rows of sequences of few: a workgroup per row, whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
+constexpr int kSlices = 8;
+__global__ __launch_bounds__(32 * kSlices) void extend_combine_few_kernel(ExtendArgs a) {
+    __shared__ __attribute__((aligned(16))) float part[2][kSlices][kPart];
+    const Geom& gm = a.gm;
+    const int c4 = (threadIdx.x & 31) * 4, slice = threadIdx.x >> 5, G = gm.G;
+    const int token = blockIdx.x / gm.Hq, head = blockIdx.x - token * gm.Hq, hk = head / G;
     const int b = a.token_seq[token];  // of a token that is in no sequence: whatever was there
     if (b < 0 || b >= gm.B) return;
     const Seq s = seq_of(a, b);
     const int at = token - s.start;
     if (at < 0 || at >= s.n) return;
-    const int pair = b * gm.Hkv + hk, code = at * G + g, per = a.head->per, tiles = a.head->tiles;
+    const Head head_ = *a.head;
     const bool routed = token_routed(a, token, head), prefix = routed && s.pos + at > gm.W;
-    Sums sums;
-    // the pieces of tile T; false: the tile is whole
-    auto pieces = [&](int T, int r) {
-        if (T >= tiles) return true;
-        const Place p{a.tiles[T].start, a.tiles[T].blocks};
-        const int f = plan::first_of(p, per), l = plan::last_of(p, per);
-        if (f >= l) return false;
-        constexpr int kAhead = 8;  // loads of this many pieces on their way together (past the end the first is read again, for nobody)
-        for (int w0 = f; w0 <= l; w0 += kAhead) {
-            f32x2 ml[kAhead];
-            f32x4 x[kAhead];
+    const int windows = window_tiles(a, s), r = at * G + head - hk * G, first = a.pairs[b * gm.Hkv + hk].first_tile;
+    if (first + windows + prefix > head_.tiles) return;
+    Sums sums[2];  // of the window's keys, of those before it
+    for (int kind = 0; kind < 2; ++kind) {
+        if (!(kind == plan::kWindow ? a.do_local : prefix)) continue;
+        const Tile& t = a.tiles[first + (kind == plan::kWindow ? 0 : windows)];
+        const Pieces p(Place{t.start, t.blocks}, head_);
+        if (kind == plan::kWindow && p.whole() && !prefix) return;  // written already
+        p.join(a, sums[kind], r, row_part(a, kind, token, head), c4, slice, kSlices);
+    }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int w = w0 + i <= l ? w0 + i : w0;
-                const float* part = a.slots + ((size_t)plan::slot(w, w == f) * a.tile_rows + r) * kPart;
-                ml[i] = *reinterpret_cast<const f32x2*>(part);
-                x[i] = *reinterpret_cast<const f32x4*>(part + 4 + c4);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (w0 + i <= l) sums.join(ml[i][0], ml[i][1], x[i]);
-        }
-        return true;
-    };
+    for (int kind = 0; kind < 2; ++kind) {
+        float* const out = part[kind][slice];
+        if (c4 == 0) out[0] = sums[kind].m, out[1] = sums[kind].l;
+        *reinterpret_cast<f32x4*>(out + 4 + c4) = sums[kind].o;
+    }
+    __syncthreads();
+    if (slice) return;
     const f32x4 z = {0.f, 0.f, 0.f, 0.f};
     f32x4 x = z;
     float lse_l = -INFINITY;
-    if (a.do_local) {
-        if (!pieces(a.pair_tile[pair] + code / a.tile_rows, code % a.tile_rows)) {
-            if (!prefix) return;  // written already
-            sums.join(a.parts[plan::kWindow] + (size_t)row * kPart, c4);
+    Sums all;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+#pragma unroll
+        for (int i = 0; i < kSlices; ++i) {
+            const float* const in = part[kind][i];
+            all.join(in[0], in[1], *reinterpret_cast<const f32x4*>(in + 4 + c4));
         }
-        x = sums.value(), lse_l = sums.lse();
+        if (kind == plan::kWindow && a.do_local) x = all.value(), lse_l = all.lse();
     }
-    if (prefix) {
-        const int i = plan::clamp(list_of(a, a.rank, s, hk)[code], 0, s.n * G - 1);
-        if (!pieces(a.pair_tile[pair] + window_tiles(a, s) + i / a.tile_rows, i % a.tile_rows))
-            sums.join(a.parts[plan::kPrefix] + (size_t)row * kPart, c4);
-    }
-    store_row(a, token, head, c4, x, routed ? sums.value() : z, lse_l, routed ? sums.lse() : -INFINITY);
+    store_row(a, token, head, c4, x, routed ? all.value() : z, lse_l, routed ? all.lse() : -INFINITY);
 }
 
 constexpr int kWorkgroups = 256;  // one per CU
@@ -916,16 +1040,17 @@ size_t lay_out(ExtendArgs& a, char* base) {
     };
     const size_t rows = (size_t)g.T * g.G, pairs = (size_t)g.B * g.Hkv;
     a.workgroups = kWorkgroups;
-    a.tile_rows = 32 * kWaves;
+    a.few = (long long)a.max_new * g.G <= 32;
+    a.tile_rows = a.few ? 32 : 32 * kWaves;
     a.most_tiles = (int)(2 * g.Hkv * (rows / a.tile_rows + g.B));
     take(a.head, 1);
     take(a.tiles, a.most_tiles);
     take(a.first_tile, a.workgroups);
-    take(a.pair_tile, pairs);
-    take(a.listed, pairs);
-    take(a.list, rows * g.Hkv);
-    take(a.rank, rows * g.Hkv);
-    take(a.token_seq, g.T);
+    take(a.segment, a.workgroups);
+    take(a.pairs, pairs);
+    take(a.list, a.few ? 0 : rows * g.Hkv);
+    take(a.rank, a.few ? 0 : rows * g.Hkv);
+    take(a.token_seq, a.few ? g.T : 0);
     take(a.slots, (size_t)2 * a.workgroups * a.tile_rows * kPart);
     take(a.parts[0], rows * g.Hkv * kPart);
     take(a.parts[1], rows * g.Hkv * kPart);
@@ -955,13 +1080,14 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     a.O = (__bf16*)O, a.S = (__bf16*)S, a.A = (__bf16*)A;
     a.lse_l = lse_l, a.lse_g = lse_g;
     lay_out(a, (char*)workspace);
-    {
+    if (!a.few) {
         KernelTimer kt("extend_list", st);
         hipLaunchKernelGGL(extend_list_kernel, dim3(g.B * g.Hkv), dim3(kListThreads), 0, st, a);
     }
     {
         KernelTimer kt("extend_plan", st);
-        hipLaunchKernelGGL(extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+        if (a.few) hipLaunchKernelGGL(extend_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        else hipLaunchKernelGGL(extend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
     }
     {
         KernelTimer kt("extend", st);
@@ -970,8 +1096,8 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     }
     {
         KernelTimer kt("extend_combine", st);
-        const long long rows = (long long)g.T * g.Hq;
-        hipLaunchKernelGGL(extend_combine_kernel, dim3((unsigned)((rows + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, a);
+        if (a.few) hipLaunchKernelGGL(extend_combine_few_kernel, dim3(g.T * g.Hq), dim3(32 * kSlices), 0, st, a);
+        else hipLaunchKernelGGL(extend_combine_kernel, dim3(a.most_tiles, a.tile_rows / kCombineRows), dim3(kThreads), 0, st, a);
     }
     return launch_status();
 }

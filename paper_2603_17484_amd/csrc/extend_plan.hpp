@@ -54,6 +54,13 @@ L2A_PLAN_FN int tile_blocks(const Range& k) { return k.hi < k.lo ? 0 : k.hi / kK
 // Rows of a sequence before the first one with keys before the window.
 L2A_PLAN_FN int rows_without_prefix(const Seq& s, int G, int W) { return clamp(W + 1 - s.pos, 0, s.n) * G; }
 
+// Tiles of keys before the window all begin at key 0.  Where they are longer than a stretch (`per` blocks, at least kSegmentLeast), segments of its
+// length are cut off their beginnings, as many for each tile of a KV head as its first and shortest has, so that a block remains; each is
+// the work of one workgroup.  The same segments of all tiles lie side by side, for workgroups on one XCD, which then read the same keys at the same
+// time.  What remains of the tiles is the line, for the workgroups that remain: there are some, since every segment has a stretch's length.
+constexpr int kSegmentLeast = 16;
+L2A_PLAN_FN int segments(int blocks, int per) { return blocks > 0 ? (blocks - 1) / per : 0; }
+
 // A tile's place in the line.
 struct Place {
     long long start;
