@@ -260,7 +260,7 @@ int l2a_attn_decode(const l2a_params* p, const void* q, const void* k_cache, con
  * skip such rows, l2a_attn_extend clamps them into range.
  *
  * Errors of the three calls: L2A_ERR_NULL, L2A_ERR_ALIGN as everywhere (all tensors 16-byte aligned, table and index arrays 4-byte);
- * L2A_ERR_SHAPE for page_size not a power of two in 16..1024, pages or max_pages < 1, more than 2^26 tokens per
+ * L2A_ERR_SHAPE for page_size not a power of two in 16..1024, pages or max_pages < 1, more than 2^25 tokens per
  * sequence, max_new < 1; L2A_ERR_UNSUPPORTED for p->dtype other than L2A_BF16, D other than 128, an unknown cache dtype,
  * L2A_FLAG_SCALAR, L2A_FLAG_RING_CACHE.
  */

@@ -179,52 +179,61 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scale: O
     c = l2a_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), k.shape[0], k.shape[2], table.shape[1],
                   L2A_FP8 if fp8 else L2A_BF16)
     c.tensors = (k, v, k_scale, v_scale, table)
+    c.shape, c.device = (k.shape[1], k.shape[3], table.shape[0]), k.get_device()
     return c
 
 
-def _check_packed(p: l2a_params, c: l2a_cache, seq_start, pos, rows, mask=None, stats=()) -> None:
-    """The sizes and types that the C ABI cannot see.  rows: [T, heads, D] bf16 tensors with their numbers of heads."""
-    k, table = c.tensors[0], c.tensors[4]
-    if k.shape[1] != p.Hkv or k.shape[3] != p.D or table.shape[0] != p.B:
-        raise ValueError(f"the cache has {k.shape[1]} KV heads of {k.shape[3]} channels and a table of {table.shape[0]} sequences")
-    if seq_start.dtype != torch.int32 or pos.dtype != torch.int32 or seq_start.numel() != p.B + 1 or pos.numel() != p.B:
-        raise ValueError("seq_start and pos must be int32 of B + 1 and B entries")
-    for t, heads in rows:
-        if t is not None and (t.dtype != torch.bfloat16 or t.numel() != p.T * heads * p.D):
-            raise ValueError(f"packed rows must be bfloat16 [T, {heads}, {p.D}]")
-    if mask is not None and (mask.element_size() != 1 or mask.numel() != p.mask_heads * p.T):
-        raise ValueError("mask must be [mask_heads, T] bytes")
-    for t in stats:
-        if t is not None and (t.dtype != torch.float32 or t.numel() != p.Hq * p.T):
-            raise ValueError("log-sum-exps must be float32 [Hq, T]")
-    here = torch.cuda.current_device()
-    for t in (k, seq_start, pos, mask, *(r for r, _ in rows), *stats):
-        if t is not None and t.device.index != here:
-            raise ValueError("tensors must be on the current device, whose stream the call is enqueued on")
+def _packed(t: Optional[torch.Tensor], dtype, numel: int, device: int, what: str):
+    """The address of a call's tensor, after the checks that the C ABI cannot make."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {numel} entries on the current device, whose stream the call is "
+                         f"enqueued on; got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _begin_packed(p: l2a_params, c: l2a_cache, seq_start, pos):
+    """-> device, its current stream, addresses of seq_start and pos."""
+    if c.shape != (p.Hkv, p.D, p.B):
+        raise ValueError(f"the cache has {c.shape[0]} KV heads of {c.shape[1]} channels and a table of {c.shape[2]} sequences")
+    dev = torch.cuda.current_device()
+    if c.device != dev:
+        raise ValueError("the cache must be on the current device, whose stream the call is enqueued on")
+    return (dev, torch._C._cuda_getCurrentRawStream(dev), _packed(seq_start, torch.int32, p.B + 1, dev, "seq_start"),
+            _packed(pos, torch.int32, p.B, dev, "pos"))
 
 
 def l2a_cache_write(p: l2a_params, c: l2a_cache, k, v, seq_start, pos) -> None:
-    _check_packed(p, c, seq_start, pos, ((k, p.Hkv), (v, p.Hkv)))
-    rc = lib().l2a_cache_write(ctypes.byref(p), ctypes.byref(c), _ptr(k), _ptr(v), _ptr(seq_start), _ptr(pos), _stream())
+    dev, stream, s, at = _begin_packed(p, c, seq_start, pos)
+    n = p.T * p.Hkv * p.D
+    rc = lib().l2a_cache_write(ctypes.byref(p), ctypes.byref(c), _packed(k, torch.bfloat16, n, dev, "k"),
+                               _packed(v, torch.bfloat16, n, dev, "v"), s, at, stream)
     if rc != 0:
         raise L2AError(rc, "l2a_cache_write")
 
 
 def l2a_cache_read(p: l2a_params, c: l2a_cache, seq_start, pos, k, v) -> None:
-    _check_packed(p, c, seq_start, pos, ((k, p.Hkv), (v, p.Hkv)))
-    rc = lib().l2a_cache_read(ctypes.byref(p), ctypes.byref(c), _ptr(seq_start), _ptr(pos), _ptr(k), _ptr(v), _stream())
+    dev, stream, s, at = _begin_packed(p, c, seq_start, pos)
+    n = p.T * p.Hkv * p.D
+    rc = lib().l2a_cache_read(ctypes.byref(p), ctypes.byref(c), s, at, _packed(k, torch.bfloat16, n, dev, "k"),
+                              _packed(v, torch.bfloat16, n, dev, "v"), stream)
     if rc != 0:
         raise L2AError(rc, "l2a_cache_read")
 
 
 def l2a_attn_extend(p: l2a_params, c: l2a_cache, q, seq_start, pos, mask, max_new: int, O, lse_local=None, lse_global=None,
                     S_opt=None, A_opt=None, workspace=None) -> None:
-    _check_packed(p, c, seq_start, pos, ((q, p.Hq), (O, p.Hq), (S_opt, p.Hq), (A_opt, p.Hq)), mask, (lse_local, lse_global))
+    dev, stream, s, at = _begin_packed(p, c, seq_start, pos)
     if workspace is None:
         workspace = alloc_extend_workspace(p, c, max_new)
-    rc = lib().l2a_attn_extend(ctypes.byref(p), ctypes.byref(c), _ptr(q), _ptr(seq_start), _ptr(pos), _ptr(mask), max_new, _ptr(O),
-                               _ptr(lse_local), _ptr(lse_global), _ptr(S_opt), _ptr(A_opt), _ptr(workspace),
-                               workspace.numel() if workspace is not None else 0, _stream())
+    bf, n, m = torch.bfloat16, p.T * p.Hq * p.D, p.Hq * p.T
+    rc = lib().l2a_attn_extend(ctypes.byref(p), ctypes.byref(c), _packed(q, bf, n, dev, "q"), s, at,
+                               _packed(mask, torch.uint8, p.mask_heads * p.T, dev, "mask"), max_new, _packed(O, bf, n, dev, "O"),
+                               _packed(lse_local, torch.float32, m, dev, "lse_local"), _packed(lse_global, torch.float32, m, dev, "lse_global"),
+                               _packed(S_opt, bf, n, dev, "S_opt"), _packed(A_opt, bf, n, dev, "A_opt"),
+                               None if workspace is None else _packed(workspace, torch.uint8, workspace.numel(), dev, "workspace"),
+                               0 if workspace is None else workspace.numel(), stream)
     if rc != 0:
         raise L2AError(rc, "l2a_attn_extend")
 

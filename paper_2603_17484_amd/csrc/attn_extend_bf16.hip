@@ -37,12 +37,15 @@ struct Tile {  // 64 bytes
 };
 struct Pair {  // a KV head of a sequence
     int first_tile, listed;      // its first tile, windows first; rows with keys before the window
-    int segments, first_segment; // of each of its tiles of keys before the window; the first of them
+    int segments, first_segment; // of each of its tiles of many rows with keys before the window; the first of them
 };
 struct Head {
     long long total;     // length of the line
     int per, tiles;      // its stretches; tiles on it
-    int segments, blocks;  // workgroups that have a segment, and its blocks
+    int segments, pad;   // workgroups that have a segment
+};
+struct Segment {
+    int tile, from, to;  // blocks, counted from the tile's first key on
 };
 
 struct ExtendArgs {
@@ -59,7 +62,7 @@ struct ExtendArgs {
     Tile* tiles;
     int most_tiles, workgroups, tile_rows, few;  // few: no sequence has more than 32 rows per KV head, and no lists are made
     int32_t* first_tile;  // [workgroups] of a stretch
-    int2* segment;        // [workgroups] tile and number
+    Segment* segment;     // [workgroups]
     Pair* pairs;          // [B * Hkv]
     int32_t* list;        // [Hkv][T G], a sequence's from its first row on: codes of the rows with keys before the window, ascending
     int32_t* rank;        // [Hkv][T G] place of a row in its list
@@ -74,6 +77,27 @@ __device__ __forceinline__ bool token_routed(const ExtendArgs& a, int token, int
     if (!a.mask) return true;
     const int mh = a.mask_heads == 1 ? 0 : (a.mask_heads == a.gm.Hq ? head : head / a.gm.G);
     return a.mask[(size_t)mh * a.gm.T + token] != 0;
+}
+__device__ __forceinline__ Place place_of(const ExtendArgs& a, const Tile& t) { return Place{t.start, t.blocks, plan::block_cost(t.rows, a.c.fp8)}; }
+// The decisions of a token for the heads of a KV head's group, a bit each.
+__device__ __forceinline__ unsigned group_routed(const ExtendArgs& a, int token, int hk) {
+    const int G = a.gm.G;
+    const unsigned all = (1u << G) - 1u;
+    if (!a.do_global) return 0u;
+    if (!a.mask) return all;
+    if (a.mask_heads != a.gm.Hq || G == 1) return token_routed(a, token, hk * G) ? all : 0u;
+    const uint8_t* p = a.mask + (size_t)hk * G * a.gm.T + token;
+    unsigned bits = 0;
+#pragma unroll
+    for (int g = 0; g < 16; ++g)  // the bytes' loads do not wait for one another
+        bits |= (unsigned)(g < G && p[(size_t)min(g, G - 1) * a.gm.T] != 0) << g;
+    return bits;
+}
+// Whether a row of a KV head is routed and has keys before its window.
+__device__ __forceinline__ bool has_prefix(const ExtendArgs& a, const Seq& s, int hk) {
+    unsigned any = 0;
+    for (int t = plan::rows_without_prefix(s, 1, a.gm.W); t < s.n; ++t) any |= group_routed(a, s.start + t, hk);
+    return any != 0;
 }
 __device__ __forceinline__ int window_tiles(const ExtendArgs& a, const Seq& s) {
     return a.do_local ? (s.n * a.gm.G + a.tile_rows - 1) / a.tile_rows : 0;
@@ -100,40 +124,41 @@ __device__ __forceinline__ void store_row(const ExtendArgs& a, int token, int he
     }
 }
 
-// Every thread takes consecutive tokens: their decisions counted, the counts summed over the workgroup, the rows written.
+// A thread per token, a round for every kListThreads of them: decisions counted, the counts summed over the workgroup, the rows written.
 constexpr int kListThreads = 1024;
 __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a) {
-    __shared__ int sums[kListThreads / 64];
+    __shared__ int sums[2][kListThreads / 64];
     const Geom& gm = a.gm;
     const int b = blockIdx.x / gm.Hkv, hk = blockIdx.x - b * gm.Hkv, G = gm.G;
     const Seq s = seq_of(a, b);
-    const int skip = plan::rows_without_prefix(s, G, gm.W) / G, n = s.n - skip;
-    const int each = (n + kListThreads - 1) / kListThreads;
-    const int t0 = min(skip + (int)threadIdx.x * each, s.n), t1 = min(t0 + each, s.n);
-    int count = 0;
-    for (int t = t0; t < t1; ++t)
-        for (int g = 0; g < G; ++g) count += token_routed(a, s.start + t, hk * G + g);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = count;  // of this wavefront's lanes up to this one
-    for (int o = 1; o < 64; o <<= 1) {
-        const int below = __shfl_up(upto, o);
-        if (lane >= o) upto += below;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int at = upto - count, total = 0;
-    for (int w = 0; w < kListThreads / 64; ++w) {
-        if (w < wave) at += sums[w];
-        total += sums[w];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, skip = plan::rows_without_prefix(s, 1, gm.W);
+    int32_t *list = list_of(a, a.list, s, hk), *rank = list_of(a, a.rank, s, hk);
+    int total = 0;
+    auto decisions = [&](int t) { return t < s.n ? group_routed(a, s.start + t, hk) : 0u; };
+    unsigned bits = decisions(skip + (int)threadIdx.x);
+    for (int t0 = skip, turn = 0; t0 < s.n; t0 += kListThreads, turn ^= 1) {
+        const int t = t0 + (int)threadIdx.x, count = __popc(bits);
+        const unsigned coming = decisions(t + kListThreads);
+        int upto = count;  // of this wavefront's lanes up to this one
+        for (int o = 1; o < 64; o <<= 1) {
+            const int below = __shfl_up(upto, o);
+            if (lane >= o) upto += below;
+        }
+        if (lane == 63) sums[turn][wave] = upto;
+        __syncthreads();
+        int at = total + upto - count;
+        for (int w = 0; w < kListThreads / 64; ++w) {
+            if (w < wave) at += sums[turn][w];
+            total += sums[turn][w];
+        }
+        for (; bits; bits &= bits - 1) {
+            const int code = t * G + __ffs((int)bits) - 1;
+            rank[code] = at;
+            list[at++] = code;
+        }
+        bits = coming;
     }
     if (threadIdx.x == 0) a.pairs[blockIdx.x].listed = total;
-    int32_t *list = list_of(a, a.list, s, hk), *rank = list_of(a, a.rank, s, hk);
-    for (int t = t0; t < t1; ++t)
-        for (int g = 0; g < G; ++g)
-            if (token_routed(a, s.start + t, hk * G + g)) {
-                rank[t * G + g] = at;
-                list[at++] = t * G + g;
-            }
     if (a.do_local) return;
     const f32x4 z = {0.f, 0.f, 0.f, 0.f};  // without windows, rows that are not routed have no tile
     for (int r = threadIdx.x >> 5; r < s.n * G; r += kListThreads / 32)
@@ -141,10 +166,11 @@ __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a)
 }
 
 // Sum over the threads before this one, and over all of them.
-constexpr int kPlanThreads = 1024;
+template <int THREADS>
 __device__ __forceinline__ void scan(int x, int* sums, int& before, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int upto = x;
+#pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int below = __shfl_up(upto, o);
         if (lane >= o) upto += below;
@@ -153,13 +179,24 @@ __device__ __forceinline__ void scan(int x, int* sums, int& before, int& total) 
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     before = upto - x, total = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) before += sums[w];
         total += sums[w];
     }
 }
+// A tile of a kind that begins at row `first`.
+__device__ __forceinline__ Tile make_tile(const ExtendArgs& a, const Seq& s, int b, int hk, int kind, int first, int of) {
+    Tile t{};
+    t.b = b, t.hk = hk, t.s = s, t.kind = kind, t.first = first, t.rows = min(a.tile_rows, of - first);
+    t.pos0 = s.pos + row_code(a, t, first) / a.gm.G, t.pos1 = s.pos + row_code(a, t, first + t.rows - 1) / a.gm.G;
+    const Range k = plan::tile_keys(kind, t.pos0, t.pos1, a.gm.W);
+    t.lo = k.lo, t.hi = k.hi;
+    t.blocks = plan::tile_blocks(k);
+    return t;
+}
 // A thread per KV head of a sequence, then one per tile, then one per stretch's beginning.
-template <bool FEW>
+constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a) {
     __shared__ int sums[kPlanThreads / 64];
     __shared__ int ends[kPlanThreads];  // tiles up to and with a pair, of the pairs at hand
@@ -169,25 +206,21 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     long long line = 0;   // where the next tile begins
     for (int p0 = 0; p0 < pairs; p0 += kPlanThreads) {
         const int mine = p0 + (int)threadIdx.x;
-        int count = 0, windows = 0, listed = 0;
-        Seq s{};
+        int count = 0, listed = 0;
         if (mine < pairs) {
             const int b = mine / gm.Hkv, hk = mine - b * gm.Hkv;
-            s = seq_of(a, b);
-            windows = window_tiles(a, s);
-            if constexpr (FEW) {  // one tile of all the sequence's rows, if one of them is routed and has keys before the window
-                bool any = false;
-                for (int r = plan::rows_without_prefix(s, G, gm.W); r < s.n * G; ++r) any |= token_routed(a, s.start + r / G, hk * G + r % G);
-                listed = any ? s.n * G : 0;
+            const Seq s = seq_of(a, b);
+            if (a.few) {  // one tile of all the sequence's rows
+                listed = has_prefix(a, s, hk) ? s.n * G : 0;
                 if (hk == 0)
                     for (int i = 0; i < s.n; ++i) a.token_seq[s.start + i] = b;
             } else {
                 listed = min(a.pairs[mine].listed, s.n * G);
             }
-            count = windows + (listed + a.tile_rows - 1) / a.tile_rows;
+            count = window_tiles(a, s) + (listed + a.tile_rows - 1) / a.tile_rows;
         }
         int before, here;
-        scan(count, sums, before, here);
+        scan<kPlanThreads>(count, sums, before, here);
         if (mine < pairs) a.pairs[mine] = Pair{tiles + before, listed, 0, 0};
         ends[threadIdx.x] = before + count;
         __syncthreads();
@@ -203,19 +236,14 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                     if (ends[mid] > i) hi = mid;
                     else lo = mid + 1;
                 }
-                t.b = (p0 + lo) / gm.Hkv, t.hk = p0 + lo - t.b * gm.Hkv;
-                t.s = seq_of(a, t.b);
-                const int w = window_tiles(a, t.s), within = i - (lo ? ends[lo - 1] : 0), rows = t.s.n * G;
-                t.kind = within < w ? plan::kWindow : plan::kPrefix;
-                t.first = (t.kind == plan::kWindow ? within : within - w) * a.tile_rows;
-                t.rows = min(a.tile_rows, (t.kind == plan::kWindow || FEW ? rows : min(a.pairs[p0 + lo].listed, rows)) - t.first);
-                t.pos0 = t.s.pos + row_code(a, t, t.first) / G, t.pos1 = t.s.pos + row_code(a, t, t.first + t.rows - 1) / G;
-                const Range k = plan::tile_keys(t.kind, t.pos0, t.pos1, gm.W);
-                t.lo = k.lo, t.hi = k.hi;
-                t.blocks = plan::tile_blocks(k);
+                const int b = (p0 + lo) / gm.Hkv, hk = p0 + lo - b * gm.Hkv;
+                const Seq s = seq_of(a, b);
+                const int w = window_tiles(a, s), within = i - (lo ? ends[lo - 1] : 0);
+                if (within < w) t = make_tile(a, s, b, hk, plan::kWindow, within * a.tile_rows, s.n * G);
+                else t = make_tile(a, s, b, hk, plan::kPrefix, (within - w) * a.tile_rows, a.pairs[p0 + lo].listed);
             }
             int at, sum;
-            scan(on ? t.blocks + plan::kStart : 0, sums, at, sum);
+            scan<kPlanThreads>(on ? (int)place_of(a, t).end() : 0, sums, at, sum);
             if (on) {
                 t.start = line + at;
                 a.tiles[tiles + i] = t;
@@ -226,19 +254,21 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
         __syncthreads();
     }
     tiles = min(tiles, a.most_tiles);
-    int per = max(plan::stretch(line, a.workgroups), 1), segments = 0, segment_blocks = per;
-    if (!FEW && a.do_global && per >= plan::kSegmentLeast) {
+    const int dearest = plan::block_cost(a.tile_rows, a.c.fp8);
+    int per = plan::stretch(line, a.workgroups, dearest), segments = 0;
+    const int segment = per / dearest;  // blocks
+    if (!a.few && a.do_global && segment >= plan::kSegmentLeast) {
         for (int p0 = 0; p0 < pairs; p0 += kPlanThreads) {  // how many each pair has
             const int mine = p0 + (int)threadIdx.x;
             int each = 0, of = 0;
             if (mine < pairs) {
                 const Pair p = a.pairs[mine];
                 const int first = p.first_tile + window_tiles(a, seq_of(a, mine / gm.Hkv));
-                of = (p.listed + a.tile_rows - 1) / a.tile_rows;
-                if (of && first + of <= tiles) each = plan::segments(a.tiles[first].blocks, per);
+                of = plan::many_tiles(p.listed, a.tile_rows);
+                if (of && first + of <= tiles) each = plan::segments(a.tiles[first].blocks, segment);
             }
             int before, here;
-            scan(each * of, sums, before, here);
+            scan<kPlanThreads>(each * of, sums, before, here);
             if (mine < pairs) a.pairs[mine].segments = each, a.pairs[mine].first_segment = segments + before;
             segments += here;
         }
@@ -251,34 +281,34 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
         line = 0;
         for (int i0 = 0; i0 < tiles; i0 += kPlanThreads) {  // which they are, and the line without them
             const int i = i0 + (int)threadIdx.x;
-            int blocks = 0, skip = 0;
+            Tile t{};
             if (i < tiles) {
-                const Tile& t = a.tiles[i];
-                blocks = t.blocks;
+                t = a.tiles[i];
                 const Pair p = a.pairs[t.b * gm.Hkv + t.hk];
-                if (t.kind == plan::kPrefix && p.segments) {
-                    skip = p.segments * per;
-                    blocks = max(blocks - skip, 0);
-                    const int of = (p.listed + a.tile_rows - 1) / a.tile_rows;
+                const int of = plan::many_tiles(p.listed, a.tile_rows), j = t.first / a.tile_rows;
+                if (t.kind == plan::kPrefix && j < of && p.segments) {
+                    t.skip = p.segments * segment;
+                    t.blocks = max(t.blocks - t.skip, 0);
                     for (int k = 0; k < p.segments; ++k) {
-                        const int w = p.first_segment + k * of + t.first / a.tile_rows;
-                        if (w < a.workgroups) a.segment[w] = int2{i, k};
+                        const int w = p.first_segment + k * of + j;
+                        if (w < a.workgroups) a.segment[w] = Segment{i, k * segment, (k + 1) * segment};
                     }
                 }
+                t.start = 0;
             }
             int at, sum;
-            scan(i < tiles ? blocks + plan::kStart : 0, sums, at, sum);
-            if (i < tiles) a.tiles[i].start = line + at, a.tiles[i].blocks = blocks, a.tiles[i].skip = skip;
+            scan<kPlanThreads>(i < tiles ? (int)place_of(a, t).end() : 0, sums, at, sum);
+            if (i < tiles) a.tiles[i].start = line + at, a.tiles[i].blocks = t.blocks, a.tiles[i].skip = t.skip;
             line += sum;
         }
-        per = max(plan::stretch(line, max(a.workgroups - segments, 1)), 1);
+        per = plan::stretch(line, max(a.workgroups - segments, 1), dearest);
     }
-    if (threadIdx.x == 0) *a.head = Head{line, per, tiles, segments, segment_blocks};
+    if (threadIdx.x == 0) *a.head = Head{line, per, tiles, segments, 0};
     __syncthreads();
     // the tile each stretch begins in
     for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
-        const Place p{a.tiles[i].start, a.tiles[i].blocks};
-        for (long long w = (p.start + per - 1) / per; w * per < p.start + p.length() && w < a.workgroups; ++w) a.first_tile[w] = i;
+        const Place p = place_of(a, a.tiles[i]);
+        for (long long w = (p.start + per - 1) / per; w * per < p.end() && w < a.workgroups; ++w) a.first_tile[w] = i;
     }
 }
 
@@ -321,18 +351,16 @@ __device__ __forceinline__ void store_converted(const u32x4& x, uint32_t exponen
     at[0] = y[0], at[1] = y[1];
 }
 
-// Shared memory of a workgroup, in bytes from its beginning: rings of blocks of K and of V; e4m3: rings of what was loaded (K, V, their
-// exponents: every wavefront's pieces its own, which it alone converts) and of the bf16 blocks made of it.  Blocks are loaded two
-// walks of the loop ahead of their use.
-constexpr int kWaves = 8;  // of a workgroup: up to 32 rows each
-template <bool FP8>
+// Shared memory of a workgroup of NW wavefronts, in bytes from its beginning: rings of blocks of K and of V; e4m3: rings of what was loaded
+// (K, V, their exponents: every wavefront's pieces its own, which it alone converts) and of the bf16 blocks made of it.  Blocks are
+// loaded two walks of the loop ahead of their use.
+template <bool FP8, int NW>
 struct Lds {
     static constexpr int kK = FP8 ? 3 : 4, kV = FP8 ? 3 : 4, kRaw = 2;
     static constexpr unsigned k = 0, v = k + kK * kBlockBytes, raw_k = v + kV * kBlockBytes;
-    static constexpr unsigned kRawBlock = kWaves * 1024, kRawScales = kWaves * 256;
+    static constexpr unsigned kRawBlock = kKeys * kD, kRawScales = kKeys / 8 * 256;
     static constexpr unsigned raw_v = raw_k + kRaw * kRawBlock, raw_ks = raw_v + kRaw * kRawBlock, raw_vs = raw_ks + kRaw * kRawScales;
-    static constexpr unsigned used = FP8 ? raw_vs + kRaw * kRawScales : raw_k, sums = kWaves * 32 * kPart * 4;  // (sums: few_rows)
-    static constexpr unsigned bytes = used > sums ? used : sums;
+    static constexpr unsigned used = FP8 ? raw_vs + kRaw * kRawScales : raw_k;
 };
 // A place in a ring of `of` blocks of `each` bytes that begins at `first`, moved on.
 __device__ __forceinline__ unsigned next(unsigned at, unsigned first, unsigned each, int of) {
@@ -343,6 +371,7 @@ __device__ __forceinline__ unsigned next(unsigned at, unsigned first, unsigned e
 #define FENCE() __builtin_amdgcn_sched_barrier(0)
 #define scalar __attribute__((address_space(4)))  // read through the scalar cache: the same for all lanes, written by earlier launches
 
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }  // of all lanes
 template <typename X>
 __device__ __forceinline__ X uniform(const X* p) {
     struct Words {
@@ -354,12 +383,14 @@ __device__ __forceinline__ X uniform(const X* p) {
 }
 
 // The blocks of a piece on their way to LDS.  Block i + 1 of K and block i of V go together (group i): a block's scores are computed
-// before the block ahead of it is multiplied with V.  A wavefront loads 8 rows of every block, which lie in one page.
-template <bool FP8>
+// before the block ahead of it is multiplied with V.  A wavefront loads its share of every block, 16 rows or 8, which lie in one page.
+template <bool FP8, int NW>
 struct Loader {
-    typedef Lds<FP8> L;
+    typedef Lds<FP8, NW> L;
     static constexpr int kRowBytes = FP8 ? kD : kD * 2;
-    static constexpr int kGroup = 4;  // instructions of a group: K and V, two each (e4m3: elements and exponents)
+    static constexpr int kShare = kKeys / NW, kRows = FP8 ? 8 : 4, kEach = kShare / kRows;  // rows of a wavefront, of an instruction; instructions
+    static constexpr int kHalf = kEach * (FP8 ? 2 : 1);  // instructions for K (e4m3: elements and exponents), and for V
+    static constexpr unsigned kApart = FP8 ? 1024 : kFour;  // what the instructions' rows are apart in LDS
     const ExtendArgs& a;
     const scalar int32_t* table;
     int hk, lo, hi, jb0, blocks;  // keys lo .. hi may be read; blocks jb0 .. jb0 + blocks - 1
@@ -368,60 +399,88 @@ struct Loader {
     unsigned k_to, v_to, ks_to, vs_to;  // where the next K and V go
     // the next group's K and V: the row of the pool where this wavefront's begin, and how many bytes behind that this lane's are
     size_t row_k, row_v;
-    unsigned off_k[2], off_v[2];
+    unsigned off_k[kHalf], off_v[kHalf];
 
+    __device__ __forceinline__ unsigned k0() const { return (FP8 ? L::raw_k : L::k) + wave * kEach * kApart; }
+    __device__ __forceinline__ unsigned v0() const { return (FP8 ? L::raw_v : L::v) + wave * kEach * kApart; }
     __device__ __forceinline__ void start() {
         issued = -2;
-        k_to = FP8 ? L::raw_k + wave * 1024 : L::k + wave * 2 * kFour, v_to = FP8 ? L::raw_v + wave * 1024 : L::v + wave * 2 * kFour;
-        ks_to = L::raw_ks + wave * 256, vs_to = L::raw_vs + wave * 256;
+        k_to = k0(), v_to = v0();
+        ks_to = L::raw_ks + wave * kEach * 256, vs_to = L::raw_vs + wave * kEach * 256;
         find(0);
     }
     // Keys out of lo .. hi (before the first row's window: their pages may have been given back; behind the last row: not written yet)
     // repeat the nearest key inside: always masked, and what lies in such rows must not meet a zero weight.
     __device__ __forceinline__ void find(int block) {
-        const int k0 = (jb0 + block) * kKeys + wave * 8, first = plan::clamp(k0, lo & -8, hi & -8);
+        const int key = (jb0 + block) * kKeys + wave * kShare, first = plan::clamp(key, lo & -kShare, hi & -kShare);
         row_k = pool_row(a.c, a.gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), hk, first);
-        int mine[2] = {load_row<FP8>(lane), load_row<FP8>(lane) + 4};  // rows behind the first
-        if (k0 < lo || k0 + 7 > hi) {
+        int mine[kEach];  // rows behind the first
 #pragma unroll
-            for (int e = 0; e < 2; ++e) mine[e] = plan::clamp(k0 + mine[e], lo, hi) - first;
+        for (int e = 0; e < kEach; ++e) mine[e] = e * kRows + load_row<FP8>(lane);
+        if (key < lo || key + kShare - 1 > hi) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) mine[e] = plan::clamp(key + mine[e], lo, hi) - first;
         }
-        off_k[0] = mine[0] * kRowBytes + load_chunk<FP8>(lane) * 16;
-        off_k[1] = FP8 ? mine[0] * kRowScales : mine[1] * kRowBytes + load_chunk<FP8>(lane) * 16;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            off_k[e] = mine[e] * kRowBytes + load_chunk<FP8>(lane) * 16;
+            if (FP8) off_k[kHalf - kEach + e] = mine[e] * kRowScales;
+        }
     }
-    __device__ __forceinline__ void issue() {  // the next group, as far as there is one
+    // The next group, as far as there is one: its instructions one by one (K's, then V's), then what comes after it.
+    __device__ __forceinline__ bool has_k() const { return issued + 2 < blocks; }
+    __device__ __forceinline__ bool has_v() const { return issued + 1 >= 0 && issued + 1 < blocks; }
+    __device__ __forceinline__ void issue_one(const char* pool, const unsigned char* scales, size_t row, const unsigned* off, unsigned to, unsigned scales_to, int e) const {
+        if (!FP8 || e < kEach) dma16_so(pool + row * kRowBytes, off[e], to + e * kApart);
+        else dma4_so(scales + row * kRowScales, off[e], scales_to + (e - kEach) * 256);
+    }
+    __device__ __forceinline__ void issue_k(int e) const {
+        if (has_k()) issue_one(a.c.k, a.c.ks, row_k, off_k, k_to, ks_to, e);
+    }
+    __device__ __forceinline__ void issue_v(int e) const {
+        if (has_v()) issue_one(a.c.v, a.c.vs, row_v, off_v, v_to, vs_to, e);
+    }
+    __device__ __forceinline__ void advance() {
         const int i = ++issued;
-        if (i + 1 < blocks) {
-            dma16_so(a.c.k + row_k * kRowBytes, off_k[0], k_to);
-            if constexpr (FP8) dma4_so(a.c.ks + row_k * kRowScales, off_k[1], ks_to);
-            else dma16_so(a.c.k + row_k * kRowBytes, off_k[1], k_to + kFour);
-        }
         if (i >= 0) {
-            if (i < blocks) {
-                dma16_so(a.c.v + row_v * kRowBytes, off_v[0], v_to);
-                if constexpr (FP8) dma4_so(a.c.vs + row_v * kRowScales, off_v[1], vs_to);
-                else dma16_so(a.c.v + row_v * kRowBytes, off_v[1], v_to + kFour);
-            }
-            v_to = FP8 ? next(v_to, L::raw_v + wave * 1024, L::kRawBlock, L::kRaw) : next(v_to, L::v + wave * 2 * kFour, kBlockBytes, L::kV);
-            if (FP8) vs_to = next(vs_to, L::raw_vs + wave * 256, L::kRawScales, L::kRaw);
+            v_to = next(v_to, v0(), FP8 ? L::kRawBlock : kBlockBytes, FP8 ? L::kRaw : L::kV);
+            if (FP8) vs_to = next(vs_to, L::raw_vs + wave * kEach * 256, L::kRawScales, L::kRaw);
         }
-        k_to = FP8 ? next(k_to, L::raw_k + wave * 1024, L::kRawBlock, L::kRaw) : next(k_to, L::k + wave * 2 * kFour, kBlockBytes, L::kK);
-        if (FP8) ks_to = next(ks_to, L::raw_ks + wave * 256, L::kRawScales, L::kRaw);
-        row_v = row_k, off_v[0] = off_k[0], off_v[1] = off_k[1];
+        k_to = next(k_to, k0(), FP8 ? L::kRawBlock : kBlockBytes, FP8 ? L::kRaw : L::kK);
+        if (FP8) ks_to = next(ks_to, L::raw_ks + wave * kEach * 256, L::kRawScales, L::kRaw);
+        row_v = row_k;
+#pragma unroll
+        for (int e = 0; e < kHalf; ++e) off_v[e] = off_k[e];
         find(min(i + 2, blocks - 1));
+    }
+    __device__ __forceinline__ void issue() {
+#pragma unroll
+        for (int e = 0; e < kHalf; ++e) issue_k(e);
+#pragma unroll
+        for (int e = 0; e < kHalf; ++e) issue_v(e);
+        advance();
     }
     // Waits until at most the last group is on its way; those at the end have half their loads or none.
     __device__ __forceinline__ void wait() const {
-        constexpr int half = kGroup / 2;
-        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * half) : "memory");
-        else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(half) : "memory");
+        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kHalf) : "memory");
+        else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalf) : "memory");
         else dma_wait();
     }
-    // e4m3: this wavefront's pieces of a loaded block (the raw-th of the ring) become bf16.
+    // e4m3: this wavefront's pieces of a loaded block (the slot-th of the ring) become bf16.
+    struct Raw {
+        u32x4 x;
+        uint32_t exponents;
+    };
+    __device__ __forceinline__ Raw raw_piece(unsigned raw, unsigned raw_scales, int slot, int e) const {
+        return Raw{*(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(raw + slot * L::kRawBlock + (wave * kEach + e) * 1024 + lane * 16),
+                   *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)(raw_scales + slot * L::kRawScales + (wave * kEach + e) * 256 + lane * 4)};
+    }
+    __device__ __forceinline__ void store_piece(const Raw& r, unsigned block, int e) const {
+        store_converted(r.x, r.exponents, (lds_ptr)(uintptr_t)block, wave * kShare + e * kRows + load_row<true>(lane), lane);
+    }
     __device__ __forceinline__ void convert(unsigned raw, unsigned raw_scales, int slot, unsigned block) const {
-        const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(raw + slot * L::kRawBlock + wave * 1024 + lane * 16);
-        const uint32_t e = *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)(raw_scales + slot * L::kRawScales + wave * 256 + lane * 4);
-        store_converted(x, e, (lds_ptr)(uintptr_t)block, wave * 8 + load_row<true>(lane), lane);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) store_piece(raw_piece(raw, raw_scales, slot, e), block, e);
     }
 };
 
@@ -467,7 +526,11 @@ __device__ __forceinline__ float largest(const f32x16& s) {
 // through shared memory of its own and with sums of its own, so that none waits for another before the end, where the eight sums are joined.
 // (All wavefronts loading blocks of 64 keys for two of them to compute: 217 us for 64 sequences of 8K tokens in e4m3, 1.5 us a block.)
 constexpr int kSub = 32;
-template <bool FP8>
+template <int NW>
+struct FewLds {
+    static constexpr unsigned block = kSub / 4 * kFour, keys = NW * 2 * block, sums = NW * 32 * kPart * 4, used = keys > sums ? keys : sums;
+};
+template <bool FP8, int NW>
 __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -480,9 +543,7 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
     const int sb1 = min(2 * jb1, t.hi / kSub + 1), sb0 = max(2 * jb0, t.lo / kSub) + wave;  // sub-blocks sb0, sb0 + 8, .. below sb1
 
     __syncthreads();  // LDS is free
-    constexpr int kSubBytes = kSub / 4 * kFour;
-    static_assert(Lds<FP8>::bytes >= kWaves * 2 * kSubBytes, "room for every wavefront's keys");
-    const unsigned k_to = wave * 2 * kSubBytes, v_to = k_to + kSubBytes;
+    const unsigned k_to = wave * 2 * FewLds<NW>::block, v_to = k_to + FewLds<NW>::block;
     const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
     constexpr int kRows = FP8 ? 8 : 4, kEach = kSub / kRows;  // rows of an instruction, which lie in one page; instructions
     const int mine = load_row<FP8>(lane);
@@ -542,9 +603,9 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
     const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
     RowSums row;
     row.clear();
-    for (int sb = sb0; sb < sb1; sb += kWaves) {
-        const bool more = sb + kWaves < sb1;
-        if (more) find(sb + kWaves);
+    for (int sb = sb0; sb < sb1; sb += NW) {
+        const bool more = sb + NW < sb1;
+        if (more) find(sb + NW);
         if constexpr (FP8) convert(kx, kse, k_to);
         else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
         bf16x8 op[8];
@@ -595,7 +656,6 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
     // ---- the eight wavefronts' sums, joined: 16 threads per row, eight channels each
     row.l += __shfl_xor(row.l, 32);
     float* const sums = reinterpret_cast<float*>(lds);  // [wave][row][kPart]
-    static_assert(Lds<FP8>::bytes >= kWaves * 32 * kPart * sizeof(float), "room for the wavefronts' sums");
     __syncthreads();  // every wavefront is done with its part of LDS
     {
         float* const at = sums + (wave * 32 + n) * kPart;
@@ -607,80 +667,167 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
                 *reinterpret_cast<f32x4*>(at + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
     }
     __syncthreads();
-    const int r = threadIdx.x >> 4, c8 = (threadIdx.x & 15) * 8;
-    if (r >= t.rows) return;
-    float m = kNone, l = 0.f;
-    f32x2 ml[kWaves];
+    const int c8 = (threadIdx.x & 15) * 8;
+    for (int r = threadIdx.x >> 4; r < t.rows; r += NW * 4) {
+        float m = kNone, l = 0.f;
+        f32x2 ml[NW];
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-        ml[v] = *reinterpret_cast<const f32x2*>(sums + (v * 32 + r) * kPart);
-        m = fmaxf(m, ml[v][0]);
-    }
-    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+        for (int v = 0; v < NW; ++v) {
+            ml[v] = *reinterpret_cast<const f32x2*>(sums + (v * 32 + r) * kPart);
+            m = fmaxf(m, ml[v][0]);
+        }
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-        const float by = fast_exp2(ml[v][0] - m);
-        const f32x4* const at = reinterpret_cast<const f32x4*>(sums + (v * 32 + r) * kPart + 4 + c8);
-        l = fmaf(ml[v][1], by, l);
-        x += at[0] * by, y += at[1] * by;
-    }
-    const int my_code = code_of(r), my_tok = my_code / G, head = hk * G + my_code - my_tok * G, token = t.s.start + my_tok;
-    const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
-    if (whole && t.kind == plan::kWindow && !(t.s.pos + my_tok > gm.W && routed)) {
-        const float inv = 1.f / l, lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
-        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-        x *= inv, y *= inv;
-        store_row(a, token, head, c8, x, routed ? x : z, lse, routed ? lse : -INFINITY);
-        store_row(a, token, head, c8 + 4, y, routed ? y : z, lse, routed ? lse : -INFINITY);
-    } else {
-        float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                           : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-        if (c8 == 0) *reinterpret_cast<f32x2*>(out) = f32x2{m, l};
-        *reinterpret_cast<f32x4*>(out + 4 + c8) = x;
-        *reinterpret_cast<f32x4*>(out + 4 + c8 + 4) = y;
+        for (int v = 0; v < NW; ++v) {
+            const float by = fast_exp2(ml[v][0] - m);
+            const f32x4* const at = reinterpret_cast<const f32x4*>(sums + (v * 32 + r) * kPart + 4 + c8);
+            l = fmaf(ml[v][1], by, l);
+            x += at[0] * by, y += at[1] * by;
+        }
+        const int my_code = code_of(r), my_tok = my_code / G, head = hk * G + my_code - my_tok * G, token = t.s.start + my_tok;
+        const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
+        if (whole && t.kind == plan::kWindow && !(t.s.pos + my_tok > gm.W && routed)) {
+            const float inv = 1.f / l, lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
+            const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+            x *= inv, y *= inv;
+            store_row(a, token, head, c8, x, routed ? x : z, lse, routed ? lse : -INFINITY);
+            store_row(a, token, head, c8 + 4, y, routed ? y : z, lse, routed ? lse : -INFINITY);
+        } else {
+            float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
+                               : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+            if (c8 == 0) *reinterpret_cast<f32x2*>(out) = f32x2{m, l};
+            *reinterpret_cast<f32x4*>(out + 4 + c8) = x;
+            *reinterpret_cast<f32x4*>(out + 4 + c8 + 4) = y;
+        }
     }
 }
 
+// Workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring segments and stretches.
+__device__ __forceinline__ int workgroup(const ExtendArgs& a) { return (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3); }
+// A workgroup's pieces, in order: f(tile, piece, workgroup).
+template <typename F>
+__device__ __forceinline__ void for_pieces(const ExtendArgs& a, F&& f) {
+    const int w = workgroup(a);
+    const Head line = uniform(a.head);
+    const bool segment = w < line.segments;  // all it does; the others share the line
+    const int stretch = w - line.segments;
+    if (!segment && (long long)stretch * line.per >= line.total) return;
+    const Segment mine = segment ? uniform(a.segment + w) : Segment{uniform(a.first_tile + stretch), 0, 0};
+    const long long x1 = (long long)(stretch + 1) * line.per;
+    for (int T = mine.tile; T < line.tiles; ++T) {
+        const Tile t = uniform(a.tiles + T);
+        plan::Piece piece{mine.from - t.skip, mine.to - t.skip, 0, 0};
+        if (!segment) {
+            if (t.start >= x1) break;
+            piece = plan::piece(place_of(a, t), line.per, stretch);
+            if (piece.from == piece.to) continue;
+        } else if (T != mine.tile) {
+            break;
+        }
+        f(t, piece, w);
+    }
+}
+// Shared memory is written and read by address: all of it there is begins at 0.
+__device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory"); }
+
+// Calls whose sequences all have few rows.  SELF: every workgroup makes the plan for itself, a thread per KV head of a sequence (at most as
+// many as threads), and the first one leaves it for the last kernel: a launch less.
+constexpr int kFewWaves = 8, kFewPairs = 64 * kFewWaves;
+struct FewPlan {
+    int start[2 * kFewPairs], of[2 * kFewPairs];  // of a tile: its place in the line; twice its pair, plus its kind
+    Seq seq[kFewPairs];
+    int sums[kFewWaves], first;
+};
+template <bool FP8, bool SELF>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void extend_few_kernel(ExtendArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[FewLds<kFewWaves>::used + (SELF ? sizeof(FewPlan) : 0)];
+    by_address(lds);
+    if constexpr (!SELF) {
+        for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) { few_rows<FP8, kFewWaves>(a, lds, t, piece, w); });
+    } else {
+        FewPlan& plan_ = *reinterpret_cast<FewPlan*>(lds + FewLds<kFewWaves>::used);
+        const Geom& gm = a.gm;
+        const int w = workgroup(a), mine = threadIdx.x, pairs = gm.B * gm.Hkv;
+        Tile t[2];
+        bool on[2] = {false, false};
+        Seq s{};
+        const int b = mine / gm.Hkv, hk = mine - b * gm.Hkv;
+        if (mine < pairs) {
+            s = seq_of(a, b);
+            on[plan::kWindow] = a.do_local && s.n;
+            on[plan::kPrefix] = has_prefix(a, s, hk);
+            plan_.seq[mine] = s;
+        }
+        int steps[2] = {0, 0};
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            if (on[kind]) {
+                t[kind] = make_tile(a, s, b, hk, kind, 0, s.n * gm.G);
+                steps[kind] = (int)place_of(a, t[kind]).end();
+            }
+        int T, tiles, at, total;
+        scan<64 * kFewWaves>(on[0] + on[1], plan_.sums, T, tiles);
+        scan<64 * kFewWaves>(steps[0] + steps[1], plan_.sums, at, total);
+        total = same(total), tiles = same(tiles);
+        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(1, FP8))), x0 = w * per;
+        const Pair pair{T, on[plan::kPrefix] ? s.n * gm.G : 0, 0, 0};
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            if (on[kind]) {
+                plan_.start[T] = at, plan_.of[T] = 2 * mine + kind;
+                if (at <= x0 && x0 < at + steps[kind]) plan_.first = T;
+                if (w == 0) {
+                    t[kind].start = at;
+                    a.tiles[T] = t[kind];
+                }
+                ++T, at += steps[kind];
+            }
+        if (w == 0 && mine < pairs) {
+            a.pairs[mine] = pair;
+            if (hk == 0)
+                for (int i = 0; i < s.n; ++i) a.token_seq[s.start + i] = b;
+            if (mine == 0) *a.head = Head{total, per, tiles, 0, 0};
+        }
+        __syncthreads();
+        if (x0 >= total) return;
+        for (int i = same(plan_.first); i < tiles; ++i) {
+            const int start = same(plan_.start[i]), of = same(plan_.of[i]);
+            if (start >= x0 + per) break;
+            const int p = of >> 1, tb = same(p / gm.Hkv);
+            const Seq ts{same(plan_.seq[p].start), same(plan_.seq[p].n), same(plan_.seq[p].pos)};
+            Tile tile = make_tile(a, ts, tb, p - tb * gm.Hkv, of & 1, 0, ts.n * gm.G);
+            tile.start = start, tile.pos0 = same(tile.pos0), tile.pos1 = same(tile.pos1), tile.lo = same(tile.lo), tile.hi = same(tile.hi), tile.blocks = same(tile.blocks);
+            const plan::Piece piece = plan::piece(place_of(a, tile), per, w);
+            if (piece.from != piece.to) few_rows<FP8, kFewWaves>(a, lds, tile, piece, w);
+        }
+    }
+}
+
+// Tiles of up to 256 rows by 8 wavefronts of 32, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself,
+// every operand serving two matrix instructions: 1732 us at 4096 tokens behind 126976, 385 at 2048 behind 32768, now 1698 and 342.
+// A wavefront alone issues one instruction at a time, and its scalar ones and waits are then not beside anything.)
+constexpr int kWaves = 8;
 template <bool FP8>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
-    typedef Lds<FP8> L;
-    __shared__ __attribute__((aligned(1024))) char lds[L::bytes];  // all there is: places in it are its addresses
+    typedef Lds<FP8, kWaves> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::used > FewLds<kWaves>::used ? L::used : FewLds<kWaves>::used];
+        by_address(lds);
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5, G = gm.G;
     const float c2 = gm.scale_log2;
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
-    asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory");  // (it is written and read by address)
-    // workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring stretches
-    const int w = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);
-    const Head line = uniform(a.head);
-    const bool segment = w < line.segments;  // all it does; the others share the line
-    const int stretch = w - line.segments;
-    if (!segment && (long long)stretch * line.per >= line.total) return;
-    const int2 mine = segment ? uniform(a.segment + w) : int2{uniform(a.first_tile + stretch), 0};
-    const long long x1 = (long long)(stretch + 1) * line.per;
 
-    for (int T = mine.x; T < line.tiles; ++T) {
-        const Tile t = uniform(a.tiles + T);
-        plan::Piece piece{mine.y * line.blocks - t.skip, (mine.y + 1) * line.blocks - t.skip, 0, 0};
-        if (!segment) {
-            if (t.start >= x1) break;
-            piece = plan::piece(Place{t.start, t.blocks}, line.per, stretch);
-            if (piece.from == piece.to) continue;
-        } else if (T != mine.x) {
-            break;
-        }
-        const int b = t.b, hk = t.hk;
-        const Seq s = t.s;
+    for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
         if (t.rows <= 32) {
-            few_rows<FP8>(a, lds, t, piece, w);
-            continue;
+            few_rows<FP8, kWaves>(a, lds, t, piece, w);
+            return;
         }
-
-        const int jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
+        const int hk = t.hk, jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
+        const Seq s = t.s;
         __syncthreads();  // LDS is free
-        Loader<FP8> load{a, (const scalar int32_t*)(a.c.table + (size_t)b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
+        Loader<FP8, kWaves> load{a, (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
         load.start();
         load.issue();
         load.issue();
@@ -688,10 +835,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         // ---- this lane's row (rows past the end repeat the last one: computed, never written).  Up to 128 rows: wavefronts 4 .. 7 take
         // the second half of the keys of every block for the rows of wavefronts 0 .. 3.
         const bool halves = t.rows <= 32 * kWaves / 2;
-        const int r = (halves ? wave & 3 : wave) * 32 + n;
+        const int r = (halves ? wave & (kWaves / 2 - 1) : wave) * 32 + n;
         const bool valid = r < t.rows, wave_on = r - n < t.rows;
-        const int code = row_code(a, t, t.first + min(r, t.rows - 1));
-        const int local_tok = code / G, g = code - local_tok * G, head = hk * G + g, token = s.start + local_tok, pos = s.pos + local_tok;
+        const int code = row_code(a, t, t.first + min(r, t.rows - 1)), tok = code / G, token = s.start + tok, head = hk * G + code - tok * G, pos = s.pos + tok;
         const Range keys = plan::row_keys(t.kind, pos, gm.W);
         bf16x8 qreg[8];
         const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
@@ -702,13 +848,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         // blocks that every row of the tile sees whole: from `whole0` to `whole1` - 1
         const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
         const int whole0 = (lo_max + kKeys - 1) / kKeys, whole1 = (hi_min + 1) / kKeys;
+        auto masked = [&](int jb) __attribute__((always_inline)) { return jb < whole0 || jb >= whole1; };
         // scores of 32 keys from k0 on, those out of the row's reach taken out
         auto mask = [&](f32x16& sc, int k0) __attribute__((always_inline)) {
             const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
         };
-        auto masked = [&](int jb) __attribute__((always_inline)) { return jb < whole0 || jb >= whole1; };
 
         RowSums row;
         row.clear();
@@ -752,15 +898,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         auto v_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + v_mine); };
         // Weights of a pair of scores, rounded to bf16; the sum is that of the weights as the matrix cores see them, so that what
         // they are divided by is exact for them.
-        auto weigh = [&](const f32x16& sc, int e) __attribute__((always_inline)) {
-            f32x2 f = {fast_exp2(fmaf(sc[e], c2, -row.m)), fast_exp2(fmaf(sc[e + 1], c2, -row.m))};
+        auto weight = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return fast_exp2(fmaf(sc[e], c2, -row.m)); };
+        auto pair = [&](float x, float y) __attribute__((always_inline)) {
+            f32x2 f = {x, y};
             const bf16x2 pb = __builtin_convertvector(f, bf16x2);
             row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
             return __builtin_bit_cast(uint32_t, pb);
         };
         if (halves) {
             // One half of 32 keys per wavefront and block, all operands read ahead; short of rows, the loads set the pace.
-            const int half = wave >> 2;
+            const int half = wave / (kWaves / 2);
             for (int j = 0; j < blocks; ++j) {
                 begin(j);
                 if (wave_on) {
@@ -778,7 +925,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
                     row.look(largest(sc) * c2);
                     u32x4 p[2];
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) p[e >> 3][(e & 7) >> 1] = weigh(sc, e);
+                    for (int e = 0; e < 16; e += 2) p[e >> 3][(e & 7) >> 1] = pair(weight(sc, e), weight(sc, e + 1));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(vop[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
                 }
@@ -788,14 +935,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             // All keys for 32 rows a wavefront, in steps of 32.  While the vector units find the weights of a step's keys, the matrix
             // cores compute the scores of the next step's and the product of the step before with V, neither of which waits for these
             // weights: 16 matrix instructions, a slot each; operands are read kAhead slots before their use.  (With the product of the
-            // same step in the second half of the slots the weights had to be found in the first ones: 1721 us at 4096 tokens behind 126976.)
+            // same step in the second half of the slots the weights had to be found in the first ones: 1755 us at 4096 tokens behind 126976.)
             constexpr int kAhead = 2;
             f32x16 sa, sb;
             u32x4 pa[2], pb[2];
             float mx;
-            auto step = [&](auto half_tag, auto first_tag, const f32x16& cur, f32x16& nxt, const u32x4 (&before)[2], u32x4 (&p)[2], lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
+            auto step = [&](auto half_tag, const f32x16& cur, f32x16& nxt, const u32x4 (&before)[2], u32x4 (&p)[2], lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
                 constexpr int H = decltype(half_tag)::value;  // nxt: the block's second half, or the next block's first
-                constexpr bool FIRST = decltype(first_tag)::value;  // nothing before
                 float by = 1.f;
                 const bool grew = __any(mx > row.m + kSlack);
                 if (grew) by = row.move(mx);
@@ -803,16 +949,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
                 auto read = [&](auto oc) __attribute__((always_inline)) {
                     constexpr int o = decltype(oc)::value;
                     if constexpr (o < 8) op[o] = k_operand(ka, o, 1 - H);
-                    else if constexpr (o < 16 && !FIRST) op[o] = v_operand(va, o & 3, 2 * (1 - H) + ((o - 8) >> 2));
+                    else if constexpr (o < 16) op[o] = v_operand(va, o & 3, 2 * (1 - H) + ((o - 8) >> 2));
                 };
                 static_for<0, kAhead>([&](auto oc) { read(oc); });
                 FENCE();
                 static_for<0, 16>([&](auto sc_) __attribute__((always_inline)) {
                     constexpr int slot = decltype(sc_)::value;
                     if constexpr (slot < 8) nxt = mfma32(op[slot], qreg[slot], slot == 0 ? zero16 : nxt);
-                    else if constexpr (!FIRST) row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, before[(slot - 8) >> 2]), row.o[slot & 3]);
+                    else row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, before[(slot - 8) >> 2]), row.o[slot & 3]);
                     read(std::integral_constant<int, slot + kAhead>{});
-                    if constexpr (slot % 2 == 0) p[slot >> 3][(slot >> 1) & 3] = weigh(cur, slot);
+                    if constexpr (slot % 2 == 0) p[slot >> 3][(slot >> 1) & 3] = pair(weight(cur, slot), weight(cur, slot + 1));
                     if constexpr (slot == 13) {
                         if (masked_next) mask(nxt, k0_next);
                         mx = largest(nxt) * c2;
@@ -830,14 +976,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
             }
             if (masked(jb0)) mask(sa, jb0 * kKeys);
             mx = largest(sa) * c2;
+            // before the first step: weights of zero for keys of the piece
             lds_cptr va = v_block(vb);
+            pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};
             for (int j = 0; j < blocks; ++j) {
-                begin(j);
                 const int jb = jb0 + j;
-                if (j == 0) step(H0{}, std::true_type{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
-                else step(H0{}, std::false_type{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
+                begin(j);
+                step(H0{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
                 va = v_block(vb);
-                step(H1{}, std::false_type{}, sb, sa, pa, pb, k_block(next_k()), va, (jb + 1) * kKeys, masked(jb + 1));
+                step(H1{}, sb, sa, pa, pb, k_block(next_k()), va, (jb + 1) * kKeys, masked(jb + 1));
                 end(j);
             }
 #pragma unroll
@@ -847,8 +994,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         // ---- out
         row.l += __shfl_xor(row.l, 32);
         if (halves) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
-            f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & 3) * (17 * 64) + lane;
-            if (wave_on && wave >= 4) {
+            f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & (kWaves / 2 - 1)) * (17 * 64) + lane;
+            if (wave_on && wave >= kWaves / 2) {
                 there[0] = f32x4{row.m, row.l, 0.f, 0.f};
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
@@ -856,13 +1003,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
                     for (int e = 0; e < 16; e += 4) there[(1 + d * 4 + e / 4) * 64] = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
             }
             __syncthreads();
-            if (wave_on && wave < 4) {
+            if (wave_on && wave < kWaves / 2) {
                 const f32x4 ml = there[0];
-                const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew);
-                const float mine = fast_exp2(row.m - mnew);
-                row.scale(mine);
+                const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew), own = fast_exp2(row.m - mnew);
+                row.scale(own);
                 row.m = mnew;
-                row.l = fmaf(ml[1], by, row.l * mine);
+                row.l = fmaf(ml[1], by, row.l * own);
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -873,30 +1019,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
                     }
             }
         }
-        if (valid && (!halves || wave < 4)) {
-            const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
-            if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
-                const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
+        if (!valid || (halves && wave >= kWaves / 2)) return;
+        const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
+        if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
+            const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
-                        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                        store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
-                    }
-            } else {
-                float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                                   : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-                if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
+                    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                    store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
+                }
+        } else {
+            float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
+                               : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+            if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
-            }
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
         }
-    }
+    });
 }
 
 // Thirty-two lanes per row, four channels each.
@@ -920,6 +1065,7 @@ struct Pieces {
     __device__ __forceinline__ Pieces(const Place& p, const Head& head) : segments(0), first_segment(0), of(0) {
         first = plan::first_of(p, head.per), last = plan::last_of(p, head.per), line = head.segments;
     }
+    Pieces() = default;
     __device__ __forceinline__ bool whole() const { return first >= last; }
     // every `step`-th of them from the `from`-th on; row_parts: where the line's sums are if it is whole
     __device__ __forceinline__ void join(const ExtendArgs& a, Sums& sums, int r, const float* row_parts, int c4, int from, int step) const {
@@ -945,39 +1091,58 @@ struct Pieces {
 __device__ __forceinline__ const float* row_part(const ExtendArgs& a, int kind, int token, int head) {
     return a.parts[kind] + ((size_t)token * a.gm.Hq + head) * kPart;
 }
-// Rows of tiles of many: 32 rows of a tile per workgroup, eight at a time.  Rows of whole tiles that have no keys before their window were
-// written by the kernel before.
+// Rows of tiles of many, 32 of a tile per workgroup: a thread per row finds out whether something is left to do (rows of whole tiles that have no
+// keys before their window were written by the kernel before) and where its sums lie, then 32 lanes take a row each of those.
 constexpr int kCombineRows = 32;
 __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) {
+    struct Row {
+        int token, head, r, routed, prefix_row;  // r: in the tile; prefix_row: in its tile of keys before the window, -1: it has none
+        Pieces prefix;
+    };
+    __shared__ Row rows[kCombineRows];
+    __shared__ int count;
     const Geom& gm = a.gm;
     const Head head_ = uniform(a.head);
     if ((int)blockIdx.x >= head_.tiles) return;
     const Tile t = uniform(a.tiles + blockIdx.x);
     const int c4 = (threadIdx.x & 31) * 4, G = gm.G, r0 = blockIdx.y * kCombineRows;
     if (r0 >= t.rows || (a.do_local && t.kind != plan::kWindow)) return;
-    const Pieces own(Place{t.start, t.blocks}, head_);
-    const Pair pair = uniform(a.pairs + t.b * gm.Hkv + t.hk);
-    const int first_prefix = pair.first_tile + window_tiles(a, t.s), prefix_tiles = (pair.listed + a.tile_rows - 1) / a.tile_rows;
+    const Pieces own(place_of(a, t), head_);
+    if (threadIdx.x < kCombineRows) {
+        const Pair pair = uniform(a.pairs + t.b * gm.Hkv + t.hk);
+        const int first_prefix = pair.first_tile + window_tiles(a, t.s), many = plan::many_tiles(pair.listed, a.tile_rows), r = r0 + (int)threadIdx.x;
+        Row row{};
+        bool todo = false;
+        if (r < t.rows) {
+            const int code = row_code(a, t, t.first + r), tok = code / G;
+            row.r = r, row.head = t.hk * G + code - tok * G, row.token = t.s.start + tok, row.prefix_row = -1;
+            row.routed = token_routed(a, row.token, row.head);
+            const bool prefix = row.routed && t.s.pos + tok > gm.W;
+            todo = !(a.do_local && own.whole() && !prefix);
+            if (prefix) {
+                const int i = plan::clamp(list_of(a, a.rank, t.s, t.hk)[code], 0, max(pair.listed - 1, 0)), j = i / a.tile_rows;
+                row.prefix_row = i - j * a.tile_rows;
+                row.prefix = Pieces(place_of(a, a.tiles[min(first_prefix + j, head_.tiles - 1)]), head_);
+                row.prefix.segments = j < many ? pair.segments : 0, row.prefix.first_segment = pair.first_segment + j, row.prefix.of = many;
+            }
+        }
+        const unsigned long long set = __ballot(todo);
+        if (todo) rows[__popcll(set & ((1ull << threadIdx.x) - 1ull))] = row;
+        if (threadIdx.x == 0) count = __popcll(set);
+    }
+    __syncthreads();
     const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-    for (int r = r0 + (threadIdx.x >> 5); r < min(r0 + kCombineRows, t.rows); r += kThreads / 32) {
-        const int code = row_code(a, t, t.first + r), tok = code / G, head = t.hk * G + code - tok * G, token = t.s.start + tok;
-        const bool routed = token_routed(a, token, head), prefix = routed && t.s.pos + tok > gm.W;
-        if (a.do_local && own.whole() && !prefix) continue;
+    for (int i = threadIdx.x >> 5; i < count; i += kThreads / 32) {
+        const Row row = rows[i];
         Sums sums;
         f32x4 x = z;
         float lse_l = -INFINITY;
         if (a.do_local) {
-            own.join(a, sums, r, row_part(a, plan::kWindow, token, head), c4, 0, 1);
+            own.join(a, sums, row.r, row_part(a, plan::kWindow, row.token, row.head), c4, 0, 1);
             x = sums.value(), lse_l = sums.lse();
         }
-        if (prefix) {
-            const int i = plan::clamp(list_of(a, a.rank, t.s, t.hk)[code], 0, max(pair.listed - 1, 0)), j = i / a.tile_rows;
-            const Tile& pt = a.tiles[min(first_prefix + j, head_.tiles - 1)];
-            Pieces p(Place{pt.start, pt.blocks}, head_);
-            p.segments = pair.segments, p.first_segment = pair.first_segment + j, p.of = prefix_tiles;
-            p.join(a, sums, i - j * a.tile_rows, row_part(a, plan::kPrefix, token, head), c4, 0, 1);
-        }
-        store_row(a, token, head, c4, x, routed ? sums.value() : z, lse_l, routed ? sums.lse() : -INFINITY);
+        if (row.prefix_row >= 0) row.prefix.join(a, sums, row.prefix_row, row_part(a, plan::kPrefix, row.token, row.head), c4, 0, 1);
+        store_row(a, row.token, row.head, c4, x, row.routed ? sums.value() : z, lse_l, row.routed ? sums.lse() : -INFINITY);
     }
 }
 // Rows of sequences of few: a workgroup per row, whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
@@ -999,8 +1164,7 @@ __global__ __launch_bounds__(32 * kSlices) void extend_combine_few_kernel(Extend
     Sums sums[2];  // of the window's keys, of those before it
     for (int kind = 0; kind < 2; ++kind) {
         if (!(kind == plan::kWindow ? a.do_local : prefix)) continue;
-        const Tile& t = a.tiles[first + (kind == plan::kWindow ? 0 : windows)];
-        const Pieces p(Place{t.start, t.blocks}, head_);
+        const Pieces p(place_of(a, a.tiles[first + (kind == plan::kWindow ? 0 : windows)]), head_);
         if (kind == plan::kWindow && p.whole() && !prefix) return;  // written already
         p.join(a, sums[kind], r, row_part(a, kind, token, head), c4, slice, kSlices);
     }
@@ -1084,15 +1248,20 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
         KernelTimer kt("extend_list", st);
         hipLaunchKernelGGL(extend_list_kernel, dim3(g.B * g.Hkv), dim3(kListThreads), 0, st, a);
     }
-    {
+    const bool self = a.few && g.B * g.Hkv <= kFewPairs;
+    if (!self) {
         KernelTimer kt("extend_plan", st);
-        if (a.few) hipLaunchKernelGGL(extend_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
-        else hipLaunchKernelGGL(extend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        hipLaunchKernelGGL(extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
     }
     {
         KernelTimer kt("extend", st);
-        if (c.fp8) hipLaunchKernelGGL(extend_kernel<true>, dim3(a.workgroups), dim3(64 * kWaves), 0, st, a);
-        else hipLaunchKernelGGL(extend_kernel<false>, dim3(a.workgroups), dim3(64 * kWaves), 0, st, a);
+        const dim3 grid(a.workgroups), threads(64 * (a.few ? kFewWaves : kWaves));
+        if (self && c.fp8) hipLaunchKernelGGL((extend_few_kernel<true, true>), grid, threads, 0, st, a);
+        else if (self) hipLaunchKernelGGL((extend_few_kernel<false, true>), grid, threads, 0, st, a);
+        else if (a.few && c.fp8) hipLaunchKernelGGL((extend_few_kernel<true, false>), grid, threads, 0, st, a);
+        else if (a.few) hipLaunchKernelGGL((extend_few_kernel<false, false>), grid, threads, 0, st, a);
+        else if (c.fp8) hipLaunchKernelGGL(extend_kernel<true>, grid, threads, 0, st, a);
+        else hipLaunchKernelGGL(extend_kernel<false>, grid, threads, 0, st, a);
     }
     {
         KernelTimer kt("extend_combine", st);

@@ -3,8 +3,9 @@
 //
 // Work is a list of tiles (rows of one KV head of a sequence that see about the same keys), each with its blocks of kKeys keys.
 // Laid end to end the tiles form one line; every workgroup takes an equal stretch of it, whatever tiles lie there, so that a
-// long tile is shared by many and short ones are taken many at a time.  A tile counts kStart more than its blocks, what
-// it costs to begin and end one.  Ends of stretches that lie closer than kLeast to an end of their tile move there.
+// long tile is shared by many and short ones are taken many at a time.  A block counts what it takes, `each` of its tile; a tile
+// counts kStart more blocks than it has, what it costs to begin and end one.  Ends of stretches that lie closer than kLeast blocks to
+// an end of their tile move there.
 #pragma once
 #include <stdint.h>
 
@@ -54,24 +55,34 @@ L2A_PLAN_FN int tile_blocks(const Range& k) { return k.hi < k.lo ? 0 : k.hi / kK
 // Rows of a sequence before the first one with keys before the window.
 L2A_PLAN_FN int rows_without_prefix(const Seq& s, int G, int W) { return clamp(W + 1 - s.pos, 0, s.n) * G; }
 
-// Tiles of keys before the window all begin at key 0.  Where they are longer than a stretch (`per` blocks, at least kSegmentLeast), segments of its
-// length are cut off their beginnings, as many for each tile of a KV head as its first and shortest has, so that a block remains; each is
-// the work of one workgroup.  The same segments of all tiles lie side by side, for workgroups on one XCD, which then read the same keys at the same
-// time.  What remains of the tiles is the line, for the workgroups that remain: there are some, since every segment has a stretch's length.
-constexpr int kSegmentLeast = 16;
-L2A_PLAN_FN int segments(int blocks, int per) { return blocks > 0 ? (blocks - 1) / per : 0; }
+// What a block takes, in units of about half a microsecond: tiles of few rows wait for their loads (e4m3 half as long), those of many for the
+// matrix cores.
+constexpr int kFewRows = 32, kManyRows = 128;
+L2A_PLAN_FN int block_cost(int rows, bool fp8) { return (rows <= kFewRows ? 1 : rows <= kManyRows ? 2 : 3) + (fp8 ? 0 : 1); }
+
+// Tiles of keys before the window all begin at key 0.  Where those of many rows are longer than a stretch, segments of its length are cut off their
+// beginnings, as many for each such tile of a KV head as its first and shortest has, so that a block remains; each is the work of one
+// workgroup.  The same segments of all tiles lie side by side, for workgroups on one XCD, which then read the same keys at the same time.
+// What remains of the tiles is the line, for the workgroups that remain: there are some, since every segment has a stretch's length.
+constexpr int kSegmentLeast = 16;  // blocks
+L2A_PLAN_FN int segments(int blocks, int segment) { return blocks > 0 && segment >= kSegmentLeast ? (blocks - 1) / segment : 0; }
+L2A_PLAN_FN int many_tiles(int rows, int tile_rows) { return rows / tile_rows + (rows % tile_rows > kManyRows ? 1 : 0); }
 
 // A tile's place in the line.
 struct Place {
     long long start;
-    int blocks;
-    L2A_PLAN_FN int length() const { return blocks + kStart; }
+    int blocks, each;
+    L2A_PLAN_FN int steps() const { return blocks + kStart; }
+    L2A_PLAN_FN long long end() const { return start + (long long)steps() * each; }
 };
-// The stretch of workgroup w: [w per, (w + 1) per).
-L2A_PLAN_FN int stretch(long long total, int workgroups) { return (int)((total + workgroups - 1) / workgroups); }
-// The stretch's end x, in the tile it lies in, moved: how far from the tile's beginning.
+// The stretch of workgroup w: [w per, (w + 1) per).  No shorter than the dearest block, so that no two ends of stretches fall on the same block.
+L2A_PLAN_FN int stretch(long long total, int workgroups, int dearest) {
+    const int per = (int)((total + workgroups - 1) / workgroups);
+    return per > dearest ? per : dearest;
+}
+// The stretch's end x, in the tile it lies in, moved: how many steps from the tile's beginning.
 L2A_PLAN_FN int moved(const Place& t, long long x) {
-    const int at = (int)(x - t.start), len = t.length();
+    const int at = (int)(x - t.start) / t.each, len = t.steps();
     if (at < kLeast) return 0;
     return len - at < kLeast ? len : at;
 }
@@ -81,10 +92,10 @@ struct Piece {
     int first, last;  // whether it holds the tile's first and last block
 };
 L2A_PLAN_FN Piece piece(const Place& t, int per, int w) {
-    const long long x0 = (long long)w * per, x1 = x0 + per, end = t.start + t.length();
-    const int a = x0 <= t.start ? 0 : moved(t, x0), b = x1 >= end ? t.length() : moved(t, x1);
+    const long long x0 = (long long)w * per, x1 = x0 + per;
+    const int a = x0 <= t.start ? 0 : moved(t, x0), b = x1 >= t.end() ? t.steps() : moved(t, x1);
     Piece p;
-    p.first = a == 0, p.last = b == t.length();
+    p.first = a == 0, p.last = b == t.steps();
     p.from = a > kStart ? a - kStart : 0;
     p.to = b > kStart ? b - kStart : 0;
     if (a >= b) p.from = p.to = 0;
@@ -93,12 +104,12 @@ L2A_PLAN_FN Piece piece(const Place& t, int per, int w) {
 // The workgroups that have pieces of a tile, from first_of to last_of: ends of stretches before `begun` move to its beginning or
 // lie before it, those from `ended` on to its end or lie behind it.
 L2A_PLAN_FN int first_of(const Place& t, int per) {
-    const long long begun = t.start + (t.length() < kLeast ? t.length() : kLeast);
+    const long long begun = t.start + (long long)(t.steps() < kLeast ? t.steps() : kLeast) * t.each;
     return (int)((begun - 1) / per);
 }
 L2A_PLAN_FN int last_of(const Place& t, int per) {
-    const long long end = t.start + t.length(), a = t.start + kLeast, b = end - kLeast + 1, c = a > b ? a : b, ended = c < end ? c : end;
-    return (int)((ended - 1) / per);
+    const int n = t.steps(), b = n - kLeast + 1, c = kLeast > b ? kLeast : b, ended = c < n ? c : n;
+    return (int)((t.start + (long long)ended * t.each - 1) / per);
 }
 // Where a piece that is not the whole tile leaves its sums: every workgroup has a place for a tile that it does not begin and
 // one for a tile that it does not end.

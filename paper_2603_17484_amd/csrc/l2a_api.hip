@@ -105,7 +105,7 @@ int check_cache(const l2a_params* p, const l2a_cache* c) {
     if (c->dtype != L2A_BF16 && c->dtype != L2A_FP8) return L2A_ERR_UNSUPPORTED;
     if (c->dtype == L2A_FP8 && (!c->k_scale || !c->v_scale)) return L2A_ERR_NULL;
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return L2A_ERR_SHAPE;
-    if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 26)) return L2A_ERR_SHAPE;
+    if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 25)) return L2A_ERR_SHAPE;
     if (misaligned(c->k) || misaligned(c->v) || (c->dtype == L2A_FP8 && (misaligned(c->k_scale) || misaligned(c->v_scale)))) return L2A_ERR_ALIGN;
     if (misaligned4(c->table)) return L2A_ERR_ALIGN;
     return L2A_OK;

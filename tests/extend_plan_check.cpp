@@ -7,20 +7,22 @@
 
 using namespace l2a::plan;
 
-extern "C" int plan_check(const int* blocks, int tiles, int workgroups, char* msg, int n) {
+extern "C" int plan_check(const int* blocks, const int* each, int tiles, int workgroups, char* msg, int n) {
     std::vector<Place> at;
     long long total = 0;
     for (int i = 0; i < tiles; ++i) {
-        at.push_back(Place{total, blocks[i]});
-        total += at.back().length();
+        at.push_back(Place{total, blocks[i], each[i]});
+        total = at.back().end();
     }
-    const int per = stretch(total, workgroups);
+    int dearest = 1;
+    for (int i = 0; i < tiles; ++i) dearest = each[i] > dearest ? each[i] : dearest;
+    const int per = stretch(total, workgroups, dearest);
     std::vector<int> done(tiles, 0), first(tiles, -1), last(tiles, -1);
     std::vector<int> used(2 * workgroups, 0);
     int T = 0;
     for (int w = 0; w < workgroups; ++w) {
         if ((long long)w * per >= total) break;
-        while (at[T].start + at[T].length() <= (long long)w * per) ++T;  // the tile the stretch begins in
+        while (at[T].end() <= (long long)w * per) ++T;  // the tile the stretch begins in
         for (int t = T; t < tiles && at[t].start < (long long)(w + 1) * per; ++t) {
             const Piece p = piece(at[t], per, w);
             if (p.from == p.to) continue;
@@ -28,6 +30,7 @@ extern "C" int plan_check(const int* blocks, int tiles, int workgroups, char* ms
             if (p.to <= p.from || p.to > blocks[t]) return snprintf(msg, n, "tile %d: piece %d..%d", t, p.from, p.to), 1;
             if ((p.from == 0) != (p.first != 0) || (p.to == blocks[t]) != (p.last != 0)) return snprintf(msg, n, "tile %d: flags of %d..%d", t, p.from, p.to), 1;
             if (first[t] < 0) first[t] = w;
+            else if (last[t] != w - 1) return snprintf(msg, n, "tile %d: nothing from workgroup %d", t, w - 1), 1;
             last[t] = w;
             done[t] = p.to;
             if (!(p.first && p.last) && used[slot(w, p.first)]++) return snprintf(msg, n, "slot of workgroup %d used twice", w), 1;

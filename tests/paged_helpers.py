@@ -170,7 +170,8 @@ def reference(s, k, v, flags=0, scale=None):
 
 
 def near(name, got, want, tol):
-    bad = ~((np.abs(got - want) <= tol) | (got == want))  # (equal infinities)
+    with np.errstate(invalid="ignore"):
+        bad = ~((np.abs(got - want) <= tol) | (got == want))  # (equal infinities)
     assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} off, first at {np.argwhere(bad)[0]}: {got[bad][0]} for {want[bad][0]}, tolerance {tol[bad][0]}"
 
 

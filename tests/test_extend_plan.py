@@ -20,10 +20,12 @@ def chk():
     return ctypes.CDLL(LIB)
 
 
-def check(chk, blocks, workgroups):
+def check(chk, blocks, workgroups, each=None):
+    each = each or [1] * len(blocks)
     msg = ctypes.create_string_buffer(256)
-    rc = chk.plan_check((ctypes.c_int * len(blocks))(*blocks), len(blocks), workgroups, msg, 256)
-    assert rc == 0, f"{msg.value.decode()}: {workgroups} workgroups, {blocks[:20]}"
+    ints = ctypes.c_int * len(blocks)
+    rc = chk.plan_check(ints(*blocks), ints(*each), len(blocks), workgroups, msg, 256)
+    assert rc == 0, f"{msg.value.decode()}: {workgroups} workgroups, {blocks[:20]} {each[:20]}"
 
 
 @pytest.mark.parametrize("workgroups", [1, 2, 7, 256, 512])
@@ -34,7 +36,9 @@ def test_every_block_once(chk, workgroups):
     check(chk, [1] * 2000, workgroups)
     for _ in range(400):
         most = rng.choice([1, 3, 5, 9, 70, 2000])
-        check(chk, [rng.randint(1, most) for _ in range(rng.choice([1, 2, 5, 40, 700]))], workgroups)
+        blocks = [rng.randint(1, most) for _ in range(rng.choice([1, 2, 5, 40, 700]))]
+        check(chk, blocks, workgroups)
+        check(chk, blocks, workgroups, [rng.choice([1, 2, 3]) for _ in blocks])
 
 
 def test_every_short_line(chk):
@@ -44,6 +48,7 @@ def test_every_short_line(chk):
             for c in range(1, 9):
                 for w in (2, 3, 4, 6, 9):
                     check(chk, [a, b, c], w)
+                    check(chk, [a, b, c], w, [1, 3, 2])
 
 
 def test_sequences_out_of_range_are_clamped(chk):

@@ -6,7 +6,7 @@ import torch
 
 from paper_2603_17484_amd import binding as B
 from paper_2603_17484_amd.runner import GuardedAllocator, to_host
-from tests.paged_helpers import D, E4M3, SENTINEL, Step, bits, cache_on_gpu, check_extend, dequantise, quantise, up
+from tests.paged_helpers import D, E4M3, HALF, SENTINEL, SMALL, WEIGHT, Step, bits, cache_on_gpu, check_extend, dequantise, near, quantise, up
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +182,71 @@ def test_flags(flags, fp8):
 def test_only_the_output_is_wanted_and_a_scale_of_its_own():
     check_extend(Step([40, 1], [100, 300], 8, 2, 50, seed=1), optional=False)
     check_extend(Step([40, 1], [100, 300], 8, 2, 50, seed=2), scale=0.3)
+
+
+def on_the_gpu(q, k, v, lo, hi, scale):
+    """q [rows, 128], k, v [keys, 128] in 64 bits; row i sees keys lo[i] .. hi[i].  -> mean, a bound for E|v - mean| (the deviation, which is
+    no less), E|v|, log-sum-exp."""
+    key = torch.arange(len(k), device="cuda")
+    out = []
+    for i in range(0, len(q), 512):
+        sc = (q[i:i + 512] @ k.t()) * scale
+        sc = sc.masked_fill((key < lo[i:i + 512, None]) | (key > hi[i:i + 512, None]), -torch.inf)
+        p = torch.softmax(sc, -1)
+        mean = p @ v
+        out.append((mean, ((p @ v.square()) - mean.square()).clamp(min=0).sqrt(), p @ v.abs(), torch.logsumexp(sc, -1)))
+    return [torch.cat(x) for x in zip(*out)]
+
+
+# lengths at which tiles are longer than a workgroup's share: segments of many tiles, the rest of them on the line; a chunk of one tile
+# cut among many; beside them single tokens, a draft, a tile of up to 128 rows
+@pytest.mark.parametrize("new,cached,Hq,Hkv,W,f,fp8,page", [
+    ([300], [40000], 8, 1, 100, 1.0, False, 64), ([300], [40000], 8, 1, 100, 1.0, True, 16), ([1, 400, 12, 1, 30], [9000, 30000, 20000, 50000, 10], 8, 1, 3000, 0.9, False, 128),
+    ([1, 400, 12, 1, 30], [9000, 30000, 20000, 50000, 10], 8, 1, 3000, 0.9, True, 32), ([20], [60000], 8, 2, 700, 0.5, False, 256), ([1, 1], [70000, 123], 16, 2, 4096, 1.0, True, 64)])
+def test_long_caches(new, cached, Hq, Hkv, W, f, fp8, page):
+    g = torch.Generator(device="cuda").manual_seed(sum(cached))
+    n, G = sum(new), Hq // Hkv
+    held = [-(-(a + b) // page) for a, b in zip(new, cached)]
+    p = B.make_params(len(new), n, Hq, Hkv, D, W)
+    c = B.alloc_cache(p, sum(held), page, max(held), fp8)
+    order = torch.randperm(sum(held), generator=g, device="cuda", dtype=torch.int32)
+    values = []
+    for pool, scale in ((c.tensors[0], c.tensors[2]), (c.tensors[1], c.tensors[3])):
+        x = torch.randn(pool.shape, generator=g, device="cuda")
+        pool.copy_(x)
+        if fp8:
+            scale.copy_(torch.randint(124, 130, scale.shape, generator=g, device="cuda"))
+            values.append((pool.double().unflatten(-1, (4, 32)) * torch.exp2(scale.double() - 127).unsqueeze(-1)).flatten(-2))
+        else:
+            values.append(pool.double())
+    at = 0
+    for b, m in enumerate(held):
+        c.tensors[4][b, :m] = order[at:at + m]
+        at += m
+    q = torch.randn(n, Hq, D, generator=g, device="cuda").bfloat16()
+    mask = (torch.rand(1, n, generator=g, device="cuda") < f).to(torch.uint8)
+    start = up(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+    O, S, A = (torch.empty_like(q) for _ in range(3))
+    ll, lg = (torch.empty(Hq, n, device="cuda") for _ in range(2))
+    B.l2a_attn_extend(p, c, q, start, up(np.array(cached, np.int32)), mask, max(new), O, ll, lg, S, A)
+    row = 0
+    for b, (m, before) in enumerate(zip(new, cached)):
+        pages = c.tensors[4][b, :held[b]].long()
+        pos = before + torch.arange(m, device="cuda")
+        routed = mask[0, row:row + m] != 0
+        for hk in range(Hkv):
+            k, v = (x[pages, hk].flatten(0, 1)[:before + m] for x in values)
+            rows = slice(hk * G, hk * G + G)
+            qs = q[row:row + m, rows].double().flatten(0, 1)
+            hi, lo = pos.repeat_interleave(G), (pos - W).clamp(min=0).repeat_interleave(G)
+            on = routed.repeat_interleave(G)
+            s, ds, es, l = on_the_gpu(qs, k, v, lo, hi, D ** -0.5)
+            a, da, ea, la = on_the_gpu(qs, k, v, torch.zeros_like(hi), hi, D ** -0.5)
+            a, da, ea, la = a * on[:, None], da * on[:, None], ea * on[:, None], la.masked_fill(~on, -torch.inf)
+            ts, ta = WEIGHT * ds + SMALL * es, WEIGHT * da + SMALL * ea
+            for name, got, want, tol in (("S", S, s, ts), ("A", A, a, ta), ("O", O, s + a, ts + ta)):
+                near(name, to_host(got[row:row + m, rows].flatten(0, 1)), want.cpu().numpy(), (tol + HALF * (want.abs() + tol)).cpu().numpy())
+            for name, got, want in (("lse_local", ll, l), ("lse_global", lg, la)):
+                want = want.cpu().numpy()
+                near(name, to_host(got[rows, row:row + m].t().flatten()), want, np.full(want.shape, WEIGHT + SMALL) + 2.0 ** -22 * np.where(np.isfinite(want), np.abs(want), 0))
+        row += m
