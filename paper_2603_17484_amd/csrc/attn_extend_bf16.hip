@@ -60,7 +60,7 @@ struct ExtendArgs {
     // workspace
     Head* head;
     Tile* tiles;
-    int most_tiles, workgroups, tile_rows, few;  // few: no sequence has more than 32 rows per KV head, and no lists are made
+    int most_tiles, workgroups, tile_rows, few;  // few: no sequence has more than 128 rows per KV head, and no lists are made
     int32_t* first_tile;  // [workgroups] of a stretch
     Segment* segment;     // [workgroups]
     Pair* pairs;          // [B * Hkv]
@@ -96,6 +96,7 @@ __device__ __forceinline__ unsigned group_routed(const ExtendArgs& a, int token,
 // Whether a row of a KV head is routed and has keys before its window.
 __device__ __forceinline__ bool has_prefix(const ExtendArgs& a, const Seq& s, int hk) {
     unsigned any = 0;
+#pragma unroll 4
     for (int t = plan::rows_without_prefix(s, 1, a.gm.W); t < s.n; ++t) any |= group_routed(a, s.start + t, hk);
     return any != 0;
 }
@@ -730,22 +731,276 @@ __device__ __forceinline__ void for_pieces(const ExtendArgs& a, F&& f) {
 // Shared memory is written and read by address: all of it there is begins at 0.
 __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory"); }
 
-// Calls whose sequences all have few rows.  SELF: every workgroup makes the plan for itself, a thread per KV head of a sequence (at most as
-// many as threads), and the first one leaves it for the last kernel: a launch less.
-constexpr int kFewWaves = 8, kFewPairs = 64 * kFewWaves;
-struct FewPlan {
-    int start[2 * kFewPairs], of[2 * kFewPairs];  // of a tile: its place in the line; twice its pair, plus its kind
-    Seq seq[kFewPairs];
-    int sums[kFewWaves], first;
-};
-template <bool FP8, bool SELF>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void extend_few_kernel(ExtendArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[FewLds<kFewWaves>::used + (SELF ? sizeof(FewPlan) : 0)];
-    by_address(lds);
-    if constexpr (!SELF) {
-        for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) { few_rows<FP8, kFewWaves>(a, lds, t, piece, w); });
+// A tile by 8 wavefronts of 32 rows, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself and every operand
+// serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one box, at 2.1 GHz and
+// 1.9.  It is the power that bounds both.)
+// HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
+constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
+static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
+template <bool FP8, bool HALVES>
+__device__ __forceinline__ void some_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
+    typedef Lds<FP8, kWaves> L;
+    const Geom& gm = a.gm;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, h = lane >> 5, G = gm.G;
+    const float c2 = gm.scale_log2;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+
+    const int hk = t.hk, jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
+    const Seq s = t.s;
+    __syncthreads();  // LDS is free
+    Loader<FP8, kWaves> load{a, (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
+    load.start();
+    load.issue();
+    load.issue();
+
+    // ---- this lane's row (rows past the end repeat the last one: computed, never written)
+    const int r = (HALVES ? wave & (kWaves / 2 - 1) : wave) * 32 + n;
+    const bool valid = r < t.rows, wave_on = r - n < t.rows;
+    const int code = row_code(a, t, t.first + min(r, t.rows - 1)), tok = code / G, token = s.start + tok, head = hk * G + code - tok * G, pos = s.pos + tok;
+    const Range keys = plan::row_keys(t.kind, pos, gm.W);
+    bf16x8 qreg[8];
+    const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
+    // blocks that every row of the tile sees whole: from `whole0` to `whole1` - 1
+    const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
+    const int whole0 = (lo_max + kKeys - 1) / kKeys, whole1 = (hi_min + 1) / kKeys;
+    auto masked = [&](int jb) __attribute__((always_inline)) { return jb < whole0 || jb >= whole1; };
+    // scores of 32 keys from k0 on, those out of the row's reach taken out
+    auto mask = [&](f32x16& sc, int k0) __attribute__((always_inline)) {
+        const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
+    };
+
+    RowSums row;
+    row.clear();
+    unsigned kb = L::k, vb = L::v;  // block j
+    auto next_k = [&]() __attribute__((always_inline)) { return next(kb, L::k, kBlockBytes, L::kK); };
+    auto next_v = [&]() __attribute__((always_inline)) { return next(vb, L::v, kBlockBytes, L::kV); };
+    if constexpr (FP8) {
+        load.wait();
+        load.convert(L::raw_k, L::raw_ks, 0, L::k);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load.issue();
+        load.wait();
+        if (blocks > 1) load.convert(L::raw_k, L::raw_ks, 1, L::k + kBlockBytes);
+        load.convert(L::raw_v, L::raw_vs, 0, L::v);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load.issue();
     } else {
-        FewPlan& plan_ = *reinterpret_cast<FewPlan*>(lds + FewLds<kFewWaves>::used);
+        load.issue();
+        load.wait();
+    }
+    __syncthreads();
+    // begins a block's work: more on its way, and e4m3 of the next group made bf16
+    auto begin = [&](int j) __attribute__((always_inline)) {
+        if constexpr (FP8) {
+            if (j + 1 < blocks) {
+                load.wait();
+                if (j + 2 < blocks) load.convert(L::raw_k, L::raw_ks, j & 1, next(next_k(), L::k, kBlockBytes, L::kK));
+                load.convert(L::raw_v, L::raw_vs, (j + 1) & 1, next_v());
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+        }
+        load.issue();
+    };
+    auto end = [&](int j) __attribute__((always_inline)) {
+        if constexpr (!FP8) load.wait();
+        __syncthreads();
+        kb = next_k(), vb = next_v();
+    };
+    const unsigned k_mine = k_lane(lane), v_mine = v_lane(lane);
+    auto k_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + k_mine); };
+    auto v_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + v_mine); };
+    // Weights of a pair of scores, rounded to bf16; the sum is that of the weights as the matrix cores see them, so that what
+    // they are divided by is exact for them.
+    auto weight = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return fast_exp2(fmaf(sc[e], c2, -row.m)); };
+    auto pair = [&](float x, float y) __attribute__((always_inline)) {
+        f32x2 f = {x, y};
+        const bf16x2 pb = __builtin_convertvector(f, bf16x2);
+        row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
+        return __builtin_bit_cast(uint32_t, pb);
+    };
+    if constexpr (HALVES) {
+        // One half of 32 keys per wavefront and block, all operands read ahead; short of rows, the loads set the pace.
+        const int half = wave / (kWaves / 2);
+        for (int j = 0; j < blocks; ++j) {
+            begin(j);
+            if (wave_on) {
+                const lds_cptr ka = k_block(kb) + half * 8 * kFour, va = v_block(vb) + half * 8 * kFour;
+                bf16x8 kop[8], vop[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) kop[i] = k_operand(ka, i, 0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) vop[i] = v_operand(va, i & 3, i >> 2);
+                FENCE();
+                f32x16 sc;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) sc = mfma32(kop[ks], qreg[ks], ks == 0 ? zero16 : sc);
+                if (masked(jb0 + j)) mask(sc, (jb0 + j) * kKeys + half * 32);
+                row.look(largest(sc) * c2);
+                u32x4 p[2];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) p[e >> 3][(e & 7) >> 1] = pair(weight(sc, e), weight(sc, e + 1));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(vop[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
+            }
+            end(j);
+        }
+    } else {
+        // All keys for 32 rows a wavefront, in steps of 32.  While the vector units find the weights of a step's keys, the matrix
+        // cores compute the scores of the next step's and the product of the step before with V, neither of which waits for these
+        // weights: 16 matrix instructions, a slot each; operands are read kAhead slots before their use.  (With the product of the
+        // same step in the second half of the slots the weights had to be found in the first ones: 1755 us at 4096 tokens behind 126976.)
+        constexpr int kAhead = 2;
+        f32x16 sa, sb;
+        u32x4 pa[2], pb[2];
+        float mx;
+        auto step = [&](auto half_tag, const f32x16& cur, f32x16& nxt, const u32x4 (&before)[2], u32x4 (&p)[2], lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
+            constexpr int H = decltype(half_tag)::value;  // nxt: the block's second half, or the next block's first
+            float by = 1.f;
+            const bool grew = __any(mx > row.m + kSlack);
+            if (grew) by = row.move(mx);
+            bf16x8 op[16 + kAhead];
+            auto read = [&](auto oc) __attribute__((always_inline)) {
+                constexpr int o = decltype(oc)::value;
+                if constexpr (o < 8) op[o] = k_operand(ka, o, 1 - H);
+                else if constexpr (o < 16) op[o] = v_operand(va, o & 3, 2 * (1 - H) + ((o - 8) >> 2));
+            };
+            static_for<0, kAhead>([&](auto oc) { read(oc); });
+            FENCE();
+            static_for<0, 16>([&](auto sc_) __attribute__((always_inline)) {
+                constexpr int slot = decltype(sc_)::value;
+                if constexpr (slot < 8) nxt = mfma32(op[slot], qreg[slot], slot == 0 ? zero16 : nxt);
+                else row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, before[(slot - 8) >> 2]), row.o[slot & 3]);
+                read(std::integral_constant<int, slot + kAhead>{});
+                if constexpr (slot % 2 == 0) p[slot >> 3][(slot >> 1) & 3] = pair(weight(cur, slot), weight(cur, slot + 1));
+                if constexpr (slot == 13) {
+                    if (masked_next) mask(nxt, k0_next);
+                    mx = largest(nxt) * c2;
+                }
+                FENCE();
+            });
+            if (grew) row.scale(by);
+        };
+        typedef std::integral_constant<int, 0> H0;
+        typedef std::integral_constant<int, 1> H1;
+        {
+            const lds_cptr ka = k_block(kb);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) sa = mfma32(k_operand(ka, ks, 0), qreg[ks], ks == 0 ? zero16 : sa);
+        }
+        if (masked(jb0)) mask(sa, jb0 * kKeys);
+        mx = largest(sa) * c2;
+        // before the first step: weights of zero for keys of the piece
+        lds_cptr va = v_block(vb);
+        pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};
+        for (int j = 0; j < blocks; ++j) {
+            const int jb = jb0 + j;
+            begin(j);
+            step(H0{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
+            va = v_block(vb);
+            step(H1{}, sb, sa, pa, pb, k_block(next_k()), va, (jb + 1) * kKeys, masked(jb + 1));
+            end(j);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(v_operand(va, i & 3, 2 + (i >> 2)), __builtin_bit_cast(bf16x8, pb[i >> 2]), row.o[i & 3]);
+    }
+
+    // ---- out
+    row.l += __shfl_xor(row.l, 32);
+    if constexpr (HALVES) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
+        f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & (kWaves / 2 - 1)) * (17 * 64) + lane;
+        if (wave_on && wave >= kWaves / 2) {
+            there[0] = f32x4{row.m, row.l, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) there[(1 + d * 4 + e / 4) * 64] = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
+        }
+        __syncthreads();
+        if (wave_on && wave < kWaves / 2) {
+            const f32x4 ml = there[0];
+            const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew), own = fast_exp2(row.m - mnew);
+            row.scale(own);
+            row.m = mnew;
+            row.l = fmaf(ml[1], by, row.l * own);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 x = there[(1 + d * 4 + e / 4) * 64];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) row.o[d][e + i] = fmaf(x[i], by, row.o[d][e + i]);
+                }
+        }
+    }
+    if (!valid || (HALVES && wave >= kWaves / 2)) return;
+    const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
+    if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
+        const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
+                const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
+            }
+    } else {
+        float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
+                           : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+        if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
+    }
+}
+
+template <bool FP8>
+struct TileLds {
+    static constexpr unsigned used = Lds<FP8, kWaves>::used > FewLds<kWaves>::used ? Lds<FP8, kWaves>::used : FewLds<kWaves>::used;
+};
+template <bool FP8>
+__global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[TileLds<FP8>::used];
+    by_address(lds);
+    for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
+        if (t.rows <= kSub) few_rows<FP8, kWaves>(a, lds, t, piece, w);
+        else if (t.rows <= kHalvesRows) some_rows<FP8, true>(a, lds, t, piece, w);
+        else some_rows<FP8, false>(a, lds, t, piece, w);
+    });
+}
+
+// Calls whose sequences all have up to 128 rows per KV head, a tile for each part of its keys; FEW: up to 32.  SELF: every workgroup makes the plan
+// for itself, a thread per KV head of a sequence (at most as many as threads), and the first one leaves it for the last kernel: a
+// launch less.
+constexpr int kShortPairs = 64 * kWaves;
+struct ShortPlan {
+    int start[2 * kShortPairs], of[2 * kShortPairs];  // of a tile: its place in the line; twice its pair, plus its kind
+    Seq seq[kShortPairs];
+    int sums[kWaves], first;
+};
+template <bool FP8, bool FEW, bool SELF>
+__global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs a) {
+    constexpr unsigned kLds = FEW ? FewLds<kWaves>::used : TileLds<FP8>::used;
+    __shared__ __attribute__((aligned(1024))) char lds[kLds + (SELF ? sizeof(ShortPlan) : 0)];
+    by_address(lds);
+    auto rows = [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
+        if (FEW || t.rows <= kSub) few_rows<FP8, kWaves>(a, lds, t, piece, w);
+        else some_rows<FP8, true>(a, lds, t, piece, w);
+    };
+    if constexpr (!SELF) {
+        for_pieces(a, rows);
+    } else {
+        ShortPlan& plan_ = *reinterpret_cast<ShortPlan*>(lds + kLds);
         const Geom& gm = a.gm;
         const int w = workgroup(a), mine = threadIdx.x, pairs = gm.B * gm.Hkv;
         Tile t[2];
@@ -766,10 +1021,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void extend_few_kernel(ExtendArg
                 steps[kind] = (int)place_of(a, t[kind]).end();
             }
         int T, tiles, at, total;
-        scan<64 * kFewWaves>(on[0] + on[1], plan_.sums, T, tiles);
-        scan<64 * kFewWaves>(steps[0] + steps[1], plan_.sums, at, total);
+        scan<64 * kWaves>(on[0] + on[1], plan_.sums, T, tiles);
+        scan<64 * kWaves>(steps[0] + steps[1], plan_.sums, at, total);
         total = same(total), tiles = same(tiles);
-        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(1, FP8))), x0 = w * per;
+        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, FP8))), x0 = w * per;
         const Pair pair{T, on[plan::kPrefix] ? s.n * gm.G : 0, 0, 0};
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
@@ -798,250 +1053,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void extend_few_kernel(ExtendArg
             Tile tile = make_tile(a, ts, tb, p - tb * gm.Hkv, of & 1, 0, ts.n * gm.G);
             tile.start = start, tile.pos0 = same(tile.pos0), tile.pos1 = same(tile.pos1), tile.lo = same(tile.lo), tile.hi = same(tile.hi), tile.blocks = same(tile.blocks);
             const plan::Piece piece = plan::piece(place_of(a, tile), per, w);
-            if (piece.from != piece.to) few_rows<FP8, kFewWaves>(a, lds, tile, piece, w);
+            if (piece.from != piece.to) rows(tile, piece, w);
         }
     }
-}
-
-// Tiles of up to 256 rows by 8 wavefronts of 32, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself,
-// every operand serving two matrix instructions: 1732 us at 4096 tokens behind 126976, 385 at 2048 behind 32768, now 1698 and 342.
-// A wavefront alone issues one instruction at a time, and its scalar ones and waits are then not beside anything.)
-constexpr int kWaves = 8;
-template <bool FP8>
-__global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
-    typedef Lds<FP8, kWaves> L;
-    __shared__ __attribute__((aligned(1024))) char lds[L::used > FewLds<kWaves>::used ? L::used : FewLds<kWaves>::used];
-        by_address(lds);
-    const Geom& gm = a.gm;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 31, h = lane >> 5, G = gm.G;
-    const float c2 = gm.scale_log2;
-    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
-
-    for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
-        if (t.rows <= 32) {
-            few_rows<FP8, kWaves>(a, lds, t, piece, w);
-            return;
-        }
-        const int hk = t.hk, jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
-        const Seq s = t.s;
-        __syncthreads();  // LDS is free
-        Loader<FP8, kWaves> load{a, (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
-        load.start();
-        load.issue();
-        load.issue();
-
-        // ---- this lane's row (rows past the end repeat the last one: computed, never written).  Up to 128 rows: wavefronts 4 .. 7 take
-        // the second half of the keys of every block for the rows of wavefronts 0 .. 3.
-        const bool halves = t.rows <= 32 * kWaves / 2;
-        const int r = (halves ? wave & (kWaves / 2 - 1) : wave) * 32 + n;
-        const bool valid = r < t.rows, wave_on = r - n < t.rows;
-        const int code = row_code(a, t, t.first + min(r, t.rows - 1)), tok = code / G, token = s.start + tok, head = hk * G + code - tok * G, pos = s.pos + tok;
-        const Range keys = plan::row_keys(t.kind, pos, gm.W);
-        bf16x8 qreg[8];
-        const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
-        // blocks that every row of the tile sees whole: from `whole0` to `whole1` - 1
-        const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
-        const int whole0 = (lo_max + kKeys - 1) / kKeys, whole1 = (hi_min + 1) / kKeys;
-        auto masked = [&](int jb) __attribute__((always_inline)) { return jb < whole0 || jb >= whole1; };
-        // scores of 32 keys from k0 on, those out of the row's reach taken out
-        auto mask = [&](f32x16& sc, int k0) __attribute__((always_inline)) {
-            const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
-        };
-
-        RowSums row;
-        row.clear();
-        unsigned kb = L::k, vb = L::v;  // block j
-        auto next_k = [&]() __attribute__((always_inline)) { return next(kb, L::k, kBlockBytes, L::kK); };
-        auto next_v = [&]() __attribute__((always_inline)) { return next(vb, L::v, kBlockBytes, L::kV); };
-        if constexpr (FP8) {
-            load.wait();
-            load.convert(L::raw_k, L::raw_ks, 0, L::k);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            load.issue();
-            load.wait();
-            if (blocks > 1) load.convert(L::raw_k, L::raw_ks, 1, L::k + kBlockBytes);
-            load.convert(L::raw_v, L::raw_vs, 0, L::v);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            load.issue();
-        } else {
-            load.issue();
-            load.wait();
-        }
-        __syncthreads();
-        // begins a block's work: more on its way, and e4m3 of the next group made bf16
-        auto begin = [&](int j) __attribute__((always_inline)) {
-            if constexpr (FP8) {
-                if (j + 1 < blocks) {
-                    load.wait();
-                    if (j + 2 < blocks) load.convert(L::raw_k, L::raw_ks, j & 1, next(next_k(), L::k, kBlockBytes, L::kK));
-                    load.convert(L::raw_v, L::raw_vs, (j + 1) & 1, next_v());
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                }
-            }
-            load.issue();
-        };
-        auto end = [&](int j) __attribute__((always_inline)) {
-            if constexpr (!FP8) load.wait();
-            __syncthreads();
-            kb = next_k(), vb = next_v();
-        };
-        const unsigned k_mine = k_lane(lane), v_mine = v_lane(lane);
-        auto k_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + k_mine); };
-        auto v_block = [&](unsigned at) __attribute__((always_inline)) { return (lds_cptr)(uintptr_t)(at + v_mine); };
-        // Weights of a pair of scores, rounded to bf16; the sum is that of the weights as the matrix cores see them, so that what
-        // they are divided by is exact for them.
-        auto weight = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return fast_exp2(fmaf(sc[e], c2, -row.m)); };
-        auto pair = [&](float x, float y) __attribute__((always_inline)) {
-            f32x2 f = {x, y};
-            const bf16x2 pb = __builtin_convertvector(f, bf16x2);
-            row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
-            return __builtin_bit_cast(uint32_t, pb);
-        };
-        if (halves) {
-            // One half of 32 keys per wavefront and block, all operands read ahead; short of rows, the loads set the pace.
-            const int half = wave / (kWaves / 2);
-            for (int j = 0; j < blocks; ++j) {
-                begin(j);
-                if (wave_on) {
-                    const lds_cptr ka = k_block(kb) + half * 8 * kFour, va = v_block(vb) + half * 8 * kFour;
-                    bf16x8 kop[8], vop[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) kop[i] = k_operand(ka, i, 0);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) vop[i] = v_operand(va, i & 3, i >> 2);
-                    FENCE();
-                    f32x16 sc;
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) sc = mfma32(kop[ks], qreg[ks], ks == 0 ? zero16 : sc);
-                    if (masked(jb0 + j)) mask(sc, (jb0 + j) * kKeys + half * 32);
-                    row.look(largest(sc) * c2);
-                    u32x4 p[2];
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) p[e >> 3][(e & 7) >> 1] = pair(weight(sc, e), weight(sc, e + 1));
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(vop[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
-                }
-                end(j);
-            }
-        } else {
-            // All keys for 32 rows a wavefront, in steps of 32.  While the vector units find the weights of a step's keys, the matrix
-            // cores compute the scores of the next step's and the product of the step before with V, neither of which waits for these
-            // weights: 16 matrix instructions, a slot each; operands are read kAhead slots before their use.  (With the product of the
-            // same step in the second half of the slots the weights had to be found in the first ones: 1755 us at 4096 tokens behind 126976.)
-            constexpr int kAhead = 2;
-            f32x16 sa, sb;
-            u32x4 pa[2], pb[2];
-            float mx;
-            auto step = [&](auto half_tag, const f32x16& cur, f32x16& nxt, const u32x4 (&before)[2], u32x4 (&p)[2], lds_cptr ka, lds_cptr va, int k0_next, bool masked_next) __attribute__((always_inline)) {
-                constexpr int H = decltype(half_tag)::value;  // nxt: the block's second half, or the next block's first
-                float by = 1.f;
-                const bool grew = __any(mx > row.m + kSlack);
-                if (grew) by = row.move(mx);
-                bf16x8 op[16 + kAhead];
-                auto read = [&](auto oc) __attribute__((always_inline)) {
-                    constexpr int o = decltype(oc)::value;
-                    if constexpr (o < 8) op[o] = k_operand(ka, o, 1 - H);
-                    else if constexpr (o < 16) op[o] = v_operand(va, o & 3, 2 * (1 - H) + ((o - 8) >> 2));
-                };
-                static_for<0, kAhead>([&](auto oc) { read(oc); });
-                FENCE();
-                static_for<0, 16>([&](auto sc_) __attribute__((always_inline)) {
-                    constexpr int slot = decltype(sc_)::value;
-                    if constexpr (slot < 8) nxt = mfma32(op[slot], qreg[slot], slot == 0 ? zero16 : nxt);
-                    else row.o[slot & 3] = mfma32(op[slot], __builtin_bit_cast(bf16x8, before[(slot - 8) >> 2]), row.o[slot & 3]);
-                    read(std::integral_constant<int, slot + kAhead>{});
-                    if constexpr (slot % 2 == 0) p[slot >> 3][(slot >> 1) & 3] = pair(weight(cur, slot), weight(cur, slot + 1));
-                    if constexpr (slot == 13) {
-                        if (masked_next) mask(nxt, k0_next);
-                        mx = largest(nxt) * c2;
-                    }
-                    FENCE();
-                });
-                if (grew) row.scale(by);
-            };
-            typedef std::integral_constant<int, 0> H0;
-            typedef std::integral_constant<int, 1> H1;
-            {
-                const lds_cptr ka = k_block(kb);
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) sa = mfma32(k_operand(ka, ks, 0), qreg[ks], ks == 0 ? zero16 : sa);
-            }
-            if (masked(jb0)) mask(sa, jb0 * kKeys);
-            mx = largest(sa) * c2;
-            // before the first step: weights of zero for keys of the piece
-            lds_cptr va = v_block(vb);
-            pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};
-            for (int j = 0; j < blocks; ++j) {
-                const int jb = jb0 + j;
-                begin(j);
-                step(H0{}, sa, sb, pb, pa, k_block(kb), va, jb * kKeys + 32, masked(jb));
-                va = v_block(vb);
-                step(H1{}, sb, sa, pa, pb, k_block(next_k()), va, (jb + 1) * kKeys, masked(jb + 1));
-                end(j);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(v_operand(va, i & 3, 2 + (i >> 2)), __builtin_bit_cast(bf16x8, pb[i >> 2]), row.o[i & 3]);
-        }
-
-        // ---- out
-        row.l += __shfl_xor(row.l, 32);
-        if (halves) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
-            f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & (kWaves / 2 - 1)) * (17 * 64) + lane;
-            if (wave_on && wave >= kWaves / 2) {
-                there[0] = f32x4{row.m, row.l, 0.f, 0.f};
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) there[(1 + d * 4 + e / 4) * 64] = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
-            }
-            __syncthreads();
-            if (wave_on && wave < kWaves / 2) {
-                const f32x4 ml = there[0];
-                const float mnew = fmaxf(row.m, ml[0]), by = fast_exp2(ml[0] - mnew), own = fast_exp2(row.m - mnew);
-                row.scale(own);
-                row.m = mnew;
-                row.l = fmaf(ml[1], by, row.l * own);
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const f32x4 x = there[(1 + d * 4 + e / 4) * 64];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) row.o[d][e + i] = fmaf(x[i], by, row.o[d][e + i]);
-                    }
-            }
-        }
-        if (!valid || (halves && wave >= kWaves / 2)) return;
-        const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
-        if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
-            const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
-                    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                    store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
-                }
-        } else {
-            float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                               : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-            if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
-        }
-    });
 }
 
 // Thirty-two lanes per row, four channels each.
@@ -1145,9 +1159,9 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
         store_row(a, row.token, row.head, c4, x, row.routed ? sums.value() : z, lse_l, row.routed ? sums.lse() : -INFINITY);
     }
 }
-// Rows of sequences of few: a workgroup per row, whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
+// Rows of short calls: a workgroup per row, whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
 constexpr int kSlices = 8;
-__global__ __launch_bounds__(32 * kSlices) void extend_combine_few_kernel(ExtendArgs a) {
+__global__ __launch_bounds__(32 * kSlices) void extend_combine_short_kernel(ExtendArgs a) {
     __shared__ __attribute__((aligned(16))) float part[2][kSlices][kPart];
     const Geom& gm = a.gm;
     const int c4 = (threadIdx.x & 31) * 4, slice = threadIdx.x >> 5, G = gm.G;
@@ -1204,8 +1218,9 @@ size_t lay_out(ExtendArgs& a, char* base) {
     };
     const size_t rows = (size_t)g.T * g.G, pairs = (size_t)g.B * g.Hkv;
     a.workgroups = kWorkgroups;
-    a.few = (long long)a.max_new * g.G <= 32;
-    a.tile_rows = a.few ? 32 : 32 * kWaves;
+    const long long most = (long long)a.max_new * g.G;  // rows of a KV head of a sequence
+    a.few = most <= kHalvesRows;
+    a.tile_rows = most <= kSub ? kSub : a.few ? kHalvesRows : 32 * kWaves;
     a.most_tiles = (int)(2 * g.Hkv * (rows / a.tile_rows + g.B));
     take(a.head, 1);
     take(a.tiles, a.most_tiles);
@@ -1248,24 +1263,28 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
         KernelTimer kt("extend_list", st);
         hipLaunchKernelGGL(extend_list_kernel, dim3(g.B * g.Hkv), dim3(kListThreads), 0, st, a);
     }
-    const bool self = a.few && g.B * g.Hkv <= kFewPairs;
+    const bool self = a.few && g.B * g.Hkv <= kShortPairs;
     if (!self) {
         KernelTimer kt("extend_plan", st);
         hipLaunchKernelGGL(extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
     }
     {
         KernelTimer kt("extend", st);
-        const dim3 grid(a.workgroups), threads(64 * (a.few ? kFewWaves : kWaves));
-        if (self && c.fp8) hipLaunchKernelGGL((extend_few_kernel<true, true>), grid, threads, 0, st, a);
-        else if (self) hipLaunchKernelGGL((extend_few_kernel<false, true>), grid, threads, 0, st, a);
-        else if (a.few && c.fp8) hipLaunchKernelGGL((extend_few_kernel<true, false>), grid, threads, 0, st, a);
-        else if (a.few) hipLaunchKernelGGL((extend_few_kernel<false, false>), grid, threads, 0, st, a);
-        else if (c.fp8) hipLaunchKernelGGL(extend_kernel<true>, grid, threads, 0, st, a);
-        else hipLaunchKernelGGL(extend_kernel<false>, grid, threads, 0, st, a);
+        auto launch = [&](auto fp8) {
+            constexpr bool FP8 = decltype(fp8)::value;
+            const dim3 grid(a.workgroups), threads(64 * kWaves);
+            if (!a.few) hipLaunchKernelGGL(extend_kernel<FP8>, grid, threads, 0, st, a);
+            else if (a.tile_rows == kSub && self) hipLaunchKernelGGL((extend_short_kernel<FP8, true, true>), grid, threads, 0, st, a);
+            else if (a.tile_rows == kSub) hipLaunchKernelGGL((extend_short_kernel<FP8, true, false>), grid, threads, 0, st, a);
+            else if (self) hipLaunchKernelGGL((extend_short_kernel<FP8, false, true>), grid, threads, 0, st, a);
+            else hipLaunchKernelGGL((extend_short_kernel<FP8, false, false>), grid, threads, 0, st, a);
+        };
+        if (c.fp8) launch(std::true_type{});
+        else launch(std::false_type{});
     }
     {
         KernelTimer kt("extend_combine", st);
-        if (a.few) hipLaunchKernelGGL(extend_combine_few_kernel, dim3(g.T * g.Hq), dim3(32 * kSlices), 0, st, a);
+        if (a.few) hipLaunchKernelGGL(extend_combine_short_kernel, dim3(g.T * g.Hq), dim3(32 * kSlices), 0, st, a);
         else hipLaunchKernelGGL(extend_combine_kernel, dim3(a.most_tiles, a.tile_rows / kCombineRows), dim3(kThreads), 0, st, a);
     }
     return launch_status();
