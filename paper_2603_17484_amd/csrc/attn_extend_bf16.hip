@@ -515,6 +515,15 @@ struct RowSums {
     __device__ __forceinline__ void look(float mx) {
         if (__any(mx > m + kSlack)) scale(move(mx));
     }
+    // An infinity or a NaN that came into a sum has stayed in it.
+    __device__ __forceinline__ bool finite() const {
+        float z = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z = fmaf(o[d][e], 0.f, z);
+        return z == 0.f;
+    }
 };
 __device__ __forceinline__ float largest(const f32x16& s) {
     float m[5];
@@ -523,16 +532,94 @@ __device__ __forceinline__ float largest(const f32x16& s) {
     return fmaxf(fmaxf(fmaxf(m[0], m[1]), m[2]), fmaxf(fmaxf(m[3], m[4]), s[15]));
 }
 
+// Whether a lane of the workgroup says so; a barrier.  votes: NW words of LDS, not used again before another barrier.
+template <int NW>
+__device__ __forceinline__ bool vote(int* votes, bool yes) {
+    if (__any(yes) && (threadIdx.x & 63) == 0) votes[threadIdx.x >> 6] = 1;
+    else if ((threadIdx.x & 63) == 0) votes[threadIdx.x >> 6] = 0;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) any |= votes[i];
+    return any != 0;
+}
+// Where the sums of row r of a piece go, and whether these are all it has: then its result does.
+struct Out {
+    int token, head;
+    bool last, routed;  // last: O is written
+    float* sums;
+};
+__device__ __forceinline__ Out out_of(const ExtendArgs& a, const Tile& t, const plan::Piece& piece, int w, int r) {
+    const int code = row_code(a, t, t.first + r), tok = code / a.gm.G;
+    Out o;
+    o.token = t.s.start + tok, o.head = t.hk * a.gm.G + code - tok * a.gm.G;
+    const bool whole = piece.first && piece.last;
+    o.routed = token_routed(a, o.token, o.head);
+    o.last = whole && t.kind == plan::kWindow && !(t.s.pos + tok > a.gm.W && o.routed);  // (routed: its window is all there is, a = s)
+    o.sums = whole ? a.parts[t.kind] + ((size_t)o.token * a.gm.Hq + o.head) * kPart : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
+    return o;
+}
+// Four channels of a row's sums.
+__device__ __forceinline__ void store_sums(const ExtendArgs& a, const Out& o, int c4, float m, float l, const f32x4& x) {
+    if (o.last) {
+        const float inv = 1.f / l, lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
+        const f32x4 y = x * inv, z = {0.f, 0.f, 0.f, 0.f};
+        store_row(a, o.token, o.head, c4, y, o.routed ? y : z, lse, o.routed ? lse : -INFINITY);
+    } else {
+        if (c4 == 0) *reinterpret_cast<f32x2*>(o.sums) = f32x2{m, l};
+        *reinterpret_cast<f32x4*>(o.sums + 4 + c4) = x;
+    }
+}
+// A piece row by row and key by key: for those with keys that are not in every row's reach and with an infinity or a NaN in a sum.  It may
+// come from such a key's values, as a weight of zero does not keep it out of the other rows' sums.
+// (Looking for them among the values themselves, in the loops: 2.5 to 11 % of the main kernel's time.)
+template <int NW>
+__device__ __forceinline__ void rows_alone(const ExtendArgs& a, const Tile& t, const plan::Piece& piece, int w) {
+    const Geom& gm = a.gm;
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c4 = lane * 4;  // 32 lanes per row
+    const int32_t* const table = a.c.table + (size_t)t.b * a.c.max_pages;
+    const int b0 = (t.lo / kKeys + t.skip + piece.from) * kKeys, b1 = (t.lo / kKeys + t.skip + piece.to) * kKeys - 1;
+    auto values = [&](const char* pool, const unsigned char* scales, size_t row) __attribute__((always_inline)) {
+        if (!a.c.fp8) return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(pool + row * (kD * 2) + c4 * 2), f32x4);
+        const uint32_t x = *reinterpret_cast<const uint32_t*>(pool + row * kD + c4);
+        const float e = exponent_value(scales[row * kRowScales + c4 / kScaleBlock]);
+        const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, false)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, true));
+        return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
+    };
+    for (int r = group; r < t.rows; r += 2 * NW) {
+        const Out o = out_of(a, t, piece, w, r);
+        const Range keys = plan::row_keys(t.kind, t.s.pos + o.token - t.s.start, gm.W);
+        const f32x4 q = __builtin_convertvector(*reinterpret_cast<const bf16x4*>(a.q + ((size_t)o.token * gm.Hq + o.head) * kD + c4), f32x4);
+        float m = kNone, l = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int key = max(keys.lo, b0); key <= min(keys.hi, b1); ++key) {
+            const size_t row = pool_row(a.c, gm.Hkv, plan::clamp(table[key >> a.c.page_log2], 0, a.c.pages - 1), t.hk, key);
+            const f32x4 k = values(a.c.k, a.c.ks, row), v = values(a.c.v, a.c.vs, row);
+            float s = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) s += __shfl_xor(s, d);
+            s *= gm.scale_log2;
+            const float mnew = fmaxf(m, s), by = fast_exp2(m - mnew), p = fast_exp2(s - mnew);
+            l = fmaf(l, by, p), m = mnew;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(x[e], by, p * v[e]);
+        }
+        store_sums(a, o, c4, m, l, x);
+    }
+}
+
+// The functions that take a piece return false, in all lanes, where it is left to rows_alone.
+//
 // A tile of up to 32 rows, as decoding has them: bound by its loads.  Every wavefront takes 32 keys at a time, every eighth of the piece's,
 // through shared memory of its own and with sums of its own, so that none waits for another before the end, where the eight sums are joined.
 // (All wavefronts loading blocks of 64 keys for two of them to compute: 217 us for 64 sequences of 8K tokens in e4m3, 1.5 us a block.)
 constexpr int kSub = 32;
 template <int NW>
 struct FewLds {
-    static constexpr unsigned block = kSub / 4 * kFour, keys = NW * 2 * block, sums = NW * 32 * kPart * 4, used = keys > sums ? keys : sums;
+    static constexpr unsigned block = kSub / 4 * kFour, keys = NW * 2 * block, sums = NW * 32 * kPart * 4, votes = keys > sums ? keys : sums, used = votes + 64;
 };
 template <bool FP8, int NW>
-__device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
+__device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5, G = gm.G, hk = t.hk;
@@ -600,6 +687,7 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
     const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
+    auto masked = [&](int sb) __attribute__((always_inline)) { return sb * kSub < lo_max || sb * kSub + kSub - 1 > hi_min; };
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
     RowSums row;
@@ -632,7 +720,7 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
         for (int i = 0; i < 8; ++i) op[i] = v_operand(v_at, i & 3, i >> 2);
         FENCE();
         const int k0 = sb * kSub;
-        if (k0 < lo_max || k0 + kSub - 1 > hi_min) {
+        if (masked(sb)) {
             const int first = keys.lo - k0 - 4 * h, last = keys.hi - k0 - 4 * h;
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = c_row(e, 0) >= first && c_row(e, 0) <= last ? sc[e] : -INFINITY;
@@ -657,7 +745,9 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
     // ---- the eight wavefronts' sums, joined: 16 threads per row, eight channels each
     row.l += __shfl_xor(row.l, 32);
     float* const sums = reinterpret_cast<float*>(lds);  // [wave][row][kPart]
-    __syncthreads();  // every wavefront is done with its part of LDS
+    const bool some_masked = masked(sb0 - wave) || masked(sb1 - 1);
+    if (vote<NW>(reinterpret_cast<int*>(lds + FewLds<NW>::votes), some_masked && !row.finite())) return false;
+    // (every wavefront is done with its part of LDS)
     {
         float* const at = sums + (wave * 32 + n) * kPart;
         if (h == 0) *reinterpret_cast<f32x2*>(at) = f32x2{row.m, row.l};
@@ -685,22 +775,11 @@ __device__ __forceinline__ void few_rows(const ExtendArgs& a, char* lds, const T
             l = fmaf(ml[v][1], by, l);
             x += at[0] * by, y += at[1] * by;
         }
-        const int my_code = code_of(r), my_tok = my_code / G, head = hk * G + my_code - my_tok * G, token = t.s.start + my_tok;
-        const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
-        if (whole && t.kind == plan::kWindow && !(t.s.pos + my_tok > gm.W && routed)) {
-            const float inv = 1.f / l, lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
-            const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-            x *= inv, y *= inv;
-            store_row(a, token, head, c8, x, routed ? x : z, lse, routed ? lse : -INFINITY);
-            store_row(a, token, head, c8 + 4, y, routed ? y : z, lse, routed ? lse : -INFINITY);
-        } else {
-            float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                               : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-            if (c8 == 0) *reinterpret_cast<f32x2*>(out) = f32x2{m, l};
-            *reinterpret_cast<f32x4*>(out + 4 + c8) = x;
-            *reinterpret_cast<f32x4*>(out + 4 + c8 + 4) = y;
-        }
+        const Out o = out_of(a, t, piece, w, r);
+        store_sums(a, o, c8, m, l, x);
+        store_sums(a, o, c8 + 4, m, l, y);
     }
+    return true;
 }
 
 // Workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring segments and stretches.
@@ -738,7 +817,7 @@ __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
 static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
 template <bool FP8, bool HALVES>
-__device__ __forceinline__ void some_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
+__device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     typedef Lds<FP8, kWaves> L;
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -912,6 +991,8 @@ __device__ __forceinline__ void some_rows(const ExtendArgs& a, char* lds, const 
         for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(v_operand(va, i & 3, 2 + (i >> 2)), __builtin_bit_cast(bf16x8, pb[i >> 2]), row.o[i & 3]);
     }
 
+    if ((masked(jb0) || masked(jb0 + blocks - 1)) && vote<kWaves>(reinterpret_cast<int*>(lds + L::used), !row.finite())) return false;
+
     // ---- out
     row.l += __shfl_xor(row.l, 32);
     if constexpr (HALVES) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
@@ -940,42 +1021,29 @@ __device__ __forceinline__ void some_rows(const ExtendArgs& a, char* lds, const 
                 }
         }
     }
-    if (!valid || (HALVES && wave >= kWaves / 2)) return;
-    const bool whole = piece.first && piece.last, routed = token_routed(a, token, head);
-    if (whole && t.kind == plan::kWindow && !(pos > gm.W && routed)) {  // (routed: its window is all there is, a = s)
-        const float inv = 1.f / row.l, lse = (row.m + __builtin_amdgcn_logf(row.l)) * kLn2;
+    if (!valid || (HALVES && wave >= kWaves / 2)) return true;
+    const Out o = out_of(a, t, piece, w, r);
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const f32x4 x = {row.o[d][e] * inv, row.o[d][e + 1] * inv, row.o[d][e + 2] * inv, row.o[d][e + 3] * inv};
-                const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                store_row(a, token, head, d * 32 + c_row(e, h), x, routed ? x : z, lse, routed ? lse : -INFINITY);
-            }
-    } else {
-        float* out = whole ? a.parts[t.kind] + ((size_t)token * gm.Hq + head) * kPart
-                           : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
-        if (h == 0) *reinterpret_cast<f32x2*>(out) = f32x2{row.m, row.l};
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<f32x4*>(out + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
-    }
+        for (int e = 0; e < 16; e += 4) store_sums(a, o, d * 32 + c_row(e, h), row.m, row.l, f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]});
+    return true;
 }
 
 template <bool FP8>
 struct TileLds {
-    static constexpr unsigned used = Lds<FP8, kWaves>::used > FewLds<kWaves>::used ? Lds<FP8, kWaves>::used : FewLds<kWaves>::used;
+    static constexpr unsigned many = Lds<FP8, kWaves>::used + 64, used = many > FewLds<kWaves>::used ? many : FewLds<kWaves>::used;  // (64: votes)
 };
 template <bool FP8>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[TileLds<FP8>::used];
     by_address(lds);
     for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
-        if (t.rows <= kSub) few_rows<FP8, kWaves>(a, lds, t, piece, w);
-        else if (t.rows <= kHalvesRows) some_rows<FP8, true>(a, lds, t, piece, w);
-        else some_rows<FP8, false>(a, lds, t, piece, w);
+        bool done;
+        if (t.rows <= kSub) done = few_rows<FP8, kWaves>(a, lds, t, piece, w);
+        else if (t.rows <= kHalvesRows) done = some_rows<FP8, true>(a, lds, t, piece, w);
+        else done = some_rows<FP8, false>(a, lds, t, piece, w);
+        if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
     });
 }
 
@@ -994,8 +1062,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
     __shared__ __attribute__((aligned(1024))) char lds[kLds + (SELF ? sizeof(ShortPlan) : 0)];
     by_address(lds);
     auto rows = [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
-        if (FEW || t.rows <= kSub) few_rows<FP8, kWaves>(a, lds, t, piece, w);
-        else some_rows<FP8, true>(a, lds, t, piece, w);
+        bool done;
+        if (FEW || t.rows <= kSub) done = few_rows<FP8, kWaves>(a, lds, t, piece, w);
+        else done = some_rows<FP8, true>(a, lds, t, piece, w);
+        if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
     };
     if constexpr (!SELF) {
         for_pieces(a, rows);

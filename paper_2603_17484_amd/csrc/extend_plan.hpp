@@ -19,8 +19,8 @@ namespace l2a {
 namespace plan {
 
 constexpr int kKeys = 64;   // keys of a block
-constexpr int kStart = 2;   // what a tile costs besides its blocks, in blocks
-constexpr int kLeast = 4;   // > kStart: a piece of a tile has at least a block
+constexpr int kStart = 3;   // what a tile costs besides its blocks, in blocks
+constexpr int kLeast = 5;   // > kStart: a piece of a tile has at least a block
 
 // A sequence of the call: new tokens start .. start + n - 1 of the packed ones, at positions pos .. pos + n - 1.  Device data that is
 // out of range is clamped: any values give rows inside the tensors and positions inside the table.

@@ -250,3 +250,108 @@ def test_long_caches(new, cached, Hq, Hkv, W, f, fp8, page):
                 want = want.cpu().numpy()
                 near(name, to_host(got[rows, row:row + m].t().flatten()), want, np.full(want.shape, WEIGHT + SMALL) + 2.0 ** -22 * np.where(np.isfinite(want), np.abs(want), 0))
         row += m
+
+
+# ------------------------------------------------------------------------------------------
+# what is out of a row's reach
+# ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("new,cached,W,fp8", [([70], [100], 30, False), ([300], [100], 30, False), ([300], [100], 200, True), ([9], [50], 20, False), ([9], [50], 20, True),
+                                              ([40, 1, 1], [60, 99, 31], 50, False), ([1, 1, 1], [60, 99, 31], 40, False), ([1, 1, 1], [60, 99, 31], 40, True), ([130], [500], 4096, False)])
+def test_infinities_and_nan_reach_the_rows_that_see_them_and_no_others(new, cached, W, fp8):
+    s = Step(new, cached, 4, 2, W, 16, fp8, f=0.4, seed=sum(new))
+    for b in range(s.B):
+        for where, x in ((cached[b] + new[b] // 2, np.nan), (cached[b] + new[b] - 1, -np.inf), (max(cached[b] - W // 2, 0), np.inf), (cached[b] // 3, np.nan)):
+            s.v[b][where, 0, 5 + where % 7] = np.nan if fp8 else x
+        s.v[b][cached[b] + new[b] - 1, 1, 77] = np.nan
+        s.k[b][cached[b] + new[b] - 1, 1, 3] = np.nan
+    check_extend(s)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_pages_before_the_window_may_be_gone(fp8):
+    """With the Local branch alone a sequence's pages before its first new token's window are not read: their entries are anything."""
+    s = Step([1, 40, 300], [400, 900, 700], 4, 2, 100, 16, fp8, seed=5)
+    for b in range(s.B):
+        first = max(s.cached[b] - s.W, 0)
+        for t in range(first):
+            s.k[b][t] = s.v[b][t] = np.nan
+        s.table[b, :first // s.page] = -7
+    s.place = lambda b, t, old=s.place: old(b, t) if s.table[b, t // s.page] >= 0 else (s.pages - 1, 0)  # (a spare page stands for those)
+    check_extend(s, B.L2A_FLAG_SKIP_GLOBAL)
+
+
+def test_sequences_that_share_pages():
+    """A prefix that two sequences have in common, in the same pages."""
+    s = Step([5, 60, 1], [64, 64, 130], 4, 2, 30, 16, f=0.6, seed=9)
+    for x in (s.k, s.v):
+        x[1][:64] = x[0][:64]
+        x[2][:64] = x[0][:64]
+    s.table[1, :4] = s.table[2, :4] = s.table[0, :4]
+    check_extend(s)
+
+
+def test_more_new_tokens_than_were_announced_are_cut_off():
+    s = Step([9, 50, 1], [20, 30, 40], 4, 2, 30, 16, f=0.6, seed=10)
+    full = check_extend(s)[0][0]
+    alloc = GuardedAllocator()
+    p, c = cache_on_gpu(s, alloc, s.pool(s.k, [None] * 3), s.pool(s.v, [None] * 3))
+    for most in (5, 33):  # short calls and long ones
+        O = alloc((s.N, 4, D), torch.bfloat16).fill_(SENTINEL)
+        ws = B.alloc_extend_workspace(p, c, most, alloc).fill_(255)
+        B.l2a_attn_extend(p, c, up(s.q, torch.bfloat16), up(s.start), up(np.array(s.cached, np.int32)), up(s.mask), most, O, workspace=ws)
+        torch.cuda.synchronize()
+        alloc.check()
+        got, want = to_host(O), to_host(full)
+        for b in range(3):
+            i, n = s.start[b], min(s.new[b], most)
+            assert np.abs(got[i:i + n] - want[i:i + n]).max() < 0.05
+            assert (got[i + n:s.start[b + 1]] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("most", [1, 8, 33, 300])
+def test_damaged_device_data_stays_inside_the_tensors(most):
+    """Starts that do not ascend or lie outside, sequences that overlap, positions and pages outside: nothing outside the buffers is written,
+    and the next call is right again."""
+    s = Step([1, 30, 300, 2], [10, 100, 200, 300], 4, 2, 50, 16, f=0.5, seed=11)
+    alloc = GuardedAllocator()
+    p, c = cache_on_gpu(s, alloc, s.pool(s.k, [None] * 4), s.pool(s.v, [None] * 4))
+    O = alloc((s.N, 4, D), torch.bfloat16)
+    ws = B.alloc_extend_workspace(p, c, most, alloc).fill_(255)
+    q, mask = up(s.q, torch.bfloat16), up(s.mask)
+    big = 2 ** 31 - 1
+    for start in ([0, 1, 31, 331, 333], [300, 200, 100, 0, 333], [0, 333, 0, 333, 0], [-5, big, -big - 1, 7, big], [50, 40, 200, 190, 333]):
+        for pos in (s.cached, [-9, big, 10 ** 6, -big - 1]):
+            for bad_pages in (False, True):
+                c.tensors[4].copy_(up(s.table if not bad_pages else np.where(s.table % 3 == 0, -big - 1, big).astype(np.int32)))
+                B.l2a_attn_extend(p, c, q, up(np.array(start, np.int32)), up(np.array(pos, np.int32)), mask, most, O, workspace=ws)
+                torch.cuda.synchronize()
+                alloc.check()
+    check_extend(s)
+
+
+def test_a_pool_beyond_four_gigabytes():
+    """Pages at the end of pools of 4.3 GB each: 64-bit places throughout."""
+    page, Hkv = 1024, 8
+    s = Step([40, 1], [1500, 2047], 16, Hkv, 700, page, f=0.5, seed=12)
+    far = 2 ** 32 // (page * Hkv * 256) + 40
+    p = s.params()
+    c = B.alloc_cache(p, far, page, s.max_pages)
+    assert c.tensors[0].numel() * 2 > 2 ** 32
+    for t in c.tensors[:2]:
+        t[far - s.pages:].zero_()
+    table = np.where((s.table >= 0) & (s.table < s.pages), s.table + far - s.pages, s.table).astype(np.int32)
+    c.tensors[4].copy_(up(table))
+    start = up(s.start)
+    full = [up(np.concatenate([np.zeros((0, Hkv, D))] + x), torch.bfloat16) for x in (s.k, s.v)]
+    lens = np.array([len(x) for x in s.k])
+    pw = B.make_params(s.B, int(lens.sum()), 16, Hkv, D, 700)
+    all_start = up(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32))
+    zero = torch.zeros(s.B, dtype=torch.int32, device="cuda")
+    B.l2a_cache_write(pw, c, *full, all_start, zero)
+    back = [torch.empty_like(x) for x in full]
+    B.l2a_cache_read(pw, c, all_start, zero, *back)
+    assert all(torch.equal(a, b) for a, b in zip(full, back))
+    O = torch.empty(s.N, 16, D, dtype=torch.bfloat16, device="cuda")
+    B.l2a_attn_extend(p, c, up(s.q, torch.bfloat16), start, up(np.array(s.cached, np.int32)), up(s.mask), 40, O)
+    near_pool = check_extend(s)[0][0]
+    assert torch.equal(O, near_pool)
