@@ -260,8 +260,8 @@ int l2a_attn_decode(const l2a_params* p, const void* q, const void* k_cache, con
  * skip such rows, l2a_attn_extend clamps them into range.
  *
  * Errors of the three calls: L2A_ERR_NULL, L2A_ERR_ALIGN as everywhere (all tensors 16-byte aligned, table and index arrays 4-byte);
- * L2A_ERR_SHAPE for page_size not a power of two in 16..1024, pages or max_pages < 1, more than 2^25 tokens per
- * sequence, max_new < 1; L2A_ERR_UNSUPPORTED for p->dtype other than L2A_BF16, D other than 128, an unknown cache dtype,
+ * L2A_ERR_SHAPE for page_size not a power of two in 16..1024, pages or max_pages < 1, max_pages * page_size > 2^24,
+ * T * Hq > 2^27, B * Hkv > 65535, max_new < 1; L2A_ERR_UNSUPPORTED for p->dtype other than L2A_BF16, D other than 128, an unknown cache dtype,
  * L2A_FLAG_SCALAR, L2A_FLAG_RING_CACHE.
  */
 typedef struct l2a_cache {
@@ -277,7 +277,8 @@ typedef struct l2a_cache {
 /*
  * Cache rows of the packed tokens: written from (l2a_cache_write) or to (l2a_cache_read) k, v [T, Hkv, D] bf16.  Writing rounds
  * an L2A_FP8 cache's elements as above, reading is exact.  Of p: B, T, Hkv, D and dtype count (the other fields must still be
- * valid).  Two packed tokens with the same place in the pool (two sequences that share a page they both write): either one's row.
+ * valid).  Two packed tokens with the same place in the pool (two sequences that share a page and both write to it): the
+ * row's contents are undefined, no other row is touched.
  */
 int l2a_cache_write(const l2a_params* p, const l2a_cache* c, const void* k, const void* v, const int32_t* seq_start,
                     const int32_t* pos, void* stream);
@@ -301,7 +302,10 @@ int l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* seq_s
  *   lse_local, lse_global  out optional [Hq,T]; lse_global is -inf where d = 0
  *   S_opt, A_opt  out optional [T,Hq,D]; A is zero where d = 0
  *   workspace   l2a_extend_workspace_bytes(p, c, max_new) bytes, 16-byte aligned; as everywhere not preserved, and calls that share one (captured
- *               graphs of them, too) must be ordered
+ *               graphs of them, too) must be ordered.  It holds the division of the work, the lists of routed rows and room for
+ *               partial sums (maximum, sum, O in fp32): two per row of the call, and two tiles (32 to 256 rows) per compute unit
+ * Outputs must not overlap inputs.  What is out of a row's reach, infinities and NaN included, never enters its result (a call
+ * whose keys in reach of some but not all rows hold infinite or NaN values does those rows singly, many times slower).
  * How a row's keys are shared out, and so the last bits of its results, depends on the whole call.
  */
 size_t l2a_extend_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_new);

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
         ends[threadIdx.x] = before + count;
         __syncthreads();
         const int of = min(pairs - p0, kPlanThreads);
-        for (int i0 = 0; i0 < here; i0 += kPlanThreads) {
+        for (int i0 = 0; i0 < here && tiles + i0 < a.most_tiles; i0 += kPlanThreads) {  // (more: sequences that overlap)
             const int i = i0 + (int)threadIdx.x;
             Tile t{};
             const bool on = i < here && tiles + i < a.most_tiles;
@@ -251,10 +251,9 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
             }
             line += sum;
         }
-        tiles += here;
+        tiles = min(tiles + here, a.most_tiles);
         __syncthreads();
     }
-    tiles = min(tiles, a.most_tiles);
     const int dearest = plan::block_cost(a.tile_rows, a.c.fp8);
     int per = plan::stretch(line, a.workgroups, dearest), segments = 0;
     const int segment = per / dearest;  // blocks
@@ -515,14 +514,15 @@ struct RowSums {
     __device__ __forceinline__ void look(float mx) {
         if (__any(mx > m + kSlack)) scale(move(mx));
     }
-    // An infinity or a NaN that came into a sum has stayed in it.
+    // An infinity or a NaN that came into a sum of values has stayed in it.  (Where the weights' sum, of both lanes of the row, is none either,
+    // the row's own scores are to blame.)
     __device__ __forceinline__ bool finite() const {
         float z = 0.f;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e) z = fmaf(o[d][e], 0.f, z);
-        return z == 0.f;
+        return z == 0.f || l * 0.f != 0.f;
     }
 };
 __device__ __forceinline__ float largest(const f32x16& s) {
@@ -991,10 +991,10 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
         for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(v_operand(va, i & 3, 2 + (i >> 2)), __builtin_bit_cast(bf16x8, pb[i >> 2]), row.o[i & 3]);
     }
 
+    row.l += __shfl_xor(row.l, 32);
     if ((masked(jb0) || masked(jb0 + blocks - 1)) && vote<kWaves>(reinterpret_cast<int*>(lds + L::used), !row.finite())) return false;
 
     // ---- out
-    row.l += __shfl_xor(row.l, 32);
     if constexpr (HALVES) {  // the second half's sums join the first's, through LDS (16-byte pieces of a lane side by side)
         f32x4* const there = reinterpret_cast<f32x4*>(lds) + (wave & (kWaves / 2 - 1)) * (17 * 64) + lane;
         if (wave_on && wave >= kWaves / 2) {

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void cache_rows_kernel(RowsArgs a) {
         if (b < 0 || tok >= a.seq_start[b + 1]) b = seq_of(a, tok);
         if (b < 0) continue;
         // places outside the table, and page numbers outside the pool, are never followed
-        const long long t = (long long)a.pos[b] + (tok - a.seq_start[b]);
+        const long long t = (long long)a.pos[b] + tok - a.seq_start[b];
         if (t < 0 || t >= a.c.capacity()) continue;
         const int page = a.c.table[(size_t)b * a.c.max_pages + (int)(t >> a.c.page_log2)];
         on[j] = page >= 0 && page < a.c.pages;

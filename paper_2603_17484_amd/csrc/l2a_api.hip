@@ -98,14 +98,18 @@ size_t bwd_workspace_bytes(const l2a_params& p) {
 
 // What the calls on a paged cache have in common: the cache's description, and sizes the kernels are built for.
 int check_cache(const l2a_params* p, const l2a_cache* c) {
-    const int rc = check_params(p);
+    if (!p) return L2A_ERR_NULL;
+    l2a_params packed = *p;
+    packed.B = 1;  // (T tokens are all there are)
+    const int rc = check_params(&packed);
     if (rc != L2A_OK) return rc;
+    if (p->B < 1 || (long long)p->B * p->Hkv > 65535 || (long long)p->T * p->Hq > (1LL << 27)) return L2A_ERR_SHAPE;
     if (!use_mfma(*p) || (p->flags & L2A_FLAG_RING_CACHE)) return L2A_ERR_UNSUPPORTED;
     if (!c || !c->k || !c->v || !c->table) return L2A_ERR_NULL;
     if (c->dtype != L2A_BF16 && c->dtype != L2A_FP8) return L2A_ERR_UNSUPPORTED;
     if (c->dtype == L2A_FP8 && (!c->k_scale || !c->v_scale)) return L2A_ERR_NULL;
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return L2A_ERR_SHAPE;
-    if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 25)) return L2A_ERR_SHAPE;
+    if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 24)) return L2A_ERR_SHAPE;
     if (misaligned(c->k) || misaligned(c->v) || (c->dtype == L2A_FP8 && (misaligned(c->k_scale) || misaligned(c->v_scale)))) return L2A_ERR_ALIGN;
     if (misaligned4(c->table)) return L2A_ERR_ALIGN;
     return L2A_OK;

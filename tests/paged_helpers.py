@@ -181,7 +181,6 @@ SENTINEL = -77.0
 def check_extend(s, flags=0, scale=None, max_new=None, optional=True):
     alloc = GuardedAllocator()
     (k, kq), (v, vq) = s.held(s.k), s.held(s.v)
-    np.seterr(invalid="ignore")
     p, c = cache_on_gpu(s, alloc, s.pool(s.k, kq), s.pool(s.v, vq))
     p = s.params(flags, scale)
     q = s.q.copy()
@@ -197,7 +196,8 @@ def check_extend(s, flags=0, scale=None, max_new=None, optional=True):
     B.l2a_attn_extend(p, c, up(q, torch.bfloat16), up(s.start), up(np.array(s.cached, np.int32)), mask, max_new, out[0], workspace=ws, **more)
     torch.cuda.synchronize()
     alloc.check()
-    S, A, tS, tA, ls, lg = reference(s, k, v, flags, scale)
+    with np.errstate(invalid="ignore"):
+        S, A, tS, tA, ls, lg = reference(s, k, v, flags, scale)
     O, So, Ao = (to_host(t) for t in out)
     outs = [("O", O, S + A, tS + tA)] + ([("S", So, S, tS), ("A", Ao, A, tA)] if optional else [])
     for name, got, want, tol in outs:
