@@ -121,3 +121,59 @@ def layer_from_numpy(q, k, v, mask, W, dtype="bf16", flags=0, scale=None, qg=Non
     up = lambda x: None if x is None else to_device(x, dtype, device)
     m = None if mask is None else torch.from_numpy(np.array(mask, dtype=np.uint8, order="C", copy=True)).to(device)
     return Layer(p, up(q), up(k), up(v), m, up(qg), up(kg), up(vg), GuardedAllocator() if guard else None)
+
+
+class PagedCache:
+    """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; p.T is set by every step) and the bookkeeping around it: pages
+    are handed out as sequences grow and taken back when they end.  The pool, the table and the steps' index arrays are on the GPU, what decides
+    about them on the host."""
+
+    def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda"):
+        self.p, self.page_size = p, page_size
+        self.cache = B.alloc_cache(p, pages, page_size, max_pages, fp8, device)
+        self.table = np.full((p.B, max_pages), -1, dtype=np.int32)
+        self.length = np.zeros(p.B, dtype=np.int32)
+        self.free = list(range(pages - 1, -1, -1))
+
+    def _upload(self, x: np.ndarray) -> torch.Tensor:
+        return torch.from_numpy(np.ascontiguousarray(x)).to(self.cache.tensors[4].device)
+
+    def begin_step(self, new):
+        """Room for new[b] tokens of every sequence.  -> (seq_start, pos) on the GPU; the params' T is their number."""
+        new = np.asarray(new, dtype=np.int32)
+        need = -(-(self.length + new) // self.page_size)
+        have = -(-self.length // self.page_size)
+        if (new < 0).any() or (need > self.table.shape[1]).any() or int((need - have).sum()) > len(self.free):
+            raise ValueError("no room for the step's tokens")
+        for b in np.nonzero(need > have)[0]:
+            for i in range(have[b], need[b]):
+                self.table[b, i] = self.free.pop()
+        self.cache.tensors[4].copy_(torch.from_numpy(self.table))
+        start, pos = self._upload(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), self._upload(self.length)
+        self.length = self.length + new
+        self.p.T = int(new.sum())
+        return start, pos
+
+    def extend(self, new, q, k, v, mask, **outs):
+        """Writes the packed new tokens' k, v and attends: q [T,Hq,D], k, v [T,Hkv,D], mask [mask_heads,T] -> o [T,Hq,D]."""
+        start, pos = self.begin_step(new)
+        O = torch.empty_like(q)
+        B.l2a_cache_write(self.p, self.cache, k, v, start, pos)
+        B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, max(int(max(new)), 1), O, **outs)
+        return O
+
+    def read(self, b: int):
+        """-> k, v [length, Hkv, D] of sequence b, as bf16."""
+        n = int(self.length[b])
+        size = np.where(np.arange(self.p.B) == b, n, 0)
+        k, v = (torch.empty(n, self.p.Hkv, self.p.D, dtype=torch.bfloat16, device=self.cache.tensors[4].device) for _ in range(2))
+        self.p.T = n
+        B.l2a_cache_read(self.p, self.cache, self._upload(np.concatenate([[0], np.cumsum(size)]).astype(np.int32)),
+                         self._upload(np.zeros(self.p.B, dtype=np.int32)), k, v)
+        return k, v
+
+    def end(self, b: int):
+        """Sequence b is over: its pages are free."""
+        used = -(-int(self.length[b]) // self.page_size)
+        self.free.extend(int(x) for x in self.table[b, :used])
+        self.table[b], self.length[b] = -1, 0
