@@ -39,6 +39,11 @@ struct Pair {  // a KV head of a sequence
     int first_tile, listed;      // its first tile, windows first; rows with keys before the window
     int segments, first_segment; // of each of its tiles of many rows with keys before the window; the first of them
 };
+struct Short {  // a KV head of a sequence in a call without lists: all that the last kernel has to know
+    Seq s;
+    int pad;
+    Place place[2];  // of its tiles on the line, by kind
+};
 struct Head {
     long long total;     // length of the line
     int per, tiles;      // its stretches; tiles on it
@@ -64,6 +69,7 @@ struct ExtendArgs {
     int32_t* first_tile;  // [workgroups] of a stretch
     Segment* segment;     // [workgroups]
     Pair* pairs;          // [B * Hkv]
+    Short* shorts;        // [B * Hkv] (few)
     int32_t* list;        // [Hkv][T G], a sequence's from its first row on: codes of the rows with keys before the window, ascending
     int32_t* rank;        // [Hkv][T G] place of a row in its list
     int32_t* token_seq;   // [T] (few)
@@ -213,6 +219,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
             const Seq s = seq_of(a, b);
             if (a.few) {  // one tile of all the sequence's rows
                 listed = has_prefix(a, s, hk) ? s.n * G : 0;
+                a.shorts[mine].s = s;
                 if (hk == 0)
                     for (int i = 0; i < s.n; ++i) a.token_seq[s.start + i] = b;
             } else {
@@ -248,6 +255,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
             if (on) {
                 t.start = line + at;
                 a.tiles[tiles + i] = t;
+                if (a.few) a.shorts[t.b * gm.Hkv + t.hk].place[t.kind] = place_of(a, t);
             }
             line += sum;
         }
@@ -543,18 +551,22 @@ __device__ __forceinline__ bool vote(int* votes, bool yes) {
     for (int i = 0; i < NW; ++i) any |= votes[i];
     return any != 0;
 }
+// Whether a row of a tile, given by its code, is routed.
+__device__ __forceinline__ bool code_routed(const ExtendArgs& a, const Tile& t, int code) {
+    return token_routed(a, t.s.start + code / a.gm.G, t.hk * a.gm.G + code % a.gm.G);
+}
 // Where the sums of row r of a piece go, and whether these are all it has: then its result does.
 struct Out {
     int token, head;
     bool last, routed;  // last: O is written
     float* sums;
 };
-__device__ __forceinline__ Out out_of(const ExtendArgs& a, const Tile& t, const plan::Piece& piece, int w, int r) {
-    const int code = row_code(a, t, t.first + r), tok = code / a.gm.G;
+__device__ __forceinline__ Out out_of(const ExtendArgs& a, const Tile& t, const plan::Piece& piece, int w, int r, int code, bool routed) {
+    const int tok = code / a.gm.G;
     Out o;
     o.token = t.s.start + tok, o.head = t.hk * a.gm.G + code - tok * a.gm.G;
     const bool whole = piece.first && piece.last;
-    o.routed = token_routed(a, o.token, o.head);
+    o.routed = routed;
     o.last = whole && t.kind == plan::kWindow && !(t.s.pos + tok > a.gm.W && o.routed);  // (routed: its window is all there is, a = s)
     o.sums = whole ? a.parts[t.kind] + ((size_t)o.token * a.gm.Hq + o.head) * kPart : a.slots + ((size_t)plan::slot(w, piece.first) * a.tile_rows + r) * kPart;
     return o;
@@ -587,7 +599,8 @@ __device__ __forceinline__ void rows_alone(const ExtendArgs& a, const Tile& t, c
         return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
     };
     for (int r = group; r < t.rows; r += 2 * NW) {
-        const Out o = out_of(a, t, piece, w, r);
+        const int code = row_code(a, t, t.first + r);
+        const Out o = out_of(a, t, piece, w, r, code, code_routed(a, t, code));
         const Range keys = plan::row_keys(t.kind, t.s.pos + o.token - t.s.start, gm.W);
         const f32x4 q = __builtin_convertvector(*reinterpret_cast<const bf16x4*>(a.q + ((size_t)o.token * gm.Hq + o.head) * kD + c4), f32x4);
         float m = kNone, l = 0.f;
@@ -775,7 +788,8 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
             l = fmaf(ml[v][1], by, l);
             x += at[0] * by, y += at[1] * by;
         }
-        const Out o = out_of(a, t, piece, w, r);
+        const int out_code = code_of(r);
+        const Out o = out_of(a, t, piece, w, r, out_code, code_routed(a, t, out_code));
         store_sums(a, o, c8, m, l, x);
         store_sums(a, o, c8 + 4, m, l, y);
     }
@@ -843,6 +857,8 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
     const __bf16* qp = a.q + ((size_t)token * gm.Hq + head) * kD + 8 * h;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+    int routed = token_routed(a, token, head);
+    asm volatile("" : "+v"(routed));
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
     // blocks that every row of the tile sees whole: from `whole0` to `whole1` - 1
@@ -1022,7 +1038,7 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
         }
     }
     if (!valid || (HALVES && wave >= kWaves / 2)) return true;
-    const Out o = out_of(a, t, piece, w, r);
+    const Out o = out_of(a, t, piece, w, r, code, routed);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -1095,7 +1111,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
         scan<64 * kWaves>(steps[0] + steps[1], plan_.sums, at, total);
         total = same(total), tiles = same(tiles);
         const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, FP8))), x0 = w * per;
-        const Pair pair{T, on[plan::kPrefix] ? s.n * gm.G : 0, 0, 0};
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (on[kind]) {
@@ -1103,12 +1118,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
                 if (at <= x0 && x0 < at + steps[kind]) plan_.first = T;
                 if (w == 0) {
                     t[kind].start = at;
-                    a.tiles[T] = t[kind];
+                    a.shorts[mine].place[kind] = place_of(a, t[kind]);
                 }
                 ++T, at += steps[kind];
             }
         if (w == 0 && mine < pairs) {
-            a.pairs[mine] = pair;
+            a.shorts[mine].s = s;
             if (hk == 0)
                 for (int i = 0; i < s.n; ++i) a.token_seq[s.start + i] = b;
             if (mine == 0) *a.head = Head{total, per, tiles, 0, 0};
@@ -1151,27 +1166,32 @@ struct Pieces {
     }
     Pieces() = default;
     __device__ __forceinline__ bool whole() const { return first >= last; }
-    // every `step`-th of them from the `from`-th on; row_parts: where the line's sums are if it is whole
-    __device__ __forceinline__ void join(const ExtendArgs& a, Sums& sums, int r, const float* row_parts, int c4, int from, int step) const {
-        constexpr int kAhead = 8;  // loads of this many on their way together (past the end the first is read again, for nobody)
-        const int n = segments + (whole() ? 1 : last - first + 1);
-        for (int i0 = from; i0 < n; i0 += kAhead * step) {
-            f32x2 ml[kAhead];
-            f32x4 x[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int i = i0 + j * step < n ? i0 + j * step : i0, k = i - segments;
-                const float* part = a.slots + ((size_t)(i < segments ? plan::slot(first_segment + i * of, 0) : plan::slot(line + first + k, k == 0)) * a.tile_rows + r) * kPart;
-                if (i >= segments && whole()) part = row_parts;
-                ml[j] = *reinterpret_cast<const f32x2*>(part);
-                x[j] = *reinterpret_cast<const f32x4*>(part + 4 + c4);
-            }
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (i0 + j * step < n) sums.join(ml[j][0], ml[j][1], x[j]);
-        }
+    __device__ __forceinline__ int count() const { return segments + (whole() ? 1 : last - first + 1); }
+    // where the i-th of row r's sums are; row_part: if it is the line's and the tile is whole there
+    __device__ __forceinline__ const float* at(const ExtendArgs& a, int i, int r, const float* row_part) const {
+        const int k = i - segments;
+        const float* const part = a.slots + ((size_t)(i < segments ? plan::slot(first_segment + i * of, 0) : plan::slot(line + first + k, k == 0)) * a.tile_rows + r) * kPart;
+        return i >= segments && whole() ? row_part : part;
     }
 };
+// Every `step`-th of n sums from the `from`-th on, at(i), joined: f(i, maximum, sum, four channels).  AHEAD loads are on their way together
+// (past the end the first is read again, for nobody).
+template <int AHEAD, typename At, typename F>
+__device__ __forceinline__ void each_part(int n, int from, int step, int c4, At&& at, F&& f) {
+    for (int i0 = from; i0 < n; i0 += AHEAD * step) {
+        f32x2 ml[AHEAD];
+        f32x4 x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const float* const part = at(i0 + j * step < n ? i0 + j * step : i0);
+            ml[j] = *reinterpret_cast<const f32x2*>(part);
+            x[j] = *reinterpret_cast<const f32x4*>(part + 4 + c4);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i0 + j * step < n) f(i0 + j * step, ml[j][0], ml[j][1], x[j]);
+    }
+}
 __device__ __forceinline__ const float* row_part(const ExtendArgs& a, int kind, int token, int head) {
     return a.parts[kind] + ((size_t)token * a.gm.Hq + head) * kPart;
 }
@@ -1187,8 +1207,8 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
     __shared__ int count;
     const Geom& gm = a.gm;
     const Head head_ = uniform(a.head);
+    const Tile t = uniform(a.tiles + blockIdx.x);  // (beside the head: there is room for as many tiles as workgroups)
     if ((int)blockIdx.x >= head_.tiles) return;
-    const Tile t = uniform(a.tiles + blockIdx.x);
     const int c4 = (threadIdx.x & 31) * 4, G = gm.G, r0 = blockIdx.y * kCombineRows;
     if (r0 >= t.rows || (a.do_local && t.kind != plan::kWindow)) return;
     const Pieces own(place_of(a, t), head_);
@@ -1218,14 +1238,21 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
     const f32x4 z = {0.f, 0.f, 0.f, 0.f};
     for (int i = threadIdx.x >> 5; i < count; i += kThreads / 32) {
         const Row row = rows[i];
-        Sums sums;
+        Sums sums, prefix;
         f32x4 x = z;
         float lse_l = -INFINITY;
-        if (a.do_local) {
-            own.join(a, sums, row.r, row_part(a, plan::kWindow, row.token, row.head), c4, 0, 1);
-            x = sums.value(), lse_l = sums.lse();
-        }
-        if (row.prefix_row >= 0) row.prefix.join(a, sums, row.prefix_row, row_part(a, plan::kPrefix, row.token, row.head), c4, 0, 1);
+        const int mine = a.do_local ? own.count() : 0, n = mine + (row.prefix_row >= 0 ? row.prefix.count() : 0);
+        each_part<4>(n, 0, 1, c4,
+                     [&](int i) {
+                         return i < mine ? own.at(a, i, row.r, row_part(a, plan::kWindow, row.token, row.head))
+                                         : row.prefix.at(a, i - mine, row.prefix_row, row_part(a, plan::kPrefix, row.token, row.head));
+                     },
+                     [&](int i, float m, float l, const f32x4& o) {
+                         if (i < mine) sums.join(m, l, o);
+                         else prefix.join(m, l, o);
+                     });
+        if (a.do_local) x = sums.value(), lse_l = sums.lse();
+        sums.join(prefix.m, prefix.l, prefix.o);
         store_row(a, row.token, row.head, c4, x, row.routed ? sums.value() : z, lse_l, row.routed ? sums.lse() : -INFINITY);
     }
 }
@@ -1236,21 +1263,22 @@ __global__ __launch_bounds__(32 * kSlices) void extend_combine_short_kernel(Exte
     const Geom& gm = a.gm;
     const int c4 = (threadIdx.x & 31) * 4, slice = threadIdx.x >> 5, G = gm.G;
     const int token = blockIdx.x / gm.Hq, head = blockIdx.x - token * gm.Hq, hk = head / G;
-    const int b = a.token_seq[token];  // of a token that is in no sequence: whatever was there
+    const int b = *(const scalar int*)(uintptr_t)(a.token_seq + token);  // of a token that is in no sequence: whatever was there
+    const Head head_ = uniform(a.head);
+    const bool routed = token_routed(a, token, head);
     if (b < 0 || b >= gm.B) return;
-    const Seq s = seq_of(a, b);
-    const int at = token - s.start;
-    if (at < 0 || at >= s.n) return;
-    const Head head_ = *a.head;
-    const bool routed = token_routed(a, token, head), prefix = routed && s.pos + at > gm.W;
-    const int windows = window_tiles(a, s), r = at * G + head - hk * G, first = a.pairs[b * gm.Hkv + hk].first_tile;
-    if (first + windows + prefix > head_.tiles) return;
+    const Short call = uniform(a.shorts + b * gm.Hkv + hk);
+    const int at = token - call.s.start;
+    if (at < 0 || at >= call.s.n) return;
+    const bool prefix = routed && call.s.pos + at > gm.W;
+    const int r = at * G + head - hk * G;
     Sums sums[2];  // of the window's keys, of those before it
     for (int kind = 0; kind < 2; ++kind) {
         if (!(kind == plan::kWindow ? a.do_local : prefix)) continue;
-        const Pieces p(place_of(a, a.tiles[first + (kind == plan::kWindow ? 0 : windows)]), head_);
+        const Pieces p(call.place[kind], head_);
         if (kind == plan::kWindow && p.whole() && !prefix) return;  // written already
-        p.join(a, sums[kind], r, row_part(a, kind, token, head), c4, slice, kSlices);
+        each_part<8>(p.count(), slice, kSlices, c4, [&](int i) { return p.at(a, i, r, row_part(a, kind, token, head)); },
+                     [&](int, float m, float l, const f32x4& o) { sums[kind].join(m, l, o); });
     }
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
@@ -1297,6 +1325,7 @@ size_t lay_out(ExtendArgs& a, char* base) {
     take(a.first_tile, a.workgroups);
     take(a.segment, a.workgroups);
     take(a.pairs, pairs);
+    take(a.shorts, a.few ? pairs : 0);
     take(a.list, a.few ? 0 : rows * g.Hkv);
     take(a.rank, a.few ? 0 : rows * g.Hkv);
     take(a.token_seq, a.few ? g.T : 0);

@@ -108,7 +108,7 @@ def test_workspace_bytes(lib, T, Hq, Hkv, Bn, max_new):
     few, tile = most <= 128, 32 if most <= 32 else 128 if most <= 128 else 256
     tiles = 2 * Hkv * (T * G // tile + Bn)
     want = 256 + up(64 * tiles) + up(4 * 256) + up(12 * 256) + up(16 * Bn * Hkv) + up(2 * 256 * tile * 132 * 4) + 2 * up(T * Hq * 132 * 4)
-    want += up(4 * T) if few else 2 * up(4 * T * Hq)
+    want += up(4 * T) + up(48 * Bn * Hkv) if few else 2 * up(4 * T * Hq)
     assert lib.l2a_extend_workspace_bytes(ref(p), ref(cache()), max_new) == want
 
 
