@@ -173,13 +173,13 @@ __global__ __launch_bounds__(kListThreads) void extend_list_kernel(ExtendArgs a)
 }
 
 // Sum over the threads before this one, and over all of them.
-template <int THREADS>
-__device__ __forceinline__ void scan(int x, int* sums, int& before, int& total) {
+template <int THREADS, typename X>
+__device__ __forceinline__ void scan(X x, X* sums, X& before, X& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = x;
+    X upto = x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int below = __shfl_up(upto, o);
+        const X below = __shfl_up(upto, o);
         if (lane >= o) upto += below;
     }
     __syncthreads();
@@ -206,6 +206,7 @@ __device__ __forceinline__ Tile make_tile(const ExtendArgs& a, const Seq& s, int
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a) {
     __shared__ int sums[kPlanThreads / 64];
+    __shared__ unsigned lengths[kPlanThreads / 64];  // (a round's tiles together are shorter than 2^32)
     __shared__ int ends[kPlanThreads];  // tiles up to and with a pair, of the pairs at hand
     const Geom& gm = a.gm;
     const int pairs = gm.B * gm.Hkv, G = gm.G;
@@ -250,8 +251,8 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                 if (within < w) t = make_tile(a, s, b, hk, plan::kWindow, within * a.tile_rows, s.n * G);
                 else t = make_tile(a, s, b, hk, plan::kPrefix, (within - w) * a.tile_rows, a.pairs[p0 + lo].listed);
             }
-            int at, sum;
-            scan<kPlanThreads>(on ? (int)place_of(a, t).end() : 0, sums, at, sum);
+            unsigned at, sum;
+            scan<kPlanThreads>(on ? (unsigned)place_of(a, t).length() : 0u, lengths, at, sum);
             if (on) {
                 t.start = line + at;
                 a.tiles[tiles + i] = t;
@@ -304,8 +305,8 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                 }
                 t.start = 0;
             }
-            int at, sum;
-            scan<kPlanThreads>(i < tiles ? (int)place_of(a, t).end() : 0, sums, at, sum);
+            unsigned at, sum;
+            scan<kPlanThreads>(i < tiles ? (unsigned)place_of(a, t).length() : 0u, lengths, at, sum);
             if (i < tiles) a.tiles[i].start = line + at, a.tiles[i].blocks = t.blocks, a.tiles[i].skip = t.skip;
             line += sum;
         }
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     // the tile each stretch begins in
     for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
         const Place p = place_of(a, a.tiles[i]);
-        for (long long w = (p.start + per - 1) / per; w * per < p.end() && w < a.workgroups; ++w) a.first_tile[w] = i;
+        for (long long w = plan::workgroup_at(p.start + per - 1, per); w * per < p.end() && w < a.workgroups; ++w) a.first_tile[w] = i;
     }
 }
 
@@ -1099,28 +1100,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
             on[plan::kPrefix] = has_prefix(a, s, hk);
             plan_.seq[mine] = s;
         }
-        int steps[2] = {0, 0};
+        int length[2] = {0, 0};
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (on[kind]) {
                 t[kind] = make_tile(a, s, b, hk, kind, 0, s.n * gm.G);
-                steps[kind] = (int)place_of(a, t[kind]).end();
+                length[kind] = place_of(a, t[kind]).length();
             }
         int T, tiles, at, total;
         scan<64 * kWaves>(on[0] + on[1], plan_.sums, T, tiles);
-        scan<64 * kWaves>(steps[0] + steps[1], plan_.sums, at, total);
+        scan<64 * kWaves>(length[0] + length[1], plan_.sums, at, total);
         total = same(total), tiles = same(tiles);
         const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, FP8))), x0 = w * per;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (on[kind]) {
                 plan_.start[T] = at, plan_.of[T] = 2 * mine + kind;
-                if (at <= x0 && x0 < at + steps[kind]) plan_.first = T;
+                if (at <= x0 && x0 < at + length[kind]) plan_.first = T;
                 if (w == 0) {
                     t[kind].start = at;
                     a.shorts[mine].place[kind] = place_of(a, t[kind]);
                 }
-                ++T, at += steps[kind];
+                ++T, at += length[kind];
             }
         if (w == 0 && mine < pairs) {
             a.shorts[mine].s = s;

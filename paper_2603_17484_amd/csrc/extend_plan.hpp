@@ -3,9 +3,9 @@
 //
 // Work is a list of tiles (rows of one KV head of a sequence that see about the same keys), each with its blocks of kKeys keys.
 // Laid end to end the tiles form one line; every workgroup takes an equal stretch of it, whatever tiles lie there, so that a
-// long tile is shared by many and short ones are taken many at a time.  A block counts what it takes, `each` of its tile; a tile
-// counts kStart more blocks than it has, what it costs to begin and end one.  Ends of stretches that lie closer than kLeast blocks to
-// an end of their tile move there.
+// long tile is shared by many and short ones are taken many at a time.  A block counts what it takes, `each` of its tile, and a tile
+// start_cost besides, what it takes to begin and end one.  Ends of stretches that lie closer than kLeast blocks to an end of their tile
+// move there.
 #pragma once
 #include <stdint.h>
 
@@ -19,8 +19,7 @@ namespace l2a {
 namespace plan {
 
 constexpr int kKeys = 64;   // keys of a block
-constexpr int kStart = 3;   // what a tile costs besides its blocks, in blocks
-constexpr int kLeast = 5;   // > kStart: a piece of a tile has at least a block
+constexpr int kLeast = 2;   // blocks of a piece
 
 // A sequence of the call: new tokens start .. start + n - 1 of the packed ones, at positions pos .. pos + n - 1.  Device data that is
 // out of range is clamped: any values give rows inside the tensors and positions inside the table.
@@ -55,10 +54,12 @@ L2A_PLAN_FN int tile_blocks(const Range& k) { return k.hi < k.lo ? 0 : k.hi / kK
 // Rows of a sequence before the first one with keys before the window.
 L2A_PLAN_FN int rows_without_prefix(const Seq& s, int G, int W) { return clamp(W + 1 - s.pos, 0, s.n) * G; }
 
-// What a block takes, in units of about half a microsecond: tiles of few rows wait for their loads (e4m3 half as long), those of many for the
-// matrix cores.
+// What a block takes, in quarters of a microsecond, and what a tile does besides.  Measured, us: 2.1 a block of many rows and 2.35 in e4m3, 1.1 and
+// 1.55 of up to 128, 0.75 and 0.5 of few, which wait for their loads; 7.5 a tile.  (In calls of few rows alone the
+// waits of one workgroup are time for another's loads, and a tile counts half as much.)
 constexpr int kFewRows = 32, kManyRows = 128;
-L2A_PLAN_FN int block_cost(int rows, bool fp8) { return (rows <= kFewRows ? 1 : rows <= kManyRows ? 2 : 3) + (fp8 ? 0 : 1); }
+L2A_PLAN_FN int block_cost(int rows, bool fp8) { return rows <= kFewRows ? (fp8 ? 2 : 3) : rows <= kManyRows ? (fp8 ? 6 : 4) : fp8 ? 9 : 8; }
+L2A_PLAN_FN int start_cost(int each) { return each <= 3 ? 16 : 30; }
 
 // Tiles of keys before the window all begin at key 0.  Where those of many rows are longer than a stretch, segments of its length are cut off their
 // beginnings, as many for each such tile of a KV head as its first and shortest has, so that a block remains; each is the work of one
@@ -72,19 +73,26 @@ L2A_PLAN_FN int many_tiles(int rows, int tile_rows) { return rows / tile_rows + 
 struct Place {
     long long start;
     int blocks, each;
-    L2A_PLAN_FN int steps() const { return blocks + kStart; }
-    L2A_PLAN_FN long long end() const { return start + (long long)steps() * each; }
+    L2A_PLAN_FN int length() const { return start_cost(each) + blocks * each; }
+    L2A_PLAN_FN long long end() const { return start + length(); }
+    // ends of stretches before `begun` move to the tile's beginning, those behind it from `ended` on to its end
+    L2A_PLAN_FN int begun() const { return clamp(start_cost(each) + kLeast * each, 0, length()); }
+    L2A_PLAN_FN int ended() const {
+        const int x = start_cost(each) + (blocks - kLeast + 1) * each;
+        return clamp(x, begun(), length());
+    }
 };
 // The stretch of workgroup w: [w per, (w + 1) per).  No shorter than the dearest block, so that no two ends of stretches fall on the same block.
 L2A_PLAN_FN int stretch(long long total, int workgroups, int dearest) {
     const int per = (int)((total + workgroups - 1) / workgroups);
     return per > dearest ? per : dearest;
 }
-// The stretch's end x, in the tile it lies in, moved: how many steps from the tile's beginning.
+// The workgroup in whose stretch x lies.  (A division of 64 bits takes the GPU several times as long as one of 32.)
+L2A_PLAN_FN int workgroup_at(long long x, int per) { return (x >> 31) == 0 ? (int)x / per : (int)(x / per); }
+// The stretch's end x, in the tile it lies in, moved: how many blocks from the tile's beginning.
 L2A_PLAN_FN int moved(const Place& t, long long x) {
-    const int at = (int)(x - t.start) / t.each, len = t.steps();
-    if (at < kLeast) return 0;
-    return len - at < kLeast ? len : at;
+    const int at = (int)(x - t.start);
+    return at < t.begun() ? 0 : at >= t.ended() ? t.blocks : (at - start_cost(t.each)) / t.each;
 }
 // Workgroup w's blocks of a tile [from, to), none: from == to.  The tile must overlap its stretch.
 struct Piece {
@@ -93,24 +101,15 @@ struct Piece {
 };
 L2A_PLAN_FN Piece piece(const Place& t, int per, int w) {
     const long long x0 = (long long)w * per, x1 = x0 + per;
-    const int a = x0 <= t.start ? 0 : moved(t, x0), b = x1 >= t.end() ? t.steps() : moved(t, x1);
     Piece p;
-    p.first = a == 0, p.last = b == t.steps();
-    p.from = a > kStart ? a - kStart : 0;
-    p.to = b > kStart ? b - kStart : 0;
-    if (a >= b) p.from = p.to = 0;
+    p.from = x0 <= t.start ? 0 : moved(t, x0), p.to = x1 >= t.end() ? t.blocks : moved(t, x1);
+    p.first = p.from == 0, p.last = p.to == t.blocks;
+    if (p.from >= p.to) p.from = p.to = 0;
     return p;
 }
-// The workgroups that have pieces of a tile, from first_of to last_of: ends of stretches before `begun` move to its beginning or
-// lie before it, those from `ended` on to its end or lie behind it.
-L2A_PLAN_FN int first_of(const Place& t, int per) {
-    const long long begun = t.start + (long long)(t.steps() < kLeast ? t.steps() : kLeast) * t.each;
-    return (int)((begun - 1) / per);
-}
-L2A_PLAN_FN int last_of(const Place& t, int per) {
-    const int n = t.steps(), b = n - kLeast + 1, c = kLeast > b ? kLeast : b, ended = c < n ? c : n;
-    return (int)((t.start + (long long)ended * t.each - 1) / per);
-}
+// The workgroups that have pieces of a tile, from first_of to last_of.
+L2A_PLAN_FN int first_of(const Place& t, int per) { return workgroup_at(t.start + t.begun() - 1, per); }
+L2A_PLAN_FN int last_of(const Place& t, int per) { return workgroup_at(t.start + t.ended() - 1, per); }
 // Where a piece that is not the whole tile leaves its sums: every workgroup has a place for a tile that it does not begin and
 // one for a tile that it does not end.
 L2A_PLAN_FN int slot(int w, int first) { return 2 * w + (first ? 1 : 0); }
