@@ -1196,9 +1196,11 @@ __device__ __forceinline__ void each_part(int n, int from, int step, int c4, At&
 __device__ __forceinline__ const float* row_part(const ExtendArgs& a, int kind, int token, int head) {
     return a.parts[kind] + ((size_t)token * a.gm.Hq + head) * kPart;
 }
-// Rows of tiles of many, 32 of a tile per workgroup: a thread per row finds out whether something is left to do (rows of whole tiles that have no
+// Rows of tiles of many, 16 of a tile per workgroup: a thread per row finds out whether something is left to do (rows of whole tiles that have no
 // keys before their window were written by the kernel before) and where its sums lie, then 32 lanes take a row each of those.
-constexpr int kCombineRows = 32;
+// (32 rows a workgroup, and so four for each group of lanes one behind the other: 18.6 us for 14.0 at 300 tokens behind 3000, 19.7 for 16.7 at 1000
+// beside 31 single ones, 15.5 for 12.5 at 500 beside 39; but 10.6 for 12.5 at 3 x 777, where most rows have nothing left to do.)
+constexpr int kCombineRows = 16;
 __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) {
     struct Row {
         int token, head, r, routed, prefix_row;  // r: in the tile; prefix_row: in its tile of keys before the window, -1: it has none
