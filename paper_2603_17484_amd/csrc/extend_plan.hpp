@@ -54,11 +54,11 @@ L2A_PLAN_FN int tile_blocks(const Range& k) { return k.hi < k.lo ? 0 : k.hi / kK
 // Rows of a sequence before the first one with keys before the window.
 L2A_PLAN_FN int rows_without_prefix(const Seq& s, int G, int W) { return clamp(W + 1 - s.pos, 0, s.n) * G; }
 
-// What a block takes, in quarters of a microsecond, and what a tile does besides.  Measured, us: 2.1 a block of many rows and 2.35 in e4m3, 1.1 and
+// What a block takes, in quarters of a microsecond, and what a tile does besides.  Measured, us: 2.1 a block of many rows and 2.35 in e4m3, 1.15 and
 // 1.55 of up to 128, 0.75 and 0.5 of few, which wait for their loads; 7.5 a tile.  (In calls of few rows alone the
 // waits of one workgroup are time for another's loads, and a tile counts half as much.)
 constexpr int kFewRows = 32, kManyRows = 128;
-L2A_PLAN_FN int block_cost(int rows, bool fp8) { return rows <= kFewRows ? (fp8 ? 2 : 3) : rows <= kManyRows ? (fp8 ? 6 : 4) : fp8 ? 9 : 8; }
+L2A_PLAN_FN int block_cost(int rows, bool fp8) { return rows <= kFewRows ? (fp8 ? 2 : 3) : rows <= kManyRows ? (fp8 ? 6 : 5) : fp8 ? 9 : 8; }
 L2A_PLAN_FN int start_cost(int each) { return each <= 3 ? 16 : 30; }
 
 // Tiles of keys before the window all begin at key 0.  Where those of many rows are longer than a stretch, segments of its length are cut off their
