@@ -167,6 +167,8 @@ class PagedCache:
         n = int(self.length[b])
         size = np.where(np.arange(self.p.B) == b, n, 0)
         k, v = (torch.empty(n, self.p.Hkv, self.p.D, dtype=torch.bfloat16, device=self.cache.tensors[4].device) for _ in range(2))
+        if n == 0:
+            return k, v
         self.p.T = n
         B.l2a_cache_read(self.p, self.cache, self._upload(np.concatenate([[0], np.cumsum(size)]).astype(np.int32)),
                          self._upload(np.zeros(self.p.B, dtype=np.int32)), k, v)

@@ -403,3 +403,33 @@ def test_a_pool_beyond_four_gigabytes():
     B.l2a_attn_extend(p, c, up(s.q, torch.bfloat16), start, up(np.array(s.cached, np.int32)), up(s.mask), 40, O)
     near_pool = check_extend(s)[0][0]
     assert torch.equal(O, near_pool)
+
+
+# ------------------------------------------------------------------------------------------
+# the largest numbers of things
+# ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("chunk", [0, 70])
+def test_more_sequences_and_tiles_than_the_plan_takes_at_a_time(chunk):
+    """2400 KV heads of sequences, up to 4800 tiles: rounds of 1024 in the plan; beside a chunk, calls with lists."""
+    n = 1200
+    s = Step([1] * (n - 1) + [max(chunk, 1)], [(i * 37) % 40 for i in range(n)], 4, 2, 6, f=0.5, seed=14, scale=0.5)
+    check_extend(s)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_sequences_that_fill_their_tables(fp8):
+    s = Step([1, 40, 16], [63, 24, 0], 8, 2, 30, 16, fp8, f=0.5, seed=15, more_pages=0, spare=0)
+    assert s.max_pages * s.page == 64
+    check_extend(s)
+
+
+def test_max_new_may_be_anything_above():
+    s = Step([5, 0, 7], [50, 20, 0], 4, 2, 30, 16, f=0.5, seed=16)
+    for most in (7, 33, 1000, 2 ** 31 - 1):
+        check_extend(s, max_new=most)
+
+
+def test_nobody_has_new_tokens():
+    s = Step([0, 0], [50, 20], 4, 2, 30, 16, seed=17, tail=4)
+    check_extend(s)
+    check_extend(s, max_new=200)

@@ -32,6 +32,7 @@ def test_steps_of_a_server(fp8):
         if new == "end":  # sequence 1's pages go to others, later to a sequence that takes its place
             cache.end(1)
             k[1], v[1] = k[1][:0], v[1][:0]
+            assert cache.read(1)[0].shape == (0, Hkv, D)
             continue
         cached, N = [len(x) for x in k], sum(new)
         q, kn, vn = randn(N, Hq, D), randn(N, Hkv, D), randn(N, Hkv, D)
