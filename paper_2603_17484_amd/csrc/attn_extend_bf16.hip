@@ -16,7 +16,7 @@
 // Calls in which no sequence has more than 128 rows per KV head make no lists, and with up to 512 KV heads of sequences every workgroup
 // makes the plan for itself (extend_short_kernel, extend_combine_short_kernel): two launches instead of four, 25 us for a token behind 32K.
 //
-// Measured (us; one call among others on one box, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 125 (main 118: 5.1
+// Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 125 (main 118: 5.1
 // TB/s); 16 x 5 behind 32K 111; a token behind 32K 24 (18); 2048 behind 32K 343 (320), 4096 behind 124K 1670-1710 (1590-1670: 1.02-1.07
 // PFLOP/s; products of 8192 x 8192 matrices reach 1.28 with nothing between them); 1000 beside 31 single ones at 16K 173 (139);
 // 3 x 777 first tokens 62 (37).  Before the main kernel: lists 5 to 11, plan 8 to 13; behind it: sums joined, 6 to 26.
@@ -833,7 +833,7 @@ __device__ __forceinline__ void for_pieces(const ExtendArgs& a, F&& f) {
 __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory"); }
 
 // A tile by 8 wavefronts of 32 rows, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself and every operand
-// serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one box, at 2.1 GHz and
+// serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one card, at 2.1 GHz and
 // 1.9.  It is the power that bounds both.)
 // HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
