@@ -210,7 +210,9 @@ __device__ __forceinline__ Tile make_tile(const ExtendArgs& a, const Seq& s, int
     return t;
 }
 // A thread per KV head of a sequence, then one per tile, then one per stretch's beginning.
-constexpr int kPlanThreads = 1024;
+// (1024 threads: 11.4 us for 10.1 at 2048 tokens behind 32K and 7.7 for 7.0 at 3 x 777, as fewer wavefronts meet faster; 12.8 for 14.6 with
+// 900 tiles, a second round of them.  256: 12.3, 8.5 and 16.6.)
+constexpr int kPlanThreads = 512;
 __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a) {
     __shared__ int sums[kPlanThreads / 64];
     __shared__ unsigned lengths[kPlanThreads / 64];  // (a round's tiles together are shorter than 2^32)

@@ -410,7 +410,7 @@ def test_a_pool_beyond_four_gigabytes():
 # ------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("chunk", [0, 70])
 def test_more_sequences_and_tiles_than_the_plan_takes_at_a_time(chunk):
-    """2400 KV heads of sequences, up to 4800 tiles: rounds of 1024 in the plan; beside a chunk, calls with lists."""
+    """2400 KV heads of sequences, up to 4800 tiles: several rounds of the plan's threads; beside a chunk, calls with lists."""
     n = 1200
     s = Step([1] * (n - 1) + [max(chunk, 1)], [(i * 37) % 40 for i in range(n)], 4, 2, 6, f=0.5, seed=14, scale=0.5)
     check_extend(s)
