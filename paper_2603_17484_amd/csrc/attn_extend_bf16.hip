@@ -16,10 +16,10 @@
 // Calls in which no sequence has more than 128 rows per KV head make no lists, and with up to 512 KV heads of sequences every workgroup
 // makes the plan for itself (extend_short_kernel, extend_combine_short_kernel): two launches instead of four, 25 us for a token behind 32K.
 //
-// Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 125 (main 118: 5.1
-// TB/s); 16 x 5 behind 32K 111; a token behind 32K 24 (18); 2048 behind 32K 343 (320), 4096 behind 124K 1670-1710 (1590-1670: 1.02-1.07
-// PFLOP/s; products of 8192 x 8192 matrices reach 1.28 with nothing between them); 1000 beside 31 single ones at 16K 173 (139);
-// 3 x 777 first tokens 62 (37).  Before the main kernel: lists 5 to 11, plan 8 to 13; behind it: sums joined, 6 to 26.
+// Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 127 (main 118: 5.2
+// TB/s); 16 x 5 behind 32K 107; a token behind 32K 24 (18); 2048 behind 32K 330 (320), 4096 behind 124K 1643 (1577: 1.08 PFLOP/s; 1734 on another;
+// products of 8192 x 8192 matrices reach 1.28 with nothing between them); 1000 beside 31 single ones at 16K 168 (140);
+// 3 x 777 first tokens 61 (37).  Before the main kernel: lists 5 to 11, plan 7 to 15; behind it: sums joined, 6 to 27.
 #include "paged.hpp"
 #include "tiles.hpp"
 
