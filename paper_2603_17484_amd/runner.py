@@ -139,27 +139,48 @@ class PagedCache:
         return torch.from_numpy(np.ascontiguousarray(x)).to(self.cache.tensors[4].device)
 
     def begin_step(self, new):
-        """Room for new[b] tokens of every sequence.  -> (seq_start, pos) on the GPU; the params' T is their number."""
+        """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
+        number."""
         new = np.asarray(new, dtype=np.int32)
         need = -(-(self.length + new) // self.page_size)
         have = -(-self.length // self.page_size)
         if (new < 0).any() or (need > self.table.shape[1]).any() or int((need - have).sum()) > len(self.free):
             raise ValueError("no room for the step's tokens")
-        for b in np.nonzero(need > have)[0]:
-            for i in range(have[b], need[b]):
-                self.table[b, i] = self.free.pop()
-        self.cache.tensors[4].copy_(torch.from_numpy(self.table))
-        start, pos = self._upload(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), self._upload(self.length)
-        self.length = self.length + new
+        before, self.length = self.length, self.length + new
+        try:
+            for b in np.nonzero(need > have)[0]:
+                for i in range(have[b], need[b]):
+                    self.table[b, i] = self.free.pop()
+            self.cache.tensors[4].copy_(torch.from_numpy(self.table))
+            start, pos = self._upload(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), self._upload(before)
+        except BaseException:
+            self._take_back(before)
+            raise
         self.p.T = int(new.sum())
         return start, pos
 
+    def _take_back(self, length: np.ndarray):
+        """The sequences are as long as they were: what lies behind is free again, the pages that were handed out last first."""
+        used, have = -(-length // self.page_size), -(-self.length // self.page_size)
+        for b in np.nonzero(have > used)[0][::-1]:
+            for i in reversed(range(used[b], have[b])):
+                if self.table[b, i] >= 0:
+                    self.free.append(int(self.table[b, i]))
+                    self.table[b, i] = -1
+        self.length = length
+
     def extend(self, new, q, k, v, mask, **outs):
-        """Writes the packed new tokens' k, v and attends: q [T,Hq,D], k, v [T,Hkv,D], mask [mask_heads,T] -> o [T,Hq,D]."""
+        """Writes the packed new tokens' k, v and attends: q [T,Hq,D], k, v [T,Hkv,D], mask [mask_heads,T] -> o [T,Hq,D].  Where a call is
+        refused, the sequences are what they were before."""
+        before = self.length
         start, pos = self.begin_step(new)
-        O = torch.empty_like(q)
-        B.l2a_cache_write(self.p, self.cache, k, v, start, pos)
-        B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, max(int(max(new)), 1), O, **outs)
+        try:
+            O = torch.empty_like(q)
+            B.l2a_cache_write(self.p, self.cache, k, v, start, pos)
+            B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, max(int(max(new)), 1), O, **outs)
+        except BaseException:
+            self._take_back(before)
+            raise
         return O
 
     def read(self, b: int):

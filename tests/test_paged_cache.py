@@ -1,0 +1,97 @@
+"""The bookkeeping of runner.PagedCache on the CPU: the library's calls are replaced by ones that note what they were given, or refuse it."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_17484_amd import binding as B
+from paper_2603_17484_amd.runner import PagedCache
+
+D, HKV, PAGE, PAGES, MOST = 128, 2, 16, 12, 6
+
+
+class Calls:
+    """Stands for the library: notes (call, T, seq_start, pos, pages in the table), and refuses the call named in `refuse`."""
+
+    def __init__(self, monkeypatch):
+        self.seen, self.refuse = [], None
+
+        def alloc_cache(p, pages, page_size, max_pages, fp8, device):
+            c = B.l2a_cache(page_size=page_size, pages=pages, max_pages=max_pages)
+            c.tensors = (None, None, None, None, torch.full((p.B, max_pages), -1, dtype=torch.int32))
+            return c
+
+        def call(name):
+            def f(p, c, *args, **kw):
+                if name == self.refuse:
+                    raise ValueError(name)
+                start, pos = (args[2], args[3]) if name == "write" else (args[1], args[2]) if name == "extend" else (args[0], args[1])
+                self.seen.append((name, p.T, start.tolist(), pos.tolist(), c.tensors[4].clone().numpy()))
+            return f
+        monkeypatch.setattr(B, "alloc_cache", alloc_cache)
+        monkeypatch.setattr(B, "l2a_cache_write", call("write"))
+        monkeypatch.setattr(B, "l2a_attn_extend", call("extend"))
+        monkeypatch.setattr(B, "l2a_cache_read", call("read"))
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    return Calls(monkeypatch)
+
+
+def make(sequences=2):
+    return PagedCache(B.make_params(sequences, 1, 4, HKV, D, 30), PAGES, PAGE, MOST, device="cpu")
+
+
+def step(cache, new):
+    n = int(np.sum(new))
+    kv = torch.zeros(n, HKV, D, dtype=torch.bfloat16)
+    return cache.extend(new, torch.zeros(n, 4, D, dtype=torch.bfloat16), kv, kv, torch.zeros(1, n, dtype=torch.uint8))
+
+
+def held(cache):
+    """What the bookkeeping says, after a look at whether it agrees with itself."""
+    used = -(-cache.length // PAGE)
+    for b, n in enumerate(used):
+        assert (cache.table[b, :n] >= 0).all() and (cache.table[b, n:] == -1).all()
+    assert sorted(list(cache.free) + cache.table[cache.table >= 0].tolist()) == list(range(PAGES))
+    return cache.length.tolist(), cache.table.copy(), list(cache.free)
+
+
+@pytest.mark.parametrize("refused", ["write", "extend"])
+def test_a_refused_step_leaves_everything_as_it_was(calls, refused):
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    calls.refuse = refused
+    with pytest.raises(ValueError, match=refused):
+        step(cache, [40, 14])  # pages would have been handed out
+    after = held(cache)
+    assert after[0] == before[0] == [20, 3] and np.array_equal(after[1], before[1]) and after[2] == before[2]
+    calls.refuse, calls.seen = None, []
+    step(cache, [2, 1])
+    assert [x[:4] for x in calls.seen] == [(name, 3, [0, 2, 3], [20, 3]) for name in ("write", "extend")]
+    assert held(cache)[0] == [22, 4]
+
+
+def test_a_step_without_room_leaves_everything_as_it_was(calls):
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    for new in ([80, 0], [70, 94], [-1, 2]):
+        with pytest.raises(ValueError, match="no room"):
+            step(cache, new)
+        after = held(cache)
+        assert after[0] == before[0] and np.array_equal(after[1], before[1]) and after[2] == before[2]
+
+
+def test_steps_pages_and_ends(calls):
+    cache = make()
+    step(cache, [20, 0])
+    step(cache, [1, 33])
+    assert held(cache)[0] == [21, 33] and len(cache.free) == PAGES - 5
+    assert [x[1:4] for x in calls.seen[::2]] == [(20, [0, 20, 20], [0, 0]), (34, [0, 1, 34], [20, 0])]
+    assert np.array_equal(calls.seen[-1][4], cache.table)
+    cache.end(0)
+    assert held(cache)[0] == [0, 33] and len(cache.free) == PAGES - 3
+    step(cache, [6 * PAGE, 2])
+    assert held(cache)[0] == [96, 35]
