@@ -142,6 +142,8 @@ class PagedCache:
         """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
         number."""
         new = np.asarray(new, dtype=np.int32)
+        if new.shape != (self.p.B,):
+            raise ValueError(f"a step has a number of new tokens for each of the {self.p.B} sequences; got {new.tolist()}")
         need = -(-(self.length + new) // self.page_size)
         have = -(-self.length // self.page_size)
         if (new < 0).any() or (need > self.table.shape[1]).any() or int((need - have).sum()) > len(self.free):

@@ -95,3 +95,15 @@ def test_steps_pages_and_ends(calls):
     assert held(cache)[0] == [0, 33] and len(cache.free) == PAGES - 3
     step(cache, [6 * PAGE, 2])
     assert held(cache)[0] == [96, 35]
+
+
+@pytest.mark.parametrize("new", [[2], [1, 1, 1], 2, [[1, 1]], []])
+def test_a_number_of_tokens_for_every_sequence(calls, new):
+    """(a list of one entry would stand for all of them)"""
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    with pytest.raises(ValueError, match="each of the 2 sequences"):
+        cache.begin_step(new)
+    after = held(cache)
+    assert after[0] == before[0] and np.array_equal(after[1], before[1]) and len(calls.seen) == 2
