@@ -178,6 +178,10 @@ class PagedCache:
         start, pos = self.begin_step(new)
         try:
             O = torch.empty_like(q)
+            if self.p.T == 0:
+                if q.numel() or k.numel() or v.numel():
+                    raise ValueError("the step has no new tokens, but rows")
+                return O
             B.l2a_cache_write(self.p, self.cache, k, v, start, pos)
             B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, max(int(max(new)), 1), O, **outs)
         except BaseException:

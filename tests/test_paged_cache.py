@@ -107,3 +107,21 @@ def test_a_number_of_tokens_for_every_sequence(calls, new):
         cache.begin_step(new)
     after = held(cache)
     assert after[0] == before[0] and np.array_equal(after[1], before[1]) and len(calls.seen) == 2
+
+
+def test_a_step_without_new_tokens(calls):
+    """(the library refuses a call of no tokens)"""
+    cache = make()
+    for _ in range(2):
+        before = held(cache)
+        assert step(cache, [0, 0]).shape == (0, 4, D)
+        after = held(cache)
+        assert after[0] == before[0] and np.array_equal(after[1], before[1])
+        step(cache, [5, 0])
+    assert [x[1] for x in calls.seen] == [5, 5, 5, 5]
+    before = held(cache)
+    for rows in ((1, 0, 0), (0, 1, 0), (0, 0, 1)):
+        q, k, v = (torch.zeros(n, h, D, dtype=torch.bfloat16) for n, h in zip(rows, (4, HKV, HKV)))
+        with pytest.raises(ValueError, match="no new tokens"):
+            cache.extend([0, 0], q, k, v, None)
+    assert held(cache)[0] == before[0]
