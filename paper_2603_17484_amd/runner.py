@@ -141,12 +141,18 @@ class PagedCache:
     def begin_step(self, new):
         """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
         number."""
-        new = np.asarray(new, dtype=np.int32)
+        new = np.asarray(new)
         if new.shape != (self.p.B,):
             raise ValueError(f"a step has a number of new tokens for each of the {self.p.B} sequences; got {new.tolist()}")
+        if new.dtype.kind not in "biuf" or (new.dtype.kind == "f" and not (new == np.floor(new)).all()) or (new == np.inf).any():
+            raise ValueError(f"numbers of new tokens are whole numbers; got {new.tolist()}")
+        # (compared as they came: what does not fit into 32 bits does not fit into the table either)
+        if (new < 0).any() or (new > self.table.shape[1] * self.page_size - self.length.astype(np.int64)).any():
+            raise ValueError("no room for the step's tokens")
+        new = new.astype(np.int32)
         need = -(-(self.length + new) // self.page_size)
         have = -(-self.length // self.page_size)
-        if (new < 0).any() or (need > self.table.shape[1]).any() or int((need - have).sum()) > len(self.free):
+        if int((need - have).sum()) > len(self.free):
             raise ValueError("no room for the step's tokens")
         before, self.length = self.length, self.length + new
         try:

@@ -43,7 +43,7 @@ def make(sequences=2):
 
 
 def step(cache, new):
-    n = int(np.sum(new))
+    n = int(np.sum(np.asarray(new)))
     kv = torch.zeros(n, HKV, D, dtype=torch.bfloat16)
     return cache.extend(new, torch.zeros(n, 4, D, dtype=torch.bfloat16), kv, kv, torch.zeros(1, n, dtype=torch.uint8))
 
@@ -125,3 +125,24 @@ def test_a_step_without_new_tokens(calls):
         with pytest.raises(ValueError, match="no new tokens"):
             cache.extend([0, 0], q, k, v, None)
     assert held(cache)[0] == before[0]
+
+
+@pytest.mark.parametrize("new", [[2 ** 31 - 1, 0], [2 ** 31 - 16, 2 ** 31 - 16], [2 ** 40, 0], [2 ** 63 - 1, 1], [-2 ** 31, 2 ** 31 - 1]])
+def test_lengths_that_pass_32_bits(calls, new):
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    with pytest.raises(ValueError, match="no room"):
+        cache.begin_step(new)
+    after = held(cache)
+    assert after[0] == before[0] and np.array_equal(after[1], before[1]) and after[2] == before[2]
+
+
+def test_lengths_that_are_no_whole_numbers(calls):
+    cache = make()
+    for new in ([1.5, 1], [float("nan"), 1], [float("inf"), 1], ["a", 1], [None, 1]):
+        with pytest.raises(ValueError, match="whole numbers"):
+            cache.begin_step(new)
+    for new in ([1, 2], [1.0, 2.0], (1, 2), np.array([1, 2], np.uint8), torch.tensor([1, 2])):
+        step(cache, new)
+    assert held(cache)[0] == [5, 10]
