@@ -138,6 +138,10 @@ class PagedCache:
     def _upload(self, x: np.ndarray) -> torch.Tensor:
         return torch.from_numpy(np.ascontiguousarray(x)).to(self.cache.tensors[4].device)
 
+    def _check(self, b: int):
+        if not 0 <= b < self.p.B:
+            raise IndexError(f"there are sequences 0 .. {self.p.B - 1}; got {b}")
+
     def begin_step(self, new):
         """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
         number."""
@@ -197,6 +201,7 @@ class PagedCache:
 
     def read(self, b: int):
         """-> k, v [length, Hkv, D] of sequence b, as bf16."""
+        self._check(b)
         n = int(self.length[b])
         size = np.where(np.arange(self.p.B) == b, n, 0)
         k, v = (torch.empty(n, self.p.Hkv, self.p.D, dtype=torch.bfloat16, device=self.cache.tensors[4].device) for _ in range(2))
@@ -209,6 +214,7 @@ class PagedCache:
 
     def end(self, b: int):
         """Sequence b is over: its pages are free."""
+        self._check(b)
         used = -(-int(self.length[b]) // self.page_size)
         self.free.extend(int(x) for x in self.table[b, :used])
         self.table[b], self.length[b] = -1, 0

@@ -146,3 +146,17 @@ def test_lengths_that_are_no_whole_numbers(calls):
     for new in ([1, 2], [1.0, 2.0], (1, 2), np.array([1, 2], np.uint8), torch.tensor([1, 2])):
         step(cache, new)
     assert held(cache)[0] == [5, 10]
+
+
+def test_sequences_that_there_are_none_of(calls):
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    for b in (-1, -2, 2, 100):
+        with pytest.raises(IndexError):
+            cache.read(b)  # (-1: the last sequence's length, and no sequence's rows)
+        with pytest.raises(IndexError):
+            cache.end(b)
+    assert held(cache)[0] == before[0] and len(calls.seen) == 2
+    k, v = cache.read(1)
+    assert k.shape == v.shape == (3, HKV, D) and calls.seen[-1][:4] == ("read", 3, [0, 0, 3], [0, 0])
