@@ -124,12 +124,12 @@ def layer_from_numpy(q, k, v, mask, W, dtype="bf16", flags=0, scale=None, qg=Non
 
 
 class PagedCache:
-    """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; p.T is set by every step) and the bookkeeping around it: pages
+    """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; a copy is kept as .p, whose T every step sets) and the bookkeeping around it: pages
     are handed out as sequences grow and taken back when they end.  The pool, the table and the steps' index arrays are on the GPU, what decides
     about them on the host."""
 
     def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda"):
-        self.p, self.page_size = p, page_size
+        self.p, self.page_size = B.l2a_params.from_buffer_copy(p), page_size
         self.cache = B.alloc_cache(p, pages, page_size, max_pages, fp8, device)
         self.table = np.full((p.B, max_pages), -1, dtype=np.int32)
         self.length = np.zeros(p.B, dtype=np.int32)

@@ -160,3 +160,13 @@ def test_sequences_that_there_are_none_of(calls):
     assert held(cache)[0] == before[0] and len(calls.seen) == 2
     k, v = cache.read(1)
     assert k.shape == v.shape == (3, HKV, D) and calls.seen[-1][:4] == ("read", 3, [0, 0, 3], [0, 0])
+
+
+def test_the_params_given_stay_as_they_are(calls):
+    p = B.make_params(2, 77, 4, HKV, D, 30, flags=B.L2A_FLAG_DENSE)
+    caches = [PagedCache(p, PAGES, PAGE, MOST, device="cpu") for _ in range(2)]
+    for cache in caches:  # (layers of one model)
+        step(cache, [20, 3])
+        cache.read(0)
+    assert p.T == 77 and [x[1] for x in calls.seen] == [23, 23, 20] * 2
+    assert all(c.p.flags == B.L2A_FLAG_DENSE and c.p.W == 30 for c in caches)
