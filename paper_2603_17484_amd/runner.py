@@ -126,7 +126,8 @@ def layer_from_numpy(q, k, v, mask, W, dtype="bf16", flags=0, scale=None, qg=Non
 class PagedCache:
     """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; a copy is kept as .p, whose T every step sets) and the bookkeeping around it: pages
     are handed out as sequences grow and taken back when they end.  The pool, the table and the steps' index arrays are on the GPU, what decides
-    about them on the host."""
+    about them on the host.  A step uploads the table and its index arrays, which waits for the stream's earlier work, and allocates its output (and
+    its workspace, where none is given).  Steps of one cache are ordered, on one stream or by the caller."""
 
     def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda"):
         self.p, self.page_size = B.l2a_params.from_buffer_copy(p), page_size
@@ -142,9 +143,15 @@ class PagedCache:
         if not 0 <= b < self.p.B:
             raise IndexError(f"there are sequences 0 .. {self.p.B - 1}; got {b}")
 
+    def _check_not_captured(self):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("steps upload their indices from the host and cannot be captured; capture l2a_cache_write and l2a_attn_extend with index "
+                               "arrays at fixed addresses")
+
     def begin_step(self, new):
         """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
         number."""
+        self._check_not_captured()
         new = np.asarray(new)
         if new.shape != (self.p.B,):
             raise ValueError(f"a step has a number of new tokens for each of the {self.p.B} sequences; got {new.tolist()}")
@@ -202,6 +209,7 @@ class PagedCache:
     def read(self, b: int):
         """-> k, v [length, Hkv, D] of sequence b, as bf16."""
         self._check(b)
+        self._check_not_captured()
         n = int(self.length[b])
         size = np.where(np.arange(self.p.B) == b, n, 0)
         k, v = (torch.empty(n, self.p.Hkv, self.p.D, dtype=torch.bfloat16, device=self.cache.tensors[4].device) for _ in range(2))

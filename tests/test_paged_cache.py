@@ -170,3 +170,16 @@ def test_the_params_given_stay_as_they_are(calls):
         cache.read(0)
     assert p.T == 77 and [x[1] for x in calls.seen] == [23, 23, 20] * 2
     assert all(c.p.flags == B.L2A_FLAG_DENSE and c.p.W == 30 for c in caches)
+
+
+def test_steps_cannot_be_captured(calls, monkeypatch):
+    """Indices come from the host's memory: a graph would repeat the step it was captured in."""
+    cache = make()
+    step(cache, [20, 3])
+    before = held(cache)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    for call in (lambda: cache.begin_step([1, 1]), lambda: step(cache, [1, 1]), lambda: cache.read(0)):
+        with pytest.raises(RuntimeError, match="captured"):
+            call()
+    after = held(cache)
+    assert after[0] == before[0] and np.array_equal(after[1], before[1]) and len(calls.seen) == 2
