@@ -144,7 +144,7 @@ class PagedCache:
             raise IndexError(f"there are sequences 0 .. {self.p.B - 1}; got {b}")
 
     def _check_not_captured(self):
-        if torch.cuda.is_current_stream_capturing():
+        if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("steps upload their indices from the host and cannot be captured; capture l2a_cache_write and l2a_attn_extend with index "
                                "arrays at fixed addresses")
 

@@ -177,6 +177,7 @@ def test_steps_cannot_be_captured(calls, monkeypatch):
     cache = make()
     step(cache, [20, 3])
     before = held(cache)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
     for call in (lambda: cache.begin_step([1, 1]), lambda: step(cache, [1, 1]), lambda: cache.read(0)):
         with pytest.raises(RuntimeError, match="captured"):
