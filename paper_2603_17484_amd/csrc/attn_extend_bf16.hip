@@ -27,6 +27,7 @@ namespace l2a {
 namespace {
 
 using plan::kKeys;
+using plan::Pieces;
 using plan::Place;
 using plan::Range;
 using plan::Seq;
@@ -274,8 +275,8 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     }
     const int dearest = plan::block_cost(a.tile_rows, a.c.fp8);
     int per = plan::stretch(line, a.workgroups, dearest), segments = 0;
-    const int segment = per / dearest;  // blocks
-    if (!a.few && a.do_global && segment >= plan::kSegmentLeast) {
+    const int segment = plan::segment_blocks(per, dearest);
+    if (!a.few && a.do_global && segment) {
         for (int p0 = 0; p0 < pairs; p0 += kPlanThreads) {  // how many each pair has
             const int mine = p0 + (int)threadIdx.x;
             int each = 0, of = 0;
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
             segments += here;
         }
         __syncthreads();
-        if (segments >= a.workgroups) {  // (only lists that others wrote over could say so: sequences that overlap)
+        if (segments >= a.workgroups) {  // (lists that others wrote over, of sequences that overlap: a first tile that is not its pair's shortest)
             for (int i = threadIdx.x; i < pairs; i += kPlanThreads) a.pairs[i].segments = 0;
             segments = 0;
             __syncthreads();
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
                     t.skip = p.segments * segment;
                     t.blocks = max(t.blocks - t.skip, 0);
                     for (int k = 0; k < p.segments; ++k) {
-                        const int w = p.first_segment + k * of + j;
+                        const int w = plan::segment_workgroup(p.first_segment, of, k, j);
                         if (w < a.workgroups) a.segment[w] = Segment{i, k * segment, (k + 1) * segment};
                     }
                 }
@@ -1167,23 +1168,11 @@ struct Sums {
     __device__ __forceinline__ f32x4 value() const { return o / l; }
     __device__ __forceinline__ float lse() const { return (m + __builtin_amdgcn_logf(l)) * kLn2; }
 };
-// The sums that row r of a tile has in pieces: its segments' and those of its stretch of the line.
-struct Pieces {
-    int segments, first_segment, of;  // segment k: workgroup first_segment + k * of
-    int first, last, line;            // workgroups on the line, of which the first is workgroup number `line`
-    __device__ __forceinline__ Pieces(const Place& p, const Head& head) : segments(0), first_segment(0), of(0) {
-        first = plan::first_of(p, head.per), last = plan::last_of(p, head.per), line = head.segments;
-    }
-    Pieces() = default;
-    __device__ __forceinline__ bool whole() const { return first >= last; }
-    __device__ __forceinline__ int count() const { return segments + (whole() ? 1 : last - first + 1); }
-    // where the i-th of row r's sums are; row_part: if it is the line's and the tile is whole there
-    __device__ __forceinline__ const float* at(const ExtendArgs& a, int i, int r, const float* row_part) const {
-        const int k = i - segments;
-        const float* const part = a.slots + ((size_t)(i < segments ? plan::slot(first_segment + i * of, 0) : plan::slot(line + first + k, k == 0)) * a.tile_rows + r) * kPart;
-        return i >= segments && whole() ? row_part : part;
-    }
-};
+// Where the i-th of the sums that row r of a tile has in pieces are; row_part: if it is the line's and the tile is whole there.
+__device__ __forceinline__ const float* sums_at(const ExtendArgs& a, const Pieces& p, int i, int r, const float* row_part) {
+    const float* const part = a.slots + ((size_t)p.slot_of(i) * a.tile_rows + r) * kPart;
+    return p.in_parts(i) ? row_part : part;
+}
 // Every `step`-th of n sums from the `from`-th on, at(i), joined: f(i, maximum, sum, four channels).  AHEAD loads are on their way together
 // (past the end the first is read again, for nobody).
 template <int AHEAD, typename At, typename F>
@@ -1223,7 +1212,7 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
     if ((int)blockIdx.x >= head_.tiles) return;
     const int c4 = (threadIdx.x & 31) * 4, G = gm.G, r0 = blockIdx.y * kCombineRows;
     if (r0 >= t.rows || (a.do_local && t.kind != plan::kWindow)) return;
-    const Pieces own(place_of(a, t), head_);
+    const Pieces own = plan::pieces_of(place_of(a, t), head_.per, head_.segments);
     if (threadIdx.x < kCombineRows) {
         const Pair pair = uniform(a.pairs + t.b * gm.Hkv + t.hk);
         const int first_prefix = pair.first_tile + window_tiles(a, t.s), many = plan::many_tiles(pair.listed, a.tile_rows), r = r0 + (int)threadIdx.x;
@@ -1238,8 +1227,8 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
             if (prefix) {
                 const int i = plan::clamp(list_of(a, a.rank, t.s, t.hk)[code], 0, max(pair.listed - 1, 0)), j = i / a.tile_rows;
                 row.prefix_row = i - j * a.tile_rows;
-                row.prefix = Pieces(place_of(a, a.tiles[min(first_prefix + j, head_.tiles - 1)]), head_);
-                row.prefix.segments = j < many ? pair.segments : 0, row.prefix.first_segment = pair.first_segment + j, row.prefix.of = many;
+                row.prefix = plan::pieces_of(place_of(a, a.tiles[min(first_prefix + j, head_.tiles - 1)]), head_.per, head_.segments);
+                row.prefix.segments = j < many ? pair.segments : 0, row.prefix.first_segment = plan::segment_workgroup(pair.first_segment, many, 0, j), row.prefix.of = many;
             }
         }
         const unsigned long long set = __ballot(todo);
@@ -1256,8 +1245,8 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
         const int mine = a.do_local ? own.count() : 0, n = mine + (row.prefix_row >= 0 ? row.prefix.count() : 0);
         each_part<4>(n, 0, 1, c4,
                      [&](int i) {
-                         return i < mine ? own.at(a, i, row.r, row_part(a, plan::kWindow, row.token, row.head))
-                                         : row.prefix.at(a, i - mine, row.prefix_row, row_part(a, plan::kPrefix, row.token, row.head));
+                         return i < mine ? sums_at(a, own, i, row.r, row_part(a, plan::kWindow, row.token, row.head))
+                                         : sums_at(a, row.prefix, i - mine, row.prefix_row, row_part(a, plan::kPrefix, row.token, row.head));
                      },
                      [&](int i, float m, float l, const f32x4& o) {
                          if (i < mine) sums.join(m, l, o);
@@ -1287,9 +1276,9 @@ __global__ __launch_bounds__(32 * kSlices) void extend_combine_short_kernel(Exte
     Sums sums[2];  // of the window's keys, of those before it
     for (int kind = 0; kind < 2; ++kind) {
         if (!(kind == plan::kWindow ? a.do_local : prefix)) continue;
-        const Pieces p(call.place[kind], head_);
+        const Pieces p = plan::pieces_of(call.place[kind], head_.per, head_.segments);
         if (kind == plan::kWindow && p.whole() && !prefix) return;  // written already
-        each_part<8>(p.count(), slice, kSlices, c4, [&](int i) { return p.at(a, i, r, row_part(a, kind, token, head)); },
+        each_part<8>(p.count(), slice, kSlices, c4, [&](int i) { return sums_at(a, p, i, r, row_part(a, kind, token, head)); },
                      [&](int, float m, float l, const f32x4& o) { sums[kind].join(m, l, o); });
     }
 #pragma unroll

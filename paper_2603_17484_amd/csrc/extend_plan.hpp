@@ -1,5 +1,5 @@
 // How the work of new tokens on a paged cache is shared out: plain integer code, compiled for the kernels and for the host, where
-// the CPU test replays every workgroup and checks that each block of keys is taken exactly once.
+// the CPU tests replay every workgroup and check that each block of keys is taken exactly once, and how even the shares are.
 //
 // Work is a list of tiles (rows of one KV head of a sequence that see about the same keys), each with its blocks of kKeys keys.
 // Laid end to end the tiles form one line; every workgroup takes an equal stretch of it, whatever tiles lie there, so that a
@@ -61,13 +61,23 @@ constexpr int kFewRows = 32, kManyRows = 128;
 L2A_PLAN_FN int block_cost(int rows, bool fp8) { return rows <= kFewRows ? (fp8 ? 2 : 3) : rows <= kManyRows ? (fp8 ? 6 : 5) : fp8 ? 9 : 8; }
 L2A_PLAN_FN int start_cost(int each) { return each <= 3 ? 16 : 30; }
 
-// Tiles of keys before the window all begin at key 0.  Where those of many rows are longer than a stretch, segments of its length are cut off their
-// beginnings, as many for each such tile of a KV head as its first and shortest has, so that a block remains; each is the work of one
-// workgroup.  The same segments of all tiles lie side by side, for workgroups on one XCD, which then read the same keys at the same time.
-// What remains of the tiles is the line, for the workgroups that remain: there are some, since every segment has a stretch's length.
+// Tiles of keys before the window all begin at key 0.  Where those of many rows are longer than a stretch, segments of its length, rounded up to whole
+// blocks, are cut off their beginnings, as many for each such tile of a KV head as its first and shortest has, so that a block remains; each is the
+// work of one workgroup.  The same segments of all tiles lie side by side, for workgroups on one XCD, which then read the same keys at the same time.
+// What remains of the tiles is the line, for the workgroups that remain.  There are some, and their stretches are no longer than `per` was: a line no
+// longer than 256 per, less s segments none of which is shorter than per, is no longer than (256 - s) per, and it is not empty.
+// (Rounded down, segments left more of the line than the remaining workgroups' share: 128 tokens of 28 / 4 heads behind 64K, window 512,
+// 20 % routed, were 252 segments and four stretches 3.7 times as long as the others' work: 174 us for 98.  313 of 12 / 1 heads behind 17548, all
+routed: 427 for 77.)
 constexpr int kSegmentLeast = 16;  // blocks
-L2A_PLAN_FN int segments(int blocks, int segment) { return blocks > 0 && segment >= kSegmentLeast ? (blocks - 1) / segment : 0; }
+L2A_PLAN_FN int segment_blocks(int per, int dearest) {  // 0: none are cut
+    const int x = (per + dearest - 1) / dearest;
+    return x >= kSegmentLeast ? x : 0;
+}
+L2A_PLAN_FN int segments(int blocks, int segment) { return blocks > 0 && segment > 0 ? (blocks - 1) / segment : 0; }
 L2A_PLAN_FN int many_tiles(int rows, int tile_rows) { return rows / tile_rows + (rows % tile_rows > kManyRows ? 1 : 0); }
+// The workgroup of segment k of the j-th of a KV head's `of` tiles that have some.
+L2A_PLAN_FN int segment_workgroup(int first_segment, int of, int k, int j) { return first_segment + k * of + j; }
 
 // A tile's place in the line.
 struct Place {
@@ -113,6 +123,19 @@ L2A_PLAN_FN int last_of(const Place& t, int per) { return workgroup_at(t.start +
 // Where a piece that is not the whole tile leaves its sums: every workgroup has a place for a tile that it does not begin and
 // one for a tile that it does not end.
 L2A_PLAN_FN int slot(int w, int first) { return 2 * w + (first ? 1 : 0); }
+// The pieces whose sums a tile's rows have: its segments, then those of its stretch of the line.
+struct Pieces {
+    int segments, first_segment, of;  // segment k: workgroup first_segment + k of
+    int first, last, line;            // workgroups on the line, of which the first is workgroup number `line`
+    L2A_PLAN_FN bool whole() const { return first >= last; }
+    L2A_PLAN_FN int count() const { return segments + (whole() ? 1 : last - first + 1); }
+    L2A_PLAN_FN bool in_parts(int i) const { return i >= segments && whole(); }  // the i-th: no slot, every row has a place for it
+    L2A_PLAN_FN int slot_of(int i) const {
+        const int k = i - segments;
+        return i < segments ? slot(segment_workgroup(first_segment, of, i, 0), 0) : slot(line + first + k, k == 0);
+    }
+};
+L2A_PLAN_FN Pieces pieces_of(const Place& t, int per, int line) { return Pieces{0, 0, 0, first_of(t, per), last_of(t, per), line}; }
 
 }  // namespace plan
 }  // namespace l2a
