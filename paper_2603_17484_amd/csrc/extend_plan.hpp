@@ -68,7 +68,7 @@ L2A_PLAN_FN int start_cost(int each) { return each <= 3 ? 16 : 30; }
 // longer than 256 per, less s segments none of which is shorter than per, is no longer than (256 - s) per, and it is not empty.
 // (Rounded down, segments left more of the line than the remaining workgroups' share: 128 tokens of 28 / 4 heads behind 64K, window 512,
 // 20 % routed, were 252 segments and four stretches 3.7 times as long as the others' work: 174 us for 98.  313 of 12 / 1 heads behind 17548, all
-routed: 427 for 77.)
+// routed: 427 for 77.)
 constexpr int kSegmentLeast = 16;  // blocks
 L2A_PLAN_FN int segment_blocks(int per, int dearest) {  // 0: none are cut
     const int x = (per + dearest - 1) / dearest;
