@@ -304,7 +304,8 @@ int l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* seq_s
  *   workspace   l2a_extend_workspace_bytes(p, c, max_new) bytes, 16-byte aligned; as everywhere not preserved, and calls that share one (captured
  *               graphs of them, too) must be ordered.  It holds the division of the work, the lists of routed rows and room for
  *               partial sums (maximum, sum, O in fp32): two per row of the call, and two tiles (32 to 256 rows) per compute unit
- * Values are expected below 2^110 in magnitude: weights up to 2^8 times one another are summed before they are divided.
+ * Values are expected below 2^110 in magnitude: weights up to 2^8 times one another are summed before they are divided.  An infinite value in
+ * a row's reach makes its result infinite (a NaN where its weight is less than 2^-126 of the largest and so counts as zero).
  * Outputs must not overlap inputs.  What is out of a row's reach, infinities and NaN included, never enters its result (a call
  * whose keys in reach of some but not all rows hold infinite or NaN values does those rows singly, many times slower).
  * How a row's keys are shared out, and so the last bits of its results, depends on the whole call.

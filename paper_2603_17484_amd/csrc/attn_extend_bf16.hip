@@ -841,6 +841,12 @@ __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__
 // HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
 static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
+template <bool FP8>
+struct TileLds {
+    static constexpr unsigned many = Lds<FP8, kWaves>::used + 64, used = many > FewLds<kWaves>::used ? many : FewLds<kWaves>::used;  // (64: votes)
+    // behind these, half a block of V that is zero, for extend_kernel: what the first of a tile's products has beside weights of zero
+    static constexpr unsigned zeros = used, kZeros = kKeys / 8 * kFour;
+};
 template <bool FP8, bool HALVES>
 __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     typedef Lds<FP8, kWaves> L;
@@ -1003,8 +1009,8 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
         }
         if (masked(jb0)) mask(sa, jb0 * kKeys);
         mx = largest(sa) * c2;
-        // before the first step: weights of zero for keys of the piece
-        lds_cptr va = v_block(vb);
+        // before the first step: weights of zero, and values of zero beside them (an infinity among the piece's own would be a NaN in all rows)
+        lds_cptr va = v_block(TileLds<FP8>::zeros - kKeys / 8 * kFour);  // its second half is what that step reads
         pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};
         for (int j = 0; j < blocks; ++j) {
             const int jb = jb0 + j;
@@ -1058,13 +1064,12 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
 }
 
 template <bool FP8>
-struct TileLds {
-    static constexpr unsigned many = Lds<FP8, kWaves>::used + 64, used = many > FewLds<kWaves>::used ? many : FewLds<kWaves>::used;  // (64: votes)
-};
-template <bool FP8>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[TileLds<FP8>::used];
+    typedef TileLds<FP8> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::zeros + L::kZeros];
     by_address(lds);
+    for (unsigned at = L::zeros + threadIdx.x * 16; at < L::zeros + L::kZeros; at += 64 * kWaves * 16)  // (every tile begins with a barrier)
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = u32x4{0u, 0u, 0u, 0u};
     for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
         bool done;
         if (t.rows <= kSub) done = few_rows<FP8, kWaves>(a, lds, t, piece, w);
