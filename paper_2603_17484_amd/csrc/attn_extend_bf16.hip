@@ -1262,13 +1262,14 @@ __global__ __launch_bounds__(kThreads) void extend_combine_kernel(ExtendArgs a) 
         store_row(a, row.token, row.head, c4, x, row.routed ? sums.value() : z, lse_l, row.routed ? sums.lse() : -INFINITY);
     }
 }
-// Rows of short calls: a workgroup per row, whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
+// Rows of short calls: a workgroup per row (from row0 on), whose pieces, many where the cache is long, are shared by kSlices groups of lanes.
 constexpr int kSlices = 8;
-__global__ __launch_bounds__(32 * kSlices) void extend_combine_short_kernel(ExtendArgs a) {
+constexpr int kShortRows = 1 << 23;  // of a launch, whose threads have to be fewer than 2^32
+__global__ __launch_bounds__(32 * kSlices) void extend_combine_short_kernel(ExtendArgs a, int row0) {
     __shared__ __attribute__((aligned(16))) float part[2][kSlices][kPart];
     const Geom& gm = a.gm;
     const int c4 = (threadIdx.x & 31) * 4, slice = threadIdx.x >> 5, G = gm.G;
-    const int token = blockIdx.x / gm.Hq, head = blockIdx.x - token * gm.Hq, hk = head / G;
+    const int row = row0 + (int)blockIdx.x, token = row / gm.Hq, head = row - token * gm.Hq, hk = head / G;
     const int b = *(const scalar int*)(uintptr_t)(a.token_seq + token);  // of a token that is in no sequence: whatever was there
     const Head head_ = uniform(a.head);
     const bool routed = token_routed(a, token, head);
@@ -1389,8 +1390,11 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     }
     {
         KernelTimer kt("extend_combine", st);
-        if (a.few) hipLaunchKernelGGL(extend_combine_short_kernel, dim3(g.T * g.Hq), dim3(32 * kSlices), 0, st, a);
-        else hipLaunchKernelGGL(extend_combine_kernel, dim3(a.most_tiles, a.tile_rows / kCombineRows), dim3(kThreads), 0, st, a);
+        if (a.few) {
+            const int rows = g.T * g.Hq;
+            for (int row0 = 0; row0 < rows; row0 += kShortRows)
+                hipLaunchKernelGGL(extend_combine_short_kernel, dim3(rows - row0 < kShortRows ? rows - row0 : kShortRows), dim3(32 * kSlices), 0, st, a, row0);
+        } else hipLaunchKernelGGL(extend_combine_kernel, dim3(a.most_tiles, a.tile_rows / kCombineRows), dim3(kThreads), 0, st, a);
     }
     return launch_status();
 }
