@@ -16,10 +16,10 @@
 // Calls in which no sequence has more than 128 rows per KV head make no lists, and with up to 512 KV heads of sequences every workgroup
 // makes the plan for itself (extend_short_kernel, extend_combine_short_kernel): two launches instead of four, 25 us for a token behind 32K.
 //
-// Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 127 (main 118: 5.2
-// TB/s); 16 x 5 behind 32K 107; a token behind 32K 24 (18); 2048 behind 32K 330 (320), 4096 behind 124K 1643 (1577: 1.08 PFLOP/s; 1734 on another;
-// products of 8192 x 8192 matrices reach 1.28 with nothing between them); 1000 beside 31 single ones at 16K 168 (140);
-// 3 x 777 first tokens 61 (37).  Before the main kernel: lists 5 to 11, plan 7 to 15; behind it: sums joined, 6 to 27.
+// Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 126 (main 118: 5.3
+// TB/s); 16 x 5 behind 32K 106; a token behind 32K 24 (18); 2048 behind 32K 338 (331), 4096 behind 124K 1697 (1642: 1.04 PFLOP/s, 1577 to 1734 from
+// card to card; products of 8192 x 8192 matrices reach 1.28 with nothing between them); 128 behind 64K 98; 1000 beside 31 single ones at 16K 169 (142);
+// 3 x 777 first tokens 61 (38).  Before the main kernel: lists 5 to 11, plan 7 to 14; behind it: sums joined, 6 to 27.
 #include "paged.hpp"
 #include "tiles.hpp"
 
@@ -355,7 +355,7 @@ __device__ __forceinline__ bf16x8 v_operand(lds_cptr at, int d, int step) {
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // The row and the 16 bytes of it that a lane loads, of the 4 (e4m3: 8) rows of an instruction.  e4m3: so that a lane's 16 elements become
-// two chunks whose stores, eight lanes at a time, touch every bank once.
+// two chunks whose stores, eight lanes at a time, touch no bank twice.  (Counted: conflicts in 5 to 7 % of the cycles even so; none in bf16.)
 template <bool FP8>
 __device__ __forceinline__ int load_row(int lane) { return FP8 ? ((lane >> 1) & 3) + 4 * (lane >> 5) : (lane >> 2) & 3; }
 template <bool FP8>
@@ -837,7 +837,7 @@ __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__
 
 // A tile by 8 wavefronts of 32 rows, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself and every operand
 // serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one card, at 2.1 GHz and
-// 1.9.  It is the power that bounds both.)
+// 1.9: fewer cycles, at a lower clock.)
 // HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
 static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
