@@ -836,8 +836,8 @@ __device__ __forceinline__ void for_pieces(const ExtendArgs& a, F&& f) {
 __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(lds))) : "memory"); }
 
 // A tile by 8 wavefronts of 32 rows, two on a SIMD.  (4 wavefronts of 64 rows, each with a SIMD and its 512 registers to itself and every operand
-// serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one card, at 2.1 GHz and
-// 1.9: fewer cycles, at a lower clock.)
+// serving two matrix instructions, took as long at 4096 tokens behind 126976: 1732 us and 1730 on one card, at clocks of
+// 2.1 GHz and 1.9: the one that needs fewer cycles gets fewer of them.)
 // HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
 static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
