@@ -139,10 +139,6 @@ class PagedCache:
     def _upload(self, x: np.ndarray) -> torch.Tensor:
         return torch.from_numpy(np.ascontiguousarray(x)).to(self.cache.tensors[4].device)
 
-    def _check(self, b: int):
-        if not 0 <= b < self.p.B:
-            raise IndexError(f"there are sequences 0 .. {self.p.B - 1}; got {b}")
-
     def _check_not_captured(self):
         if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("steps upload their indices from the host and cannot be captured; capture l2a_cache_write and l2a_attn_extend with index "
@@ -208,7 +204,7 @@ class PagedCache:
 
     def read(self, b: int):
         """-> k, v [length, Hkv, D] of sequence b, as bf16."""
-        self._check(b)
+        b = range(self.p.B)[b]  # (-1: the last one)
         self._check_not_captured()
         n = int(self.length[b])
         size = np.where(np.arange(self.p.B) == b, n, 0)
@@ -222,7 +218,7 @@ class PagedCache:
 
     def end(self, b: int):
         """Sequence b is over: its pages are free."""
-        self._check(b)
+        b = range(self.p.B)[b]  # (-1: the last one)
         used = -(-int(self.length[b]) // self.page_size)
         self.free.extend(int(x) for x in self.table[b, :used])
         self.table[b], self.length[b] = -1, 0

@@ -152,14 +152,17 @@ def test_sequences_that_there_are_none_of(calls):
     cache = make()
     step(cache, [20, 3])
     before = held(cache)
-    for b in (-1, -2, 2, 100):
+    for b in (-3, 2, 100):
         with pytest.raises(IndexError):
-            cache.read(b)  # (-1: the last sequence's length, and no sequence's rows)
+            cache.read(b)
         with pytest.raises(IndexError):
             cache.end(b)
     assert held(cache)[0] == before[0] and len(calls.seen) == 2
-    k, v = cache.read(1)
-    assert k.shape == v.shape == (3, HKV, D) and calls.seen[-1][:4] == ("read", 3, [0, 0, 3], [0, 0])
+    for b in (1, -1):  # (the last sequence's length came with no sequence's rows)
+        k, v = cache.read(b)
+        assert k.shape == v.shape == (3, HKV, D) and calls.seen[-1][:4] == ("read", 3, [0, 0, 3], [0, 0])
+    cache.end(-1)
+    assert held(cache)[0] == [20, 0]
 
 
 def test_the_params_given_stay_as_they_are(calls):
