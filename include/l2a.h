@@ -33,6 +33,7 @@
  *   - Return value: 0 on success, a negative L2A_ERR_* otherwise.  On an argument error
  *     nothing is launched and no output is touched.
  *   - Data pointers must be 16-byte aligned.
+ *   - l2a_rope alone takes token strides (l2a_rotary).
  */
 #ifndef L2A_H_
 #define L2A_H_
@@ -44,7 +45,7 @@
 extern "C" {
 #endif
 
-enum { L2A_BF16 = 0, L2A_FP32 = 1, L2A_FP8 = 2 /* elements of an l2a_cache only, see there */ };
+enum { L2A_BF16 = 0, L2A_FP32 = 1, L2A_FP8 = 2, L2A_FP4 = 3 /* the last two: elements of an l2a_cache only, see there */ };
 
 enum {
     L2A_FLAG_DENSE = 1,       /* every token is routed (d = 1 everywhere): the in-house dense causal
@@ -237,16 +238,21 @@ int l2a_attn_decode(const l2a_params* p, const void* q, const void* k_cache, con
  * Serving on a paged KV cache (Sec. 3.4): new tokens of many sequences at once, packed one sequence behind the other -- chunks of
  * prompts, drafts of a few tokens, single tokens, in any mixture.  A step is
  *     l2a_router_decide (B = 1, T = packed tokens)  ->  l2a_cache_write  ->  l2a_attn_extend
- * and l2a_cache_read hands cached rows back (a prefix for l2a_attn_fwd, a sequence that is moved).  bf16, D = 128.
+ * and l2a_cache_read hands cached rows back (a prefix for l2a_attn_fwd, a sequence that is moved).  bf16, D = 128.  Where memory is short,
+ * l2a_cache_weights adds up what attention rows receive and l2a_cache_evict gives up those that received least; l2a_rope comes before all.
  *
  * The cache is a pool of pages of page_size tokens; row r of sequence b is row r mod page_size of page table[b][r / page_size].
- *   k, v              [pages, Hkv, page_size, D] elements: the rows of a KV head in a page lie one behind the other
+ *   k, v              [pages, Hkv, page_size, D] elements (L2A_FP4: D / 2 bytes): the rows of a KV head in a page lie one behind the other
  *   L2A_BF16          bf16 elements
  *   L2A_FP8           e4m3 elements (OCP: no infinities, largest 448) in blocks of 32 channels, each with a power of two of its own:
  *                     k_scale, v_scale [pages, Hkv, page_size, D / 32] uint8 hold its exponent plus 127, and an
  *                     element stands for e4m3 * 2^(byte - 127), which is a bf16 number.  The exponent of a block whose largest
  *                     magnitude is m is the least integer e with m <= 448 * 2^e, clamped into -118..119; elements are rounded to
  *                     nearest, ties to even (magnitudes above 448 * 2^119 become that).  A NaN stays a NaN, an infinity becomes one.  A row takes 132 bytes instead of 256.
+ *   L2A_FP4           e2m1 elements (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives), two a byte, the lower channel in the lower bits, in
+ *                     blocks of 32 channels with k_scale, v_scale as above.  e is the least integer with m <= 6 * 2^e, clamped into
+ *                     -125..125; elements are rounded to nearest, ties to even (magnitudes above 6 * 2^125 become that).  A block with a NaN
+ *                     or an infinity becomes NaN throughout (exponent byte 255).  A row takes 68 bytes.
  *   table             [B, max_pages] int32, device memory.  Entries of pages that a call has no use for may hold anything.
  * The struct is host memory and is read during the call; what it points to is device memory owned by the caller.
  *
@@ -266,17 +272,17 @@ int l2a_attn_decode(const l2a_params* p, const void* q, const void* k_cache, con
  */
 typedef struct l2a_cache {
     void *k, *v;
-    void *k_scale, *v_scale; /* L2A_FP8 only */
+    void *k_scale, *v_scale; /* L2A_FP8 and L2A_FP4 only */
     const int32_t* table;
     int32_t pages;           /* of the pool */
     int32_t page_size;       /* tokens of a page */
     int32_t max_pages;       /* entries of a sequence in the table */
-    int32_t dtype;           /* L2A_BF16 | L2A_FP8 */
+    int32_t dtype;           /* L2A_BF16 | L2A_FP8 | L2A_FP4 */
 } l2a_cache;
 
 /*
  * Cache rows of the packed tokens: written from (l2a_cache_write) or to (l2a_cache_read) k, v [T, Hkv, D] bf16.  Writing rounds
- * an L2A_FP8 cache's elements as above, reading is exact.  Of p: B, T, Hkv, D and dtype count (the other fields must still be
+ * an L2A_FP8 or L2A_FP4 cache's elements as above, reading is exact.  Of p: B, T, Hkv, D and dtype count (the other fields must still be
  * valid).  Two packed tokens with the same place in the pool (two sequences that share a page and both write to it): the
  * row's contents are undefined, no other row is touched.
  */
@@ -314,6 +320,77 @@ size_t l2a_extend_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32
 int l2a_attn_extend(const l2a_params* p, const l2a_cache* c, const void* q, const int32_t* seq_start, const int32_t* pos,
                     const uint8_t* mask, int32_t max_new, void* O, float* lse_local, float* lse_global, void* S_opt,
                     void* A_opt, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The attention weights that cached rows receive from the packed new tokens of a step:
+ *     weight_j = decay * weight_in_j + sum over the G heads of the group and the routed tokens t >= j of exp(scale <q_t, k_j> - lse_global_t),
+ * for every row j up to a sequence's last new token, and for every KV head.  Called behind l2a_attn_extend, whose lse_global it takes: tokens
+ * that are not routed have -inf there, and rows whose log-sum-exp is not finite add nothing (a Local window's weights are not counted: what
+ * it reads is not up for eviction).  K is read once, V not at all.  Sums are fp32, in an order that depends on the call's sizes
+ * and lengths; the same call gives the same bits.  Every KV head's row has a sum of its own: an infinity or a NaN of one key stays with it.
+ *
+ *   q           in  [T,Hq,D]
+ *   lse_global  in  [Hq,T]
+ *   decay       finite, >= 0.  1 adds up, less lets old weights fade, 0 forgets them (weight_in is not read then)
+ *   weight_in   in  [pages, Hkv, page_size] float: the weights so far, laid out as the cache's rows; may be NULL (all zero) and may be
+ *                   `weight`.  Rows of the new tokens begin at zero, whatever it holds there
+ *   weight      out [pages, Hkv, page_size] float.  Rows of sequences without new tokens, rows behind a sequence's last token and pages of nobody are left as
+ *                   they were; of sequences that share pages, the shared rows' weights are undefined
+ *   workspace   l2a_weights_workspace_bytes(p, c, max_new) bytes (0 is possible), as for l2a_attn_extend
+ * seq_start, pos, max_new and values out of range as in l2a_attn_extend (rows in pages outside the pool are skipped).  Errors besides those: L2A_ERR_SHAPE for decay.
+ */
+size_t l2a_weights_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_new);
+int l2a_cache_weights(const l2a_params* p, const l2a_cache* c, const void* q, const int32_t* seq_start, const int32_t* pos,
+                      const float* lse_global, int32_t max_new, float decay, const float* weight_in, float* weight, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction: of the first rows[b] rows of sequence b every KV head keeps the keep[b] of greatest weight, which then are rows 0 .. keep[b] - 1.  Of
+ * equal weights the first row stays; 0 and -0 are equal, NaN is less than everything.  Kept rows before row keep[b] stay where they are; the
+ * i-th place before it that becomes free takes the i-th kept row behind it.  K, V, their exponents and the weights move, bit for bit.  Rows
+ * keep[b] .. rows[b] - 1 are left as they were and stand for nothing any more; rows from rows[b] on are not touched.
+ *   Where rows[b] and keep[b] are multiples of the page size, the caller drops the pages between from the table, and the sequence is rows[b] - keep[b]
+ * rows shorter.  That leaves later rows in order, so that Local windows stay right as long as rows[b] is no larger than the
+ * sequence's length less W.  Global attention does not ask for the order of rows (a new token's row comes behind them all), and rotary positions are in the keys.
+ *
+ *   rows, keep  in  [B] int32, device memory; clamped into 0 .. max_rows (and the table), and 0 .. rows[b]
+ *   max_rows    most rows[b] of this call, at most 2^24
+ *   weight_in   in  [pages, Hkv, page_size] float
+ *   weight      out the same: rows 0 .. keep[b] - 1 are written.  May be weight_in
+ *   kept_opt    out optional [B, Hkv, max_rows] int32: which row each of rows 0 .. keep[b] - 1 was before; entries behind are left as they were
+ *   workspace   l2a_evict_workspace_bytes(p, c, max_rows) bytes
+ * Of p: B, Hkv and D count (the other fields must still be valid).  Rows in pages outside the pool are not moved.  Sequences that share pages must not
+ * be evicted from in one call, nor may one of them while the other still needs them.  Errors as for the other calls; L2A_ERR_SHAPE for max_rows.
+ */
+size_t l2a_evict_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_rows);
+int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows, const int32_t* keep, int32_t max_rows,
+                    const float* weight_in, float* weight, int32_t* kept_opt, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions of q and k, with 1 to 4 axes (a text's position; time, height and width of images and video): pair i of n channel
+ * pairs is turned by the angle pos[axis][token] * freq[i],  (x, y) -> (x cos - y sin, y cos + x sin).  The first pairs[0] pairs belong to
+ * axis 0, the next pairs[1] to axis 1, and so on; n is their sum.  Pair i is channels i and n + i, or 2 i and 2 i + 1 with
+ * L2A_ROTARY_ADJACENT; channels from 2 n on are copied.  L2A_ROTARY_INVERSE turns back, which is the gradient's way too: dq = inverse(d q_out).
+ * For the layer's inputs before l2a_attn_fwd, for new tokens before l2a_cache_write and l2a_attn_extend (B = 1, T = packed tokens), and for
+ * the gradients behind l2a_attn_bwd.  bf16 or fp32; angles are formed in fp64, results are rounded once.
+ *
+ *   q      in  [B,T,Hq,D], k in [B,T,Hkv,D]; either may be NULL.  Heads of a token lie one behind the other, tokens q_stride (k_stride) elements apart
+ *              over all B T, so that both may be parts of the rows of a fused projection; 0: contiguous
+ *   pos    in  [axes, B*T] int32, device memory, any values
+ *   q_out, k_out  out, as q and k; each may be its input (with the same stride).  Other overlaps are not allowed
+ * Errors: L2A_ERR_SHAPE for axes outside 1..4, pairs < 0, n not a positive multiple of 8 or 2 n > D, a stride smaller than a token's row or not a multiple of 16
+ * bytes; L2A_ERR_UNSUPPORTED for unknown flags, in place with two strides.
+ */
+enum { L2A_ROTARY_ADJACENT = 1, L2A_ROTARY_INVERSE = 2 };
+typedef struct l2a_rotary {
+    int32_t axes;
+    int32_t pairs[4];    /* of each axis; entries from `axes` on are ignored */
+    int32_t flags;       /* L2A_ROTARY_* */
+    int32_t q_stride, k_stride, q_out_stride, k_out_stride;
+    const float* freq;   /* [n] device memory: radians per position of each pair */
+} l2a_rotary;
+int l2a_rope(const l2a_params* p, const l2a_rotary* r, const void* q, const void* k, const int32_t* pos, void* q_out, void* k_out,
+             void* stream);
 
 /*
  * Backward (Sec. 3.2: gradients only for the active queries, reusing the saved log-sum-exp

@@ -16,16 +16,18 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libl2a.so")
 
-L2A_BF16, L2A_FP32, L2A_FP8 = 0, 1, 2
+L2A_BF16, L2A_FP32, L2A_FP8, L2A_FP4 = 0, 1, 2, 3
 L2A_FLAG_DENSE, L2A_FLAG_SKIP_LOCAL, L2A_FLAG_SKIP_GLOBAL = 1, 2, 4
 L2A_FLAG_SEQUENTIAL = 8
 L2A_FLAG_RING_CACHE = 16
 L2A_FLAG_SCALAR = 1 << 16
+L2A_ROTARY_ADJACENT, L2A_ROTARY_INVERSE = 1, 2
 
 EXPORTS = ("l2a_version", "l2a_strerror", "l2a_route_workspace_bytes", "l2a_attn_workspace_bytes",
            "l2a_kblk_entries", "l2a_route_compact", "l2a_route_compact_static", "l2a_router_decide", "l2a_attn_fwd", "l2a_attn_bwd",
            "l2a_decode_workspace_bytes", "l2a_attn_decode",
            "l2a_cache_write", "l2a_cache_read", "l2a_extend_workspace_bytes", "l2a_attn_extend",
+           "l2a_weights_workspace_bytes", "l2a_cache_weights", "l2a_evict_workspace_bytes", "l2a_cache_evict", "l2a_rope",
            "l2a_profile_enable", "l2a_profile_read")
 
 
@@ -40,6 +42,12 @@ class l2a_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("table", ctypes.c_void_p), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("dtype", ctypes.c_int32)]
+
+
+class l2a_rotary(ctypes.Structure):
+    """Rotary positions (make_rotary fills one and keeps the frequencies alive)."""
+    _fields_ = [("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4), ("flags", ctypes.c_int32), ("q_stride", ctypes.c_int32),
+                ("k_stride", ctypes.c_int32), ("q_out_stride", ctypes.c_int32), ("k_out_stride", ctypes.c_int32), ("freq", ctypes.c_void_p)]
 
 
 class L2AError(RuntimeError):
@@ -87,6 +95,15 @@ def lib() -> ctypes.CDLL:
         L.l2a_extend_workspace_bytes.argtypes = [pp, cp, ctypes.c_int32]
         L.l2a_attn_extend.restype = ctypes.c_int
         L.l2a_attn_extend.argtypes = [pp, cp] + [vp] * 4 + [ctypes.c_int32] + [vp] * 5 + [vp, ctypes.c_size_t, vp]
+        for f in (L.l2a_weights_workspace_bytes, L.l2a_evict_workspace_bytes):
+            f.restype = ctypes.c_size_t
+            f.argtypes = [pp, cp, ctypes.c_int32]
+        L.l2a_cache_weights.restype = ctypes.c_int
+        L.l2a_cache_weights.argtypes = [pp, cp] + [vp] * 4 + [ctypes.c_int32, ctypes.c_float] + [vp] * 3 + [ctypes.c_size_t, vp]
+        L.l2a_cache_evict.restype = ctypes.c_int
+        L.l2a_cache_evict.argtypes = [pp, cp] + [vp] * 2 + [ctypes.c_int32] + [vp] * 4 + [ctypes.c_size_t, vp]
+        L.l2a_rope.restype = ctypes.c_int
+        L.l2a_rope.argtypes = [pp, ctypes.POINTER(l2a_rotary)] + [vp] * 5 + [vp]
         L.l2a_attn_fwd.restype = ctypes.c_int
         L.l2a_attn_fwd.argtypes = [pp] + [vp] * 6 + [i32p] * 3 + [vp] * 5 + [vp, ctypes.c_size_t, vp]
         L.l2a_attn_bwd.restype = ctypes.c_int
@@ -164,22 +181,23 @@ def l2a_attn_decode(p: l2a_params, q, k_cache, v_cache, pos, mask, O, lse_local=
 
 def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                v_scale: Optional[torch.Tensor] = None) -> l2a_cache:
-    """k, v [pages, Hkv, page_size, 128]: bfloat16, or float8_e4m3fn with k_scale, v_scale [pages, Hkv, page_size, 4] uint8;
-    table [B, max_pages] int32."""
-    fp8 = k.dtype == torch.float8_e4m3fn
-    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or not (fp8 or k.dtype == torch.bfloat16):
-        raise ValueError("k and v must be [pages, Hkv, page_size, 128], both bfloat16 or both float8_e4m3fn")
+    """k, v [pages, Hkv, page_size, 128]: bfloat16, or float8_e4m3fn with k_scale, v_scale [pages, Hkv, page_size, 4] uint8, or with such
+    scales [pages, Hkv, page_size, 64] uint8, two elements of 4 bits a byte; table [B, max_pages] int32."""
+    fp8, fp4 = k.dtype == torch.float8_e4m3fn, k.dtype == torch.uint8
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or not (fp8 or fp4 or k.dtype == torch.bfloat16):
+        raise ValueError("k and v must be [pages, Hkv, page_size, 128], both bfloat16 or both float8_e4m3fn, or [pages, Hkv, page_size, 64], both uint8")
+    D = k.shape[3] * (2 if fp4 else 1)
     for s in (k_scale, v_scale):
-        if (s is None) == fp8 or (fp8 and (s.dtype != torch.uint8 or tuple(s.shape) != tuple(k.shape[:3]) + (k.shape[3] // 32,))):
-            raise ValueError("float8_e4m3fn caches have k_scale and v_scale [pages, Hkv, page_size, 4] uint8, bfloat16 ones have none")
+        if (s is None) == (fp8 or fp4) or (s is not None and (s.dtype != torch.uint8 or tuple(s.shape) != tuple(k.shape[:3]) + (D // 32,))):
+            raise ValueError("float8_e4m3fn and uint8 caches have k_scale and v_scale [pages, Hkv, page_size, 4] uint8, bfloat16 ones have none")
     if table.dim() != 2 or table.dtype != torch.int32:
         raise ValueError("table must be [B, max_pages] int32")
     if len({t.device for t in (k, v, table, k_scale, v_scale) if t is not None}) > 1:
         raise ValueError("a cache's tensors must be on one device")
     c = l2a_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), k.shape[0], k.shape[2], table.shape[1],
-                  L2A_FP8 if fp8 else L2A_BF16)
+                  L2A_FP8 if fp8 else L2A_FP4 if fp4 else L2A_BF16)
     c.tensors = (k, v, k_scale, v_scale, table)
-    c.shape, c.device = (k.shape[1], k.shape[3], table.shape[0]), k.get_device()
+    c.shape, c.device = (k.shape[1], D, table.shape[0]), k.get_device()
     return c
 
 
@@ -193,15 +211,20 @@ def _packed(t: Optional[torch.Tensor], dtype, numel: int, device: int, what: str
     return t.data_ptr()
 
 
-def _begin_packed(p: l2a_params, c: l2a_cache, seq_start, pos):
-    """-> device, its current stream, addresses of seq_start and pos."""
+def _begin_cache(p: l2a_params, c: l2a_cache):
+    """-> device, its current stream."""
     if c.shape != (p.Hkv, p.D, p.B):
         raise ValueError(f"the cache has {c.shape[0]} KV heads of {c.shape[1]} channels and a table of {c.shape[2]} sequences")
     dev = torch.cuda.current_device()
     if c.device != dev:
         raise ValueError("the cache must be on the current device, whose stream the call is enqueued on")
-    return (dev, torch._C._cuda_getCurrentRawStream(dev), _packed(seq_start, torch.int32, p.B + 1, dev, "seq_start"),
-            _packed(pos, torch.int32, p.B, dev, "pos"))
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _begin_packed(p: l2a_params, c: l2a_cache, seq_start, pos):
+    """-> device, its current stream, addresses of seq_start and pos."""
+    dev, stream = _begin_cache(p, c)
+    return dev, stream, _packed(seq_start, torch.int32, p.B + 1, dev, "seq_start"), _packed(pos, torch.int32, p.B, dev, "pos")
 
 
 def l2a_cache_write(p: l2a_params, c: l2a_cache, k, v, seq_start, pos) -> None:
@@ -236,6 +259,80 @@ def l2a_attn_extend(p: l2a_params, c: l2a_cache, q, seq_start, pos, mask, max_ne
                                0 if workspace is None else workspace.numel(), stream)
     if rc != 0:
         raise L2AError(rc, "l2a_attn_extend")
+
+
+def l2a_cache_weights(p: l2a_params, c: l2a_cache, q, seq_start, pos, lse_global, max_new: int, decay: float, weight_in, weight, workspace=None) -> None:
+    """weight_in (None: all zero; may be weight), weight [pages, Hkv, page_size] float32."""
+    dev, stream, s, at = _begin_packed(p, c, seq_start, pos)
+    if workspace is None:
+        workspace = alloc_weights_workspace(p, c, max_new)
+    n = c.pages * p.Hkv * c.page_size
+    rc = lib().l2a_cache_weights(ctypes.byref(p), ctypes.byref(c), _packed(q, torch.bfloat16, p.T * p.Hq * p.D, dev, "q"), s, at,
+                                 _packed(lse_global, torch.float32, p.Hq * p.T, dev, "lse_global"), max_new, decay,
+                                 _packed(weight_in, torch.float32, n, dev, "weight_in"), _packed(weight, torch.float32, n, dev, "weight"),
+                                 None if workspace is None else _packed(workspace, torch.uint8, workspace.numel(), dev, "workspace"),
+                                 0 if workspace is None else workspace.numel(), stream)
+    if rc != 0:
+        raise L2AError(rc, "l2a_cache_weights")
+
+
+def l2a_cache_evict(p: l2a_params, c: l2a_cache, rows, keep, max_rows: int, weight_in, weight, kept=None, workspace=None) -> None:
+    """rows, keep [B] int32; weight_in, weight (may be the same) [pages, Hkv, page_size] float32; kept [B, Hkv, max_rows] int32."""
+    dev, stream = _begin_cache(p, c)
+    if workspace is None:
+        workspace = alloc_evict_workspace(p, c, max_rows)
+    n = c.pages * p.Hkv * c.page_size
+    rc = lib().l2a_cache_evict(ctypes.byref(p), ctypes.byref(c), _packed(rows, torch.int32, p.B, dev, "rows"), _packed(keep, torch.int32, p.B, dev, "keep"),
+                               max_rows, _packed(weight_in, torch.float32, n, dev, "weight_in"), _packed(weight, torch.float32, n, dev, "weight"),
+                               _packed(kept, torch.int32, p.B * p.Hkv * max_rows, dev, "kept"),
+                               None if workspace is None else _packed(workspace, torch.uint8, workspace.numel(), dev, "workspace"),
+                               0 if workspace is None else workspace.numel(), stream)
+    if rc != 0:
+        raise L2AError(rc, "l2a_cache_evict")
+
+
+def make_rotary(freq: torch.Tensor, pairs, adjacent: bool = False, inverse: bool = False) -> l2a_rotary:
+    """freq [n] float32: radians per position of each channel pair; pairs: how many of them each axis turns, up to 4 axes, n in all.  inverse: turns
+    back, as gradients go."""
+    pairs = [int(x) for x in pairs]
+    if freq.dim() != 1 or freq.dtype != torch.float32 or not 1 <= len(pairs) <= 4 or sum(pairs) != freq.numel():
+        raise ValueError("freq must be [n] float32, with the pairs of 1 to 4 axes adding up to n")
+    r = l2a_rotary(len(pairs), (ctypes.c_int32 * 4)(*pairs), (L2A_ROTARY_ADJACENT if adjacent else 0) | (L2A_ROTARY_INVERSE if inverse else 0), 0, 0, 0, 0, _ptr(freq))
+    r.tensors, r.device = (freq,), freq.get_device()
+    return r
+
+
+def _token_rows(t: Optional[torch.Tensor], p: l2a_params, heads: int, device: int, what: str):
+    """-> address and token stride in elements of a tensor [B, T, heads, D] or [B T, heads, D] whose heads lie one behind the other."""
+    if t is None:
+        return None, 0
+    tokens = p.B * p.T
+    ok = t.dtype == torch_dtype(p) and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, p.D) and t.shape[0] == (tokens if t.dim() == 3 else p.B)
+    ok = ok and (t.dim() == 3 or t.shape[1] == p.T) and t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == p.D)
+    if ok:
+        stride = heads * p.D if tokens == 1 else t.stride(-3) if t.dim() == 3 or p.T > 1 else t.stride(0)
+        ok = heads * p.D <= stride < 2 ** 31 and (t.dim() == 3 or p.B == 1 or p.T == 1 or t.stride(0) == p.T * stride)
+    if not ok:
+        raise ValueError(f"{what} must be [{p.B}, {p.T}, {heads}, {p.D}] or [{tokens}, {heads}, {p.D}] {torch_dtype(p)} on the current device, with one stride from "
+                         f"token to token and the heads of a token one behind the other; got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+    return t.data_ptr(), stride
+
+
+def l2a_rope(p: l2a_params, r: l2a_rotary, q, k, pos, q_out, k_out) -> None:
+    """q, q_out [B, T, Hq, D], k, k_out [B, T, Hkv, D] (or [B T, ..]; views into rows of a fused projection are fine; q or k may be None); pos [axes, B, T]
+    int32.  In place: q_out = q, k_out = k."""
+    dev = torch.cuda.current_device()
+    if r.device != dev:
+        raise ValueError("the frequencies must be on the current device, whose stream the call is enqueued on")
+    call = l2a_rotary.from_buffer_copy(r)
+    q_at, call.q_stride = _token_rows(q, p, p.Hq, dev, "q")
+    k_at, call.k_stride = _token_rows(k, p, p.Hkv, dev, "k")
+    qo_at, call.q_out_stride = _token_rows(q_out, p, p.Hq, dev, "q_out")
+    ko_at, call.k_out_stride = _token_rows(k_out, p, p.Hkv, dev, "k_out")
+    rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(call), q_at, k_at, _packed(pos, torch.int32, r.axes * p.B * p.T, dev, "pos"), qo_at, ko_at,
+                        torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        raise L2AError(rc, "l2a_rope")
 
 
 def l2a_attn_fwd(p: l2a_params, q_loc, k_loc, v_loc, q_glb, k_glb, v_glb, row_idx, count, kblk_first_row, O,
@@ -314,12 +411,22 @@ def alloc_extend_workspace(p: l2a_params, c: l2a_cache, max_new: int, alloc=None
     return _ws(lib().l2a_extend_workspace_bytes(ctypes.byref(p), ctypes.byref(c), max_new), c.tensors[0].device, alloc)
 
 
-def alloc_cache(p: l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", alloc=None) -> l2a_cache:
+def alloc_weights_workspace(p: l2a_params, c: l2a_cache, max_new: int, alloc=None):
+    return _ws(lib().l2a_weights_workspace_bytes(ctypes.byref(p), ctypes.byref(c), max_new), c.tensors[0].device, alloc)
+
+
+def alloc_evict_workspace(p: l2a_params, c: l2a_cache, max_rows: int, alloc=None):
+    return _ws(lib().l2a_evict_workspace_bytes(ctypes.byref(p), ctypes.byref(c), max_rows), c.tensors[0].device, alloc)
+
+
+def alloc_cache(p: l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", alloc=None, fp4: bool = False) -> l2a_cache:
     """A pool of pages and an empty table (all entries -1)."""
+    if fp8 and fp4:
+        raise ValueError("a cache's elements have 8 bits or 4")
     e = alloc or torch.empty
-    shape = (pages, p.Hkv, page_size, p.D)
-    k, v = (e(shape, dtype=torch.float8_e4m3fn if fp8 else torch.bfloat16, device=device) for _ in range(2))
-    ks, vs = (e(shape[:3] + (p.D // 32,), dtype=torch.uint8, device=device) if fp8 else None for _ in range(2))
+    shape = (pages, p.Hkv, page_size, p.D // 2 if fp4 else p.D)
+    k, v = (e(shape, dtype=torch.float8_e4m3fn if fp8 else torch.uint8 if fp4 else torch.bfloat16, device=device) for _ in range(2))
+    ks, vs = (e(shape[:3] + (p.D // 32,), dtype=torch.uint8, device=device) if fp8 or fp4 else None for _ in range(2))
     return make_cache(k, v, e((p.B, max_pages), dtype=torch.int32, device=device).fill_(-1), ks, vs)
 
 

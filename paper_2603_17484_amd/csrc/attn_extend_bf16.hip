@@ -92,7 +92,7 @@ __device__ __forceinline__ bool token_routed(const ExtendArgs& a, int token, int
     const int mh = a.mask_heads == 1 ? 0 : (a.mask_heads == a.gm.Hq ? head : head / a.gm.G);
     return a.mask[(size_t)mh * a.gm.T + token] != 0;
 }
-__device__ __forceinline__ Place place_of(const ExtendArgs& a, const Tile& t) { return Place{t.start, t.blocks, plan::block_cost(t.rows, a.c.fp8)}; }
+__device__ __forceinline__ Place place_of(const ExtendArgs& a, const Tile& t) { return Place{t.start, t.blocks, plan::block_cost(t.rows, a.c.bits < 16)}; }
 // The decisions of a token for the heads of a KV head's group, a bit each.
 __device__ __forceinline__ unsigned group_routed(const ExtendArgs& a, int token, int hk) {
     const int G = a.gm.G;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
         tiles = min(tiles + here, a.most_tiles);
         __syncthreads();
     }
-    const int dearest = plan::block_cost(a.tile_rows, a.c.fp8);
+    const int dearest = plan::block_cost(a.tile_rows, a.c.bits < 16);
     int per = plan::stretch(line, a.workgroups, dearest), segments = 0;
     const int segment = plan::segment_blocks(per, dearest);
     if (!a.few && a.do_global && segment) {
@@ -354,32 +354,42 @@ __device__ __forceinline__ bf16x8 v_operand(lds_cptr at, int d, int step) {
     const s16x4 v2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + d * 256 + (step * 4 + 2) * kFour));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// The row and the 16 bytes of it that a lane loads, of the 4 (e4m3: 8) rows of an instruction.  e4m3: so that a lane's 16 elements become
-// two chunks whose stores, eight lanes at a time, touch no bank twice.  (Counted: conflicts in 5 to 7 % of the cycles even so; none in bf16.)
-template <bool FP8>
-__device__ __forceinline__ int load_row(int lane) { return FP8 ? ((lane >> 1) & 3) + 4 * (lane >> 5) : (lane >> 2) & 3; }
-template <bool FP8>
-__device__ __forceinline__ int load_chunk(int lane) { return FP8 ? (lane & 1) + 2 * ((lane >> 3) & 3) : (lane >> 4) * 4 + (lane & 3); }
-// e4m3: a lane's 16 elements of `row`, with the exponents of the row, become bf16
+// The row and the 16 bytes of it that a lane loads, of the 4 (e4m3: 8, e2m1: 16) rows of an instruction.  Elements of fewer bits: so that a
+// lane's 16 or 32 become two or four chunks whose stores, eight lanes at a time, touch no bank twice.  (Counted: conflicts in 5 to 7 % of the cycles
+// even so in e4m3; none in bf16.)
+template <int BITS>
+__device__ __forceinline__ int load_row(int lane) {
+    if constexpr (BITS == 4) return (lane & 1) + 4 * ((lane >> 1) & 3) + 2 * ((lane >> 3) & 1);
+    return BITS == 8 ? ((lane >> 1) & 3) + 4 * (lane >> 5) : (lane >> 2) & 3;
+}
+template <int BITS>
+__device__ __forceinline__ int load_chunk(int lane) {
+    if constexpr (BITS == 4) return lane >> 4;
+    return BITS == 8 ? (lane & 1) + 2 * ((lane >> 3) & 3) : (lane >> 4) * 4 + (lane & 3);
+}
+// e4m3, e2m1: a lane's 16 bytes of `row`, with the exponents of the row, become bf16
 typedef __attribute__((address_space(3))) char* lds_ptr;
+template <int BITS>
 __device__ __forceinline__ void store_converted(const u32x4& x, uint32_t exponents, lds_ptr block, int row, int lane) {
-    const int c = load_chunk<true>(lane);
-    u32x4 y[2];
-    dequantise16(x, exponent_value((exponents >> (8 * (c >> 1))) & 0xffu), y);
-    __attribute__((address_space(3))) u32x4* const at = (__attribute__((address_space(3))) u32x4*)(block + chunk_at(row, 2 * c));
-    at[0] = y[0], at[1] = y[1];
+    constexpr int kChunks = 16 / BITS;
+    const int c = load_chunk<BITS>(lane), scale = c * kChunks / 4;
+    u32x4 y[kChunks];
+    dequantise<BITS>(x, exponent_value((exponents >> (8 * scale)) & 0xffu), y);
+    __attribute__((address_space(3))) u32x4* const at = (__attribute__((address_space(3))) u32x4*)(block + chunk_at(row, kChunks * c));
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) at[i] = y[i];
 }
 
-// Shared memory of a workgroup of NW wavefronts, in bytes from its beginning: rings of blocks of K and of V; e4m3: rings of what was loaded
+// Shared memory of a workgroup of NW wavefronts, in bytes from its beginning: rings of blocks of K and of V; e4m3, e2m1: rings of what was loaded
 // (K, V, their exponents: every wavefront's pieces its own, which it alone converts) and of the bf16 blocks made of it.  Blocks are
 // loaded two walks of the loop ahead of their use.
-template <bool FP8, int NW>
+template <int BITS, int NW>
 struct Lds {
-    static constexpr int kK = FP8 ? 3 : 4, kV = FP8 ? 3 : 4, kRaw = 2;
+    static constexpr int kK = BITS < 16 ? 3 : 4, kV = BITS < 16 ? 3 : 4, kRaw = 2;
     static constexpr unsigned k = 0, v = k + kK * kBlockBytes, raw_k = v + kV * kBlockBytes;
-    static constexpr unsigned kRawBlock = kKeys * kD, kRawScales = kKeys / 8 * 256;
+    static constexpr unsigned kRawBlock = kKeys * kD * BITS / 8, kRawScales = kKeys * BITS / 64 * 256;
     static constexpr unsigned raw_v = raw_k + kRaw * kRawBlock, raw_ks = raw_v + kRaw * kRawBlock, raw_vs = raw_ks + kRaw * kRawScales;
-    static constexpr unsigned used = FP8 ? raw_vs + kRaw * kRawScales : raw_k;
+    static constexpr unsigned used = BITS < 16 ? raw_vs + kRaw * kRawScales : raw_k;
 };
 // A place in a ring of `of` blocks of `each` bytes that begins at `first`, moved on.
 __device__ __forceinline__ unsigned next(unsigned at, unsigned first, unsigned each, int of) {
@@ -403,70 +413,77 @@ __device__ __forceinline__ X uniform(const X* p) {
 
 // The blocks of a piece on their way to LDS.  Block i + 1 of K and block i of V go together (group i): a block's scores are computed
 // before the block ahead of it is multiplied with V.  A wavefront loads its share of every block, 16 rows or 8, which lie in one page.
-template <bool FP8, int NW>
+// e2m1: an instruction takes 16 rows, more than an eighth of a block, so that one half of the wavefronts loads (and converts) K, the other V.
+template <int BITS, int NW>
 struct Loader {
-    typedef Lds<FP8, NW> L;
-    static constexpr int kRowBytes = FP8 ? kD : kD * 2;
-    static constexpr int kShare = kKeys / NW, kRows = FP8 ? 8 : 4, kEach = kShare / kRows;  // rows of a wavefront, of an instruction; instructions
-    static constexpr int kHalf = kEach * (FP8 ? 2 : 1);  // instructions for K (e4m3: elements and exponents), and for V
-    static constexpr unsigned kApart = FP8 ? 1024 : kFour;  // what the instructions' rows are apart in LDS
+    typedef Lds<BITS, NW> L;
+    static constexpr bool kRoles = BITS == 4;
+    static constexpr int kParts = kRoles ? NW / 2 : NW;
+    static constexpr int kRowBytes = kD * BITS / 8;
+    static constexpr int kShare = kKeys / kParts, kRows = 64 / BITS, kEach = kShare / kRows;  // rows of a wavefront, of an instruction; instructions
+    static_assert(kEach >= 1 && kShare <= 16, "whole instructions, whose rows lie in one page");
+    static constexpr int kHalf = kEach * (BITS < 16 ? 2 : 1);  // instructions for K (with scales: elements and exponents), and for V
+    static constexpr unsigned kApart = BITS < 16 ? 1024 : kFour;  // what the instructions' rows are apart in LDS
     const ExtendArgs& a;
     const scalar int32_t* table;
     int hk, lo, hi, jb0, blocks;  // keys lo .. hi may be read; blocks jb0 .. jb0 + blocks - 1
     int wave, lane;
     int issued;                   // last group issued
+    __device__ __forceinline__ int part() const { return kRoles ? wave & (kParts - 1) : wave; }  // of every block's rows
+    __device__ __forceinline__ bool takes_k() const { return !kRoles || wave < kParts; }
+    __device__ __forceinline__ bool takes_v() const { return !kRoles || wave >= kParts; }
     unsigned k_to, v_to, ks_to, vs_to;  // where the next K and V go
     // the next group's K and V: the row of the pool where this wavefront's begin, and how many bytes behind that this lane's are
     size_t row_k, row_v;
     unsigned off_k[kHalf], off_v[kHalf];
 
-    __device__ __forceinline__ unsigned k0() const { return (FP8 ? L::raw_k : L::k) + wave * kEach * kApart; }
-    __device__ __forceinline__ unsigned v0() const { return (FP8 ? L::raw_v : L::v) + wave * kEach * kApart; }
+    __device__ __forceinline__ unsigned k0() const { return (BITS < 16 ? L::raw_k : L::k) + part() * kEach * kApart; }
+    __device__ __forceinline__ unsigned v0() const { return (BITS < 16 ? L::raw_v : L::v) + part() * kEach * kApart; }
     __device__ __forceinline__ void start() {
         issued = -2;
         k_to = k0(), v_to = v0();
-        ks_to = L::raw_ks + wave * kEach * 256, vs_to = L::raw_vs + wave * kEach * 256;
+        ks_to = L::raw_ks + part() * kEach * 256, vs_to = L::raw_vs + part() * kEach * 256;
         find(0);
     }
     // Keys out of lo .. hi (before the first row's window: their pages may have been given back; behind the last row: not written yet)
     // repeat the nearest key inside: always masked, and what lies in such rows must not meet a zero weight.
     __device__ __forceinline__ void find(int block) {
-        const int key = (jb0 + block) * kKeys + wave * kShare, first = plan::clamp(key, lo & -kShare, hi & -kShare);
+        const int key = (jb0 + block) * kKeys + part() * kShare, first = plan::clamp(key, lo & -kShare, hi & -kShare);
         row_k = pool_row(a.c, a.gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), hk, first);
         int mine[kEach];  // rows behind the first
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) mine[e] = e * kRows + load_row<FP8>(lane);
+        for (int e = 0; e < kEach; ++e) mine[e] = e * kRows + load_row<BITS>(lane);
         if (key < lo || key + kShare - 1 > hi) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) mine[e] = plan::clamp(key + mine[e], lo, hi) - first;
         }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            off_k[e] = mine[e] * kRowBytes + load_chunk<FP8>(lane) * 16;
-            if (FP8) off_k[kHalf - kEach + e] = mine[e] * kRowScales;
+            off_k[e] = mine[e] * kRowBytes + load_chunk<BITS>(lane) * 16;
+            if (BITS < 16) off_k[kHalf - kEach + e] = mine[e] * kRowScales;
         }
     }
     // The next group, as far as there is one: its instructions one by one (K's, then V's), then what comes after it.
     __device__ __forceinline__ bool has_k() const { return issued + 2 < blocks; }
     __device__ __forceinline__ bool has_v() const { return issued + 1 >= 0 && issued + 1 < blocks; }
     __device__ __forceinline__ void issue_one(const char* pool, const unsigned char* scales, size_t row, const unsigned* off, unsigned to, unsigned scales_to, int e) const {
-        if (!FP8 || e < kEach) dma16_so(pool + row * kRowBytes, off[e], to + e * kApart);
+        if (BITS == 16 || e < kEach) dma16_so(pool + row * kRowBytes, off[e], to + e * kApart);
         else dma4_so(scales + row * kRowScales, off[e], scales_to + (e - kEach) * 256);
     }
     __device__ __forceinline__ void issue_k(int e) const {
-        if (has_k()) issue_one(a.c.k, a.c.ks, row_k, off_k, k_to, ks_to, e);
+        if (takes_k() && has_k()) issue_one(a.c.k, a.c.ks, row_k, off_k, k_to, ks_to, e);
     }
     __device__ __forceinline__ void issue_v(int e) const {
-        if (has_v()) issue_one(a.c.v, a.c.vs, row_v, off_v, v_to, vs_to, e);
+        if (takes_v() && has_v()) issue_one(a.c.v, a.c.vs, row_v, off_v, v_to, vs_to, e);
     }
     __device__ __forceinline__ void advance() {
         const int i = ++issued;
         if (i >= 0) {
-            v_to = next(v_to, v0(), FP8 ? L::kRawBlock : kBlockBytes, FP8 ? L::kRaw : L::kV);
-            if (FP8) vs_to = next(vs_to, L::raw_vs + wave * kEach * 256, L::kRawScales, L::kRaw);
+            v_to = next(v_to, v0(), BITS < 16 ? L::kRawBlock : kBlockBytes, BITS < 16 ? L::kRaw : L::kV);
+            if (BITS < 16) vs_to = next(vs_to, L::raw_vs + part() * kEach * 256, L::kRawScales, L::kRaw);
         }
-        k_to = next(k_to, k0(), FP8 ? L::kRawBlock : kBlockBytes, FP8 ? L::kRaw : L::kK);
-        if (FP8) ks_to = next(ks_to, L::raw_ks + wave * kEach * 256, L::kRawScales, L::kRaw);
+        k_to = next(k_to, k0(), BITS < 16 ? L::kRawBlock : kBlockBytes, BITS < 16 ? L::kRaw : L::kK);
+        if (BITS < 16) ks_to = next(ks_to, L::raw_ks + part() * kEach * 256, L::kRawScales, L::kRaw);
         row_v = row_k;
 #pragma unroll
         for (int e = 0; e < kHalf; ++e) off_v[e] = off_k[e];
@@ -481,25 +498,34 @@ struct Loader {
     }
     // Waits until at most the last group is on its way; those at the end have half their loads or none.
     __device__ __forceinline__ void wait() const {
-        if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kHalf) : "memory");
+        if constexpr (kRoles) {
+            if (takes_k() ? issued + 1 < blocks : issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalf) : "memory");
+            else dma_wait();
+        } else if (issued + 1 < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kHalf) : "memory");
         else if (issued < blocks) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalf) : "memory");
         else dma_wait();
     }
-    // e4m3: this wavefront's pieces of a loaded block (the slot-th of the ring) become bf16.
+    // e4m3, e2m1: this wavefront's pieces of a loaded block (the slot-th of the ring) become bf16.
     struct Raw {
         u32x4 x;
         uint32_t exponents;
     };
     __device__ __forceinline__ Raw raw_piece(unsigned raw, unsigned raw_scales, int slot, int e) const {
-        return Raw{*(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(raw + slot * L::kRawBlock + (wave * kEach + e) * 1024 + lane * 16),
-                   *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)(raw_scales + slot * L::kRawScales + (wave * kEach + e) * 256 + lane * 4)};
+        return Raw{*(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(raw + slot * L::kRawBlock + (part() * kEach + e) * 1024 + lane * 16),
+                   *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)(raw_scales + slot * L::kRawScales + (part() * kEach + e) * 256 + lane * 4)};
     }
     __device__ __forceinline__ void store_piece(const Raw& r, unsigned block, int e) const {
-        store_converted(r.x, r.exponents, (lds_ptr)(uintptr_t)block, wave * kShare + e * kRows + load_row<true>(lane), lane);
+        store_converted<BITS>(r.x, r.exponents, (lds_ptr)(uintptr_t)block, part() * kShare + e * kRows + load_row<BITS>(lane), lane);
     }
     __device__ __forceinline__ void convert(unsigned raw, unsigned raw_scales, int slot, unsigned block) const {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) store_piece(raw_piece(raw, raw_scales, slot, e), block, e);
+    }
+    __device__ __forceinline__ void convert_k(int slot, unsigned block) const {
+        if (takes_k()) convert(L::raw_k, L::raw_ks, slot, block);
+    }
+    __device__ __forceinline__ void convert_v(int slot, unsigned block) const {
+        if (takes_v()) convert(L::raw_v, L::raw_vs, slot, block);
     }
 };
 
@@ -603,9 +629,14 @@ __device__ __forceinline__ void rows_alone(const ExtendArgs& a, const Tile& t, c
     const int32_t* const table = a.c.table + (size_t)t.b * a.c.max_pages;
     const int b0 = (t.lo / kKeys + t.skip + piece.from) * kKeys, b1 = (t.lo / kKeys + t.skip + piece.to) * kKeys - 1;
     auto values = [&](const char* pool, const unsigned char* scales, size_t row) __attribute__((always_inline)) {
-        if (!a.c.fp8) return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(pool + row * (kD * 2) + c4 * 2), f32x4);
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(pool + row * kD + c4);
+        if (a.c.bits == 16) return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(pool + row * (kD * 2) + c4 * 2), f32x4);
         const float e = exponent_value(scales[row * kRowScales + c4 / kScaleBlock]);
+        if (a.c.bits == 4) {
+            const uint32_t x = *reinterpret_cast<const uint16_t*>(pool + row * (kD / 2) + c4 / 2);
+            const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 0)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 1));
+            return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
+        }
+        const uint32_t x = *reinterpret_cast<const uint32_t*>(pool + row * kD + c4);
         const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, false)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, true));
         return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
     };
@@ -642,7 +673,7 @@ template <int NW>
 struct FewLds {
     static constexpr unsigned block = kSub / 4 * kFour, keys = NW * 2 * block, sums = NW * 32 * kPart * 4, votes = keys > sums ? keys : sums, used = votes + 64;
 };
-template <bool FP8, int NW>
+template <int BITS, int NW>
 __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -657,10 +688,10 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     __syncthreads();  // LDS is free
     const unsigned k_to = wave * 2 * FewLds<NW>::block, v_to = k_to + FewLds<NW>::block;
     const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
-    constexpr int kRows = FP8 ? 8 : 4, kEach = kSub / kRows;  // rows of an instruction, which lie in one page; instructions
-    const int mine = load_row<FP8>(lane);
-    u32x4 kx[FP8 ? kEach : 1], vx[FP8 ? kEach : 1];
-    uint32_t kse[FP8 ? kEach : 1], vse[FP8 ? kEach : 1];
+    constexpr int kRows = 64 / BITS, kEach = kSub / kRows, kRowBytes = kD * BITS / 8;  // rows of an instruction, which lie in one page; instructions
+    const int mine = load_row<BITS>(lane);
+    u32x4 kx[BITS < 16 ? kEach : 1], vx[BITS < 16 ? kEach : 1];
+    uint32_t kse[BITS < 16 ? kEach : 1], vse[BITS < 16 ? kEach : 1];
     size_t rows[kEach];   // where the instructions' rows begin in the pool, and how far behind that this lane's row is
     unsigned off[kEach];
     // keys out of the tile's repeat the nearest one in it (see Loader)
@@ -685,17 +716,17 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     auto load = [&](const char* pool, const unsigned char* scales, u32x4* x, uint32_t* se, unsigned to) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            if constexpr (!FP8) {
-                dma16_so(pool + rows[e] * (kD * 2), off[e] * (kD * 2) + load_chunk<FP8>(lane) * 16, to + e * kFour);
+            if constexpr (BITS == 16) {
+                dma16_so(pool + rows[e] * kRowBytes, off[e] * kRowBytes + load_chunk<BITS>(lane) * 16, to + e * kFour);
             } else {
-                x[e] = *reinterpret_cast<const u32x4*>(pool + rows[e] * kD + off[e] * kD + load_chunk<FP8>(lane) * 16);
+                x[e] = *reinterpret_cast<const u32x4*>(pool + rows[e] * kRowBytes + off[e] * kRowBytes + load_chunk<BITS>(lane) * 16);
                 se[e] = *reinterpret_cast<const uint32_t*>(scales + rows[e] * kRowScales + off[e] * kRowScales);
             }
         }
     };
     auto convert = [&](const u32x4* x, const uint32_t* se, unsigned block) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) store_converted(x[e], se[e], (lds_ptr)(uintptr_t)block, e * kRows + mine, lane);
+        for (int e = 0; e < kEach; ++e) store_converted<BITS>(x[e], se[e], (lds_ptr)(uintptr_t)block, e * kRows + mine, lane);
     };
     if (sb0 < sb1) {
         find(sb0);
@@ -719,19 +750,19 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     for (int sb = sb0; sb < sb1; sb += NW) {
         const bool more = sb + NW < sb1;
         if (more) find(sb + NW);
-        if constexpr (FP8) convert(kx, kse, k_to);
+        if constexpr (BITS < 16) convert(kx, kse, k_to);
         else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
         bf16x8 op[8];
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) op[ks] = k_operand(k_at, ks, 0);
-        if constexpr (FP8) {
+        if constexpr (BITS < 16) {
             if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
         }
         FENCE();
         f32x16 sc;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) sc = mfma32(op[ks], qreg[ks], ks == 0 ? zero16 : sc);
-        if constexpr (!FP8) {
+        if constexpr (BITS == 16) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of K have returned
             if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
             if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
@@ -758,7 +789,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
             row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
             p[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pb);
         }
-        if constexpr (!FP8) {
+        if constexpr (BITS == 16) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of V have returned
             if (more) load(a.c.v, a.c.vs, vx, vse, v_to);
         }
@@ -841,15 +872,15 @@ __device__ __forceinline__ void by_address(char* lds) { asm volatile("" ::"s"(__
 // HALVES, up to 128 rows: wavefronts 4 .. 7 take the second half of the keys of every block for the rows of wavefronts 0 .. 3.
 constexpr int kWaves = 8, kHalvesRows = 32 * kWaves / 2;
 static_assert(kHalvesRows == plan::kManyRows && kSub == plan::kFewRows, "costs and kernels agree on what are few rows, and many");
-template <bool FP8>
+template <int BITS>
 struct TileLds {
-    static constexpr unsigned many = Lds<FP8, kWaves>::used + 64, used = many > FewLds<kWaves>::used ? many : FewLds<kWaves>::used;  // (64: votes)
+    static constexpr unsigned many = Lds<BITS, kWaves>::used + 64, used = many > FewLds<kWaves>::used ? many : FewLds<kWaves>::used;  // (64: votes)
     // behind these, half a block of V that is zero, for extend_kernel: what the first of a tile's products has beside weights of zero
     static constexpr unsigned zeros = used, kZeros = kKeys / 8 * kFour;
 };
-template <bool FP8, bool HALVES>
+template <int BITS, bool HALVES>
 __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
-    typedef Lds<FP8, kWaves> L;
+    typedef Lds<BITS, kWaves> L;
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5, G = gm.G;
@@ -860,7 +891,7 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
     const int hk = t.hk, jb0 = t.lo / kKeys + t.skip + piece.from, blocks = piece.to - piece.from;
     const Seq s = t.s;
     __syncthreads();  // LDS is free
-    Loader<FP8, kWaves> load{a, (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
+    Loader<BITS, kWaves> load{a, (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages), hk, t.lo, t.hi, jb0, blocks, wave, lane};
     load.start();
     load.issue();
     load.issue();
@@ -894,14 +925,14 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
     unsigned kb = L::k, vb = L::v;  // block j
     auto next_k = [&]() __attribute__((always_inline)) { return next(kb, L::k, kBlockBytes, L::kK); };
     auto next_v = [&]() __attribute__((always_inline)) { return next(vb, L::v, kBlockBytes, L::kV); };
-    if constexpr (FP8) {
+    if constexpr (BITS < 16) {
         load.wait();
-        load.convert(L::raw_k, L::raw_ks, 0, L::k);
+        load.convert_k(0, L::k);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         load.issue();
         load.wait();
-        if (blocks > 1) load.convert(L::raw_k, L::raw_ks, 1, L::k + kBlockBytes);
-        load.convert(L::raw_v, L::raw_vs, 0, L::v);
+        if (blocks > 1) load.convert_k(1, L::k + kBlockBytes);
+        load.convert_v(0, L::v);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         load.issue();
     } else {
@@ -909,20 +940,20 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
         load.wait();
     }
     __syncthreads();
-    // begins a block's work: more on its way, and e4m3 of the next group made bf16
+    // begins a block's work: more on its way, and e4m3 or e2m1 of the next group made bf16
     auto begin = [&](int j) __attribute__((always_inline)) {
-        if constexpr (FP8) {
+        if constexpr (BITS < 16) {
             if (j + 1 < blocks) {
                 load.wait();
-                if (j + 2 < blocks) load.convert(L::raw_k, L::raw_ks, j & 1, next(next_k(), L::k, kBlockBytes, L::kK));
-                load.convert(L::raw_v, L::raw_vs, (j + 1) & 1, next_v());
+                if (j + 2 < blocks) load.convert_k(j & 1, next(next_k(), L::k, kBlockBytes, L::kK));
+                load.convert_v((j + 1) & 1, next_v());
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
         }
         load.issue();
     };
     auto end = [&](int j) __attribute__((always_inline)) {
-        if constexpr (!FP8) load.wait();
+        if constexpr (BITS == 16) load.wait();
         __syncthreads();
         kb = next_k(), vb = next_v();
     };
@@ -1010,7 +1041,7 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
         if (masked(jb0)) mask(sa, jb0 * kKeys);
         mx = largest(sa) * c2;
         // before the first step: weights of zero, and values of zero beside them (an infinity among the piece's own would be a NaN in all rows)
-        lds_cptr va = v_block(TileLds<FP8>::zeros - kKeys / 8 * kFour);  // its second half is what that step reads
+        lds_cptr va = v_block(TileLds<BITS>::zeros - kKeys / 8 * kFour);  // its second half is what that step reads
         pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};
         for (int j = 0; j < blocks; ++j) {
             const int jb = jb0 + j;
@@ -1063,18 +1094,18 @@ __device__ __forceinline__ bool some_rows(const ExtendArgs& a, char* lds, const 
     return true;
 }
 
-template <bool FP8>
+template <int BITS>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
-    typedef TileLds<FP8> L;
+    typedef TileLds<BITS> L;
     __shared__ __attribute__((aligned(1024))) char lds[L::zeros + L::kZeros];
     by_address(lds);
     for (unsigned at = L::zeros + threadIdx.x * 16; at < L::zeros + L::kZeros; at += 64 * kWaves * 16)  // (every tile begins with a barrier)
         *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = u32x4{0u, 0u, 0u, 0u};
     for_pieces(a, [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
         bool done;
-        if (t.rows <= kSub) done = few_rows<FP8, kWaves>(a, lds, t, piece, w);
-        else if (t.rows <= kHalvesRows) done = some_rows<FP8, true>(a, lds, t, piece, w);
-        else done = some_rows<FP8, false>(a, lds, t, piece, w);
+        if (t.rows <= kSub) done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
+        else if (t.rows <= kHalvesRows) done = some_rows<BITS, true>(a, lds, t, piece, w);
+        else done = some_rows<BITS, false>(a, lds, t, piece, w);
         if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
     });
 }
@@ -1088,15 +1119,15 @@ struct ShortPlan {
     Seq seq[kShortPairs];
     int sums[kWaves], first;
 };
-template <bool FP8, bool FEW, bool SELF>
+template <int BITS, bool FEW, bool SELF>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs a) {
-    constexpr unsigned kLds = FEW ? FewLds<kWaves>::used : TileLds<FP8>::used;
+    constexpr unsigned kLds = FEW ? FewLds<kWaves>::used : TileLds<BITS>::used;
     __shared__ __attribute__((aligned(1024))) char lds[kLds + (SELF ? sizeof(ShortPlan) : 0)];
     by_address(lds);
     auto rows = [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
         bool done;
-        if (FEW || t.rows <= kSub) done = few_rows<FP8, kWaves>(a, lds, t, piece, w);
-        else done = some_rows<FP8, true>(a, lds, t, piece, w);
+        if (FEW || t.rows <= kSub) done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
+        else done = some_rows<BITS, true>(a, lds, t, piece, w);
         if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
     };
     if constexpr (!SELF) {
@@ -1126,7 +1157,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
         scan<64 * kWaves>(on[0] + on[1], plan_.sums, T, tiles);
         scan<64 * kWaves>(length[0] + length[1], plan_.sums, at, total);
         total = same(total), tiles = same(tiles);
-        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, FP8))), x0 = w * per;
+        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, BITS < 16))), x0 = w * per;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (on[kind]) {
@@ -1376,17 +1407,18 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     }
     {
         KernelTimer kt("extend", st);
-        auto launch = [&](auto fp8) {
-            constexpr bool FP8 = decltype(fp8)::value;
+        auto launch = [&](auto bits) {
+            constexpr int BITS = decltype(bits)::value;
             const dim3 grid(a.workgroups), threads(64 * kWaves);
-            if (!a.few) hipLaunchKernelGGL(extend_kernel<FP8>, grid, threads, 0, st, a);
-            else if (a.tile_rows == kSub && self) hipLaunchKernelGGL((extend_short_kernel<FP8, true, true>), grid, threads, 0, st, a);
-            else if (a.tile_rows == kSub) hipLaunchKernelGGL((extend_short_kernel<FP8, true, false>), grid, threads, 0, st, a);
-            else if (self) hipLaunchKernelGGL((extend_short_kernel<FP8, false, true>), grid, threads, 0, st, a);
-            else hipLaunchKernelGGL((extend_short_kernel<FP8, false, false>), grid, threads, 0, st, a);
+            if (!a.few) hipLaunchKernelGGL(extend_kernel<BITS>, grid, threads, 0, st, a);
+            else if (a.tile_rows == kSub && self) hipLaunchKernelGGL((extend_short_kernel<BITS, true, true>), grid, threads, 0, st, a);
+            else if (a.tile_rows == kSub) hipLaunchKernelGGL((extend_short_kernel<BITS, true, false>), grid, threads, 0, st, a);
+            else if (self) hipLaunchKernelGGL((extend_short_kernel<BITS, false, true>), grid, threads, 0, st, a);
+            else hipLaunchKernelGGL((extend_short_kernel<BITS, false, false>), grid, threads, 0, st, a);
         };
-        if (c.fp8) launch(std::true_type{});
-        else launch(std::false_type{});
+        if (c.bits == 16) launch(std::integral_constant<int, 16>{});
+        else if (c.bits == 8) launch(std::integral_constant<int, 8>{});
+        else launch(std::integral_constant<int, 4>{});
     }
     {
         KernelTimer kt("extend_combine", st);

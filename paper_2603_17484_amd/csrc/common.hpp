@@ -145,6 +145,17 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
                 int mask_heads, int max_new, int do_local, int do_global, void* O, float* lse_l, float* lse_g, void* S, void* A,
                 void* workspace, hipStream_t st);
 
+// ---- cache_weights.hip, cache_evict.hip : attention weights that cached rows receive, and the eviction of those that receive least
+size_t weights_workspace(const Geom& g, int max_new);
+int cache_weights(const Geom& g, const Pages& c, const void* q, const int32_t* seq_start, const int32_t* pos, const float* lse, int max_new,
+                  float decay, const float* weight_in, float* weight, void* workspace, hipStream_t st);
+size_t evict_workspace(const Geom& g, int max_rows);
+int cache_evict(const Geom& g, const Pages& c, const int32_t* rows, const int32_t* keep, int max_rows, const float* weight_in, float* weight,
+                int32_t* kept, void* workspace, hipStream_t st);
+
+// ---- rope.hip : rotary positions
+int rope(const l2a_params& p, const l2a_rotary& r, const void* q, const void* k, const int32_t* pos, void* q_out, void* k_out, hipStream_t st);
+
 // ---- pack.hip : layout pre-passes (token-minor copies for the matrix-core kernels)
 struct Fill {  // n 32-bit words of one value
     uint32_t* p;

@@ -106,20 +106,21 @@ int check_cache(const l2a_params* p, const l2a_cache* c) {
     if (p->B < 1 || (long long)p->B * p->Hkv > 65535 || (long long)p->T * p->Hq > (1LL << 27)) return L2A_ERR_SHAPE;
     if (!use_mfma(*p) || (p->flags & L2A_FLAG_RING_CACHE)) return L2A_ERR_UNSUPPORTED;
     if (!c || !c->k || !c->v || !c->table) return L2A_ERR_NULL;
-    if (c->dtype != L2A_BF16 && c->dtype != L2A_FP8) return L2A_ERR_UNSUPPORTED;
-    if (c->dtype == L2A_FP8 && (!c->k_scale || !c->v_scale)) return L2A_ERR_NULL;
+    if (c->dtype != L2A_BF16 && c->dtype != L2A_FP8 && c->dtype != L2A_FP4) return L2A_ERR_UNSUPPORTED;
+    const bool scaled = c->dtype != L2A_BF16;
+    if (scaled && (!c->k_scale || !c->v_scale)) return L2A_ERR_NULL;
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return L2A_ERR_SHAPE;
     if (c->pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1LL << 24)) return L2A_ERR_SHAPE;
-    if (misaligned(c->k) || misaligned(c->v) || (c->dtype == L2A_FP8 && (misaligned(c->k_scale) || misaligned(c->v_scale)))) return L2A_ERR_ALIGN;
+    if (misaligned(c->k) || misaligned(c->v) || (scaled && (misaligned(c->k_scale) || misaligned(c->v_scale)))) return L2A_ERR_ALIGN;
     if (misaligned4(c->table)) return L2A_ERR_ALIGN;
     return L2A_OK;
 }
 Pages make_pages(const l2a_cache& c) {
     int log2 = 0;
     while ((1 << log2) < c.page_size) ++log2;
-    const bool fp8 = c.dtype == L2A_FP8;
-    return Pages{(char*)c.k, (char*)c.v, fp8 ? (unsigned char*)c.k_scale : nullptr, fp8 ? (unsigned char*)c.v_scale : nullptr, c.table,
-                 c.pages, log2, c.max_pages, fp8};
+    const bool scaled = c.dtype != L2A_BF16;
+    return Pages{(char*)c.k, (char*)c.v, scaled ? (unsigned char*)c.k_scale : nullptr, scaled ? (unsigned char*)c.v_scale : nullptr, c.table,
+                 c.pages, log2, c.max_pages, c.dtype == L2A_FP4 ? 4 : scaled ? 8 : 16};
 }
 Geom packed_geom(const l2a_params& p, const Pages& c) {
     Geom g = make_geom(p);
@@ -374,6 +375,82 @@ int l2a_attn_extend(const l2a_params* p, const l2a_cache* c, const void* q, cons
     if (misaligned(workspace)) return L2A_ERR_ALIGN;
     return mfma_extend(g, pages, q, seq_start, pos, dense ? nullptr : mask, p->mask_heads, max_new, do_local, do_global, O, lse_local,
                        lse_global, S_opt, A_opt, workspace, (hipStream_t)stream);
+}
+
+size_t l2a_weights_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_new) {
+    if (check_cache(p, c) != L2A_OK || max_new < 1) return 0;
+    return weights_workspace(packed_geom(*p, make_pages(*c)), max_new);
+}
+
+int l2a_cache_weights(const l2a_params* p, const l2a_cache* c, const void* q, const int32_t* seq_start, const int32_t* pos,
+                      const float* lse_global, int32_t max_new, float decay, const float* weight_in, float* weight, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    const int rc = check_cache(p, c);
+    if (rc != L2A_OK) return rc;
+    if (max_new < 1 || !(decay >= 0.f && decay < INFINITY)) return L2A_ERR_SHAPE;
+    if (!q || !seq_start || !pos || !lse_global || !weight) return L2A_ERR_NULL;
+    if (misaligned(q)) return L2A_ERR_ALIGN;
+    const void* words[] = {seq_start, pos, lse_global, weight_in, weight};
+    for (const void* x : words)
+        if (x && misaligned4(x)) return L2A_ERR_ALIGN;
+    const Pages pages = make_pages(*c);
+    const Geom g = packed_geom(*p, pages);
+    const size_t need = weights_workspace(g, max_new);
+    if (need && (!workspace || workspace_bytes < need)) return L2A_ERR_WORKSPACE;
+    if (need && misaligned(workspace)) return L2A_ERR_ALIGN;
+    return cache_weights(g, pages, q, seq_start, pos, lse_global, max_new, decay, decay > 0.f ? weight_in : nullptr, weight, workspace, (hipStream_t)stream);
+}
+
+size_t l2a_evict_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_rows) {
+    if (check_cache(p, c) != L2A_OK || max_rows < 1 || max_rows > (1 << 24)) return 0;
+    return evict_workspace(packed_geom(*p, make_pages(*c)), max_rows);
+}
+
+int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows, const int32_t* keep, int32_t max_rows,
+                    const float* weight_in, float* weight, int32_t* kept_opt, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_cache(p, c);
+    if (rc != L2A_OK) return rc;
+    if (max_rows < 1 || max_rows > (1 << 24)) return L2A_ERR_SHAPE;
+    if (!rows || !keep || !weight_in || !weight) return L2A_ERR_NULL;
+    const void* words[] = {rows, keep, weight_in, weight, kept_opt};
+    for (const void* x : words)
+        if (x && misaligned4(x)) return L2A_ERR_ALIGN;
+    const Pages pages = make_pages(*c);
+    const Geom g = packed_geom(*p, pages);
+    if (!workspace || workspace_bytes < evict_workspace(g, max_rows)) return L2A_ERR_WORKSPACE;
+    if (misaligned(workspace)) return L2A_ERR_ALIGN;
+    return cache_evict(g, pages, rows, keep, max_rows, weight_in, weight, kept_opt, workspace, (hipStream_t)stream);
+}
+
+int l2a_rope(const l2a_params* p, const l2a_rotary* r, const void* q, const void* k, const int32_t* pos, void* q_out, void* k_out,
+             void* stream) {
+    const int rc = check_params(p);
+    if (rc != L2A_OK) return rc;
+    if (!r || !r->freq || !pos || (!q && !k) || (q && !q_out) || (k && !k_out)) return L2A_ERR_NULL;
+    if (r->axes < 1 || r->axes > 4) return L2A_ERR_SHAPE;
+    long long pairs = 0;
+    for (int i = 0; i < r->axes; ++i) {
+        if (r->pairs[i] < 0) return L2A_ERR_SHAPE;
+        pairs += r->pairs[i];
+    }
+    if (pairs < 8 || pairs % 8 != 0 || 2 * pairs > p->D) return L2A_ERR_SHAPE;
+    if (r->flags & ~(L2A_ROTARY_ADJACENT | L2A_ROTARY_INVERSE)) return L2A_ERR_UNSUPPORTED;
+    struct {
+        const void *in, *out;
+        int32_t in_stride, out_stride;
+        int heads;
+    } const tensors[] = {{q, q_out, r->q_stride, r->q_out_stride, p->Hq}, {k, k_out, r->k_stride, r->k_out_stride, p->Hkv}};
+    const int vec = p->dtype == L2A_BF16 ? 8 : 4;
+    for (const auto& t : tensors) {
+        if (!t.in) continue;
+        for (const int32_t s : {t.in_stride, t.out_stride})
+            if (s != 0 && (s < (long long)t.heads * p->D || s % vec != 0)) return L2A_ERR_SHAPE;
+        if (misaligned(t.in) || misaligned(t.out)) return L2A_ERR_ALIGN;
+        const int dense = t.heads * p->D;
+        if (t.in == t.out && (t.in_stride ? t.in_stride : dense) != (t.out_stride ? t.out_stride : dense)) return L2A_ERR_UNSUPPORTED;
+    }
+    if (misaligned4(pos) || misaligned4(r->freq)) return L2A_ERR_ALIGN;
+    return rope(*p, *r, q, k, pos, q_out, k_out, (hipStream_t)stream);
 }
 
 int l2a_attn_bwd(const l2a_params* p, const void* dO, const void* q_loc, const void* k_loc,

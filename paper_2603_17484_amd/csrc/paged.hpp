@@ -5,6 +5,9 @@
 // stands for e4m3 * 2^(exponent - 127).  Four significant bits times a power of two are a bf16 number, so that reading such a cache
 // rounds nothing, the conversion instruction takes the scale along, and the matrix cores see bf16 either way.  (One float
 // per row would cost the same four bytes, and a multiplication of every score and every weight.)
+// Elements of 4 bits are e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6) in the same blocks, the lower channel of a byte in its lower bits; they too are bf16
+// numbers with their scale.  The elements hold neither infinities nor NaN: the exponent byte 255 makes a block NaN, which the conversion
+// instruction does by itself.
 #pragma once
 #include "extend_plan.hpp"
 #include "mfma.hpp"
@@ -13,15 +16,19 @@ namespace l2a {
 
 struct Pages {
     char *k, *v;
-    unsigned char *ks, *vs;  // e4m3: 4 exponents per row; otherwise null
+    unsigned char *ks, *vs;  // e4m3, e2m1: 4 exponents per row; otherwise null
     const int32_t* table;    // [B, max_pages]
-    int pages, page_log2, max_pages, fp8;
+    int pages, page_log2, max_pages, bits;  // bits: of an element, 16 (bf16), 8 (e4m3) or 4 (e2m1)
     __host__ __device__ int capacity() const { return max_pages << page_log2; }
 };
 
 constexpr int kScaleBlock = 32;                  // channels that share an exponent
 constexpr int kRowScales = kD / kScaleBlock;     // exponents of a row
-constexpr int kMinExponent = -118, kMaxExponent = 119;  // 2^-9 (the smallest element) and 448 times these are bf16 numbers
+// of a block: the smallest element (e4m3 2^-9, e2m1 2^-1) and the largest (448, 6) times 2 to these are bf16 numbers
+template <int BITS>
+constexpr int kMinExponent = BITS == 8 ? -118 : -125;
+template <int BITS>
+constexpr int kMaxExponent = BITS == 8 ? 119 : 125;
 
 // The row of a token in the pool (rows of all pages counted through), page number p.
 __device__ __forceinline__ size_t pool_row(const Pages& c, int hkv, int p, int hk, int t) {
@@ -33,12 +40,25 @@ __device__ __forceinline__ plan::Seq seq_at(const Geom& gm, const Pages& c, cons
 // 2^(e - 127) for the exponents that the cache holds
 __device__ __forceinline__ float exponent_value(unsigned e) { return __uint_as_float(e << 23); }
 
-// Sixteen e4m3 elements -> sixteen bf16 values, all times `scale`.
-__device__ __forceinline__ void dequantise16(const u32x4& x, float scale, u32x4 (&y)[2]) {
+// Eight e2m1 elements -> bf16 values, times `scale`.
+__device__ __forceinline__ void dequantise8(uint32_t x, float scale, u32x4& y) {
+    y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0));
+    y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1));
+    y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2));
+    y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
+}
+// Sixteen bytes of elements -> bf16 values, all times `scale`: 16 of e4m3 in two vectors, 32 of e2m1 in four.
+template <int BITS>
+__device__ __forceinline__ void dequantise(const u32x4& x, float scale, u32x4 (&y)[16 / BITS]) {
+    if constexpr (BITS == 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[i >> 1][(i & 1) * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, false));
-        y[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, true));
+        for (int i = 0; i < 4; ++i) {
+            y[i >> 1][(i & 1) * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, false));
+            y[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, true));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dequantise8(x[i], scale, y[i]);
     }
 }
 

@@ -127,11 +127,16 @@ class PagedCache:
     """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; a copy is kept as .p, whose T every step sets) and the bookkeeping around it: pages
     are handed out as sequences grow and taken back when they end.  The pool, the table and the steps' index arrays are on the GPU, what decides
     about them on the host.  A step uploads the table and its index arrays, which waits for the stream's earlier work, and allocates its output (and
-    its workspace, where none is given).  Steps of one cache are ordered, on one stream or by the caller."""
+    its workspace, where none is given).  Steps of one cache are ordered, on one stream or by the caller.
+    fp8, fp4: elements of 8 or 4 bits.  decay: a number keeps the attention weights that rows receive (`weight`), which fade by it in every step of
+    their sequence; evict() goes by them.  Rows of a sequence that was evicted from are no longer its positions: positions() has those."""
 
-    def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda"):
-        self.p, self.page_size = B.l2a_params.from_buffer_copy(p), page_size
-        self.cache = B.alloc_cache(p, pages, page_size, max_pages, fp8, device)
+    def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", fp4: bool = False,
+                 decay: Optional[float] = None):
+        self.p, self.page_size, self.decay = B.l2a_params.from_buffer_copy(p), page_size, decay
+        self.cache = B.alloc_cache(p, pages, page_size, max_pages, fp8, device, **({"fp4": True} if fp4 else {}))
+        self.weight = None if decay is None else torch.zeros(pages, p.Hkv, page_size, dtype=torch.float32, device=device)
+        self.evicted = np.zeros(p.B, dtype=np.int64)  # rows given up
         self.table = np.full((p.B, max_pages), -1, dtype=np.int32)
         self.length = np.zeros(p.B, dtype=np.int32)
         self.free = list(range(pages - 1, -1, -1))
@@ -144,10 +149,8 @@ class PagedCache:
             raise RuntimeError("steps upload their indices from the host and cannot be captured; capture l2a_cache_write and l2a_attn_extend with index "
                                "arrays at fixed addresses")
 
-    def begin_step(self, new):
-        """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
-        number."""
-        self._check_not_captured()
+    def _numbers(self, new) -> np.ndarray:
+        """Numbers of new tokens for which the table has room."""
         new = np.asarray(new)
         if new.shape != (self.p.B,):
             raise ValueError(f"a step has a number of new tokens for each of the {self.p.B} sequences; got {new.tolist()}")
@@ -156,7 +159,22 @@ class PagedCache:
         # (compared as they came: what does not fit into 32 bits does not fit into the table either)
         if (new < 0).any() or (new > self.table.shape[1] * self.page_size - self.length.astype(np.int64)).any():
             raise ValueError("no room for the step's tokens")
-        new = new.astype(np.int32)
+        return new.astype(np.int32)
+
+    def positions(self, new) -> torch.Tensor:
+        """-> [1, T] int32 on the GPU: the positions in their sequences of the tokens of a step that is to come, for l2a_rope."""
+        self._check_not_captured()
+        new = self._numbers(new)
+        first = self.length + self.evicted
+        if (first + new > np.iinfo(np.int32).max).any():
+            raise ValueError("positions have 32 bits")
+        return self._upload(np.concatenate([f + np.arange(n) for f, n in zip(first, new)]).astype(np.int32)).view(1, -1)
+
+    def begin_step(self, new):
+        """Room for new[b] tokens of every sequence, which count as theirs from here on.  -> (seq_start, pos) on the GPU; the params' T is their
+        number."""
+        self._check_not_captured()
+        new = self._numbers(new)
         need = -(-(self.length + new) // self.page_size)
         have = -(-self.length // self.page_size)
         if int((need - have).sum()) > len(self.free):
@@ -196,7 +214,12 @@ class PagedCache:
                     raise ValueError("the step has no new tokens, but rows")
                 return O
             B.l2a_cache_write(self.p, self.cache, k, v, start, pos)
-            B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, max(int(max(new)), 1), O, **outs)
+            most = max(int(max(new)), 1)
+            if self.weight is not None and outs.get("lse_global") is None:
+                outs["lse_global"] = torch.empty(self.p.Hq, self.p.T, dtype=torch.float32, device=q.device)
+            B.l2a_attn_extend(self.p, self.cache, q, start, pos, mask, most, O, **outs)
+            if self.weight is not None:
+                B.l2a_cache_weights(self.p, self.cache, q, start, pos, outs["lse_global"], most, self.decay, self.weight, self.weight)
         except BaseException:
             self._take_back(before)
             raise
@@ -216,9 +239,40 @@ class PagedCache:
                          self._upload(np.zeros(self.p.B, dtype=np.int32)), k, v)
         return k, v
 
+    def evict(self, limit, recent: Optional[int] = None) -> np.ndarray:
+        """Sequences with more than limit (one number, or one each) rows give rows up, in whole pages, down to the limit or as far as they can:
+        every KV head those that received the least attention, never one of the last `recent` (default and least: the window W).  -> rows given
+        up by each sequence, whose pages are free."""
+        if self.weight is None:
+            raise ValueError("the cache keeps no attention weights (decay)")
+        self._check_not_captured()
+        local = not self.p.flags & B.L2A_FLAG_SKIP_LOCAL
+        recent = self.p.W if recent is None else int(recent)
+        if recent < 0 or (local and recent < self.p.W):
+            raise ValueError(f"the last {self.p.W} rows are in the window")
+        limit = np.broadcast_to(np.asarray(limit, dtype=np.int64), (self.p.B,))
+        if (limit < 0).any():
+            raise ValueError("limits are numbers of rows")
+        over = self.length > limit
+        rows = np.where(over, np.maximum(self.length.astype(np.int64) - recent, 0) // self.page_size * self.page_size, 0)
+        keep = np.clip((limit - (self.length - rows)) // self.page_size * self.page_size, 0, rows)
+        gone = rows - keep
+        if not gone.any():
+            return gone
+        self.p.T = 1
+        B.l2a_cache_evict(self.p, self.cache, self._upload(rows.astype(np.int32)), self._upload(keep.astype(np.int32)), int(rows.max()), self.weight, self.weight)
+        for b in np.nonzero(gone)[0]:
+            first, last = keep[b] // self.page_size, rows[b] // self.page_size
+            self.free.extend(int(x) for x in self.table[b, first:last])
+            self.table[b] = np.concatenate([self.table[b, :first], self.table[b, last:], np.full(last - first, -1, dtype=np.int32)])
+        self.length = (self.length - gone).astype(np.int32)
+        self.evicted = self.evicted + gone
+        self.cache.tensors[4].copy_(torch.from_numpy(self.table))
+        return gone
+
     def end(self, b: int):
         """Sequence b is over: its pages are free."""
         b = range(self.p.B)[b]  # (-1: the last one)
         used = -(-int(self.length[b]) // self.page_size)
         self.free.extend(int(x) for x in self.table[b, :used])
-        self.table[b], self.length[b] = -1, 0
+        self.table[b], self.length[b], self.evicted[b] = -1, 0, 0
