@@ -4,8 +4,13 @@
 // independent of one another, in place, and no more bytes move than have to.  The order of rows does not matter to the attention over them:
 // their positions are in the keys.
 //
-//   evict_select_kernel  a workgroup per KV head of a sequence: the weight of the last row that stays, by radix selection (8 bits a
-//                        pass over the weights' bits, ordered as whole numbers), and the lists of places and of rows that move there
+// Which rows stay is a radix selection over the weights' bits, ordered as whole numbers: the histogram of their highest bits says in which bin
+// the last row that stays lies, that of the bits below among the rows of this bin where in it, and so on.  Then the lists: places that become free, and
+// rows that move there, both ascending.
+//   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 8 bits a pass
+//   evict_first_kernel, evict_second_kernel, evict_third_kernel, evict_list_kernel
+//                        more: a workgroup per 8192 rows (or 1/64), 11, 11 and 10 bits; each leaves its own histogram, and each workgroup of the next
+//                        kernel adds up those of its KV head (no atomics on memory, nothing to clear)
 //   evict_move_kernel    the moves: K, V, exponents, weights
 #include "paged.hpp"
 
@@ -13,7 +18,10 @@ namespace l2a {
 namespace {
 
 constexpr int kSelectThreads = 1024;
-constexpr int kBins = 256;
+constexpr int kPer = 8;                          // rows of a thread
+constexpr int kBlock = kSelectThreads * kPer;
+constexpr int kMostSegments = 64;                // workgroups of a KV head of a sequence
+constexpr int kBins1 = 2048, kBins3 = 1024;      // 11, 11 and 10 bits
 
 struct EvictArgs {
     Geom gm;
@@ -26,6 +34,12 @@ struct EvictArgs {
     // workspace
     int32_t* moves;   // [B * Hkv]: how many
     int32_t *to, *from;  // [B * Hkv][max_rows / 2]
+    // of calls with more than kBlock rows
+    int segments, segment;  // of a KV head of a sequence; rows of each, whole blocks
+    uint32_t* keys;   // [B * Hkv][max_rows] order of the weights
+    int32_t *bins1, *bins2;  // [B * Hkv][segments][kBins1]
+    int32_t* bins3;   // [B * Hkv][segments][2][kBins3]: of rows before the keep-th and behind
+    int32_t* above;   // [B * Hkv][segments][2]: rows whose upper 22 bits say that they stay, before and behind
 };
 
 __device__ __forceinline__ int rows_of(const EvictArgs& a, int b) { return plan::clamp(a.rows[b], 0, min(a.max_rows, a.c.capacity())); }
@@ -40,99 +54,380 @@ __device__ __forceinline__ size_t row_at(const EvictArgs& a, int b, int hk, int 
     return pool_row(a.c, a.gm.Hkv, plan::clamp(page_at(a, b, row), 0, a.c.pages - 1), hk, row);
 }
 
-// Sum of x over the threads before this one, and over all.
-__device__ __forceinline__ void scan(int x, int* sums, int& before, int& total) {
+struct Sizes {
+    int pair, b, hk, n, m;
+};
+__device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int pair) {
+    Sizes z;
+    z.pair = pair, z.b = pair / a.gm.Hkv, z.hk = pair - z.b * a.gm.Hkv;
+    z.n = rows_of(a, z.b), z.m = plan::clamp(a.keep[z.b], 0, z.n);
+    return z;
+}
+// Row i0 + 1024 j + thread of a block as order; 0 past the end.
+__device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
+    float w[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        w[j] = i < z.n ? a.weight_in[row_at(a, z.b, z.hk, i)] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x[j] = i0 + j * kSelectThreads + (int)threadIdx.x < z.n ? order(w[j]) : 0u;
+}
+__device__ __forceinline__ void load_keys(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
+    const uint32_t* const keys = a.keys + (size_t)z.pair * a.max_rows;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        x[j] = i < z.n ? keys[i] : 0u;
+    }
+}
+
+struct Shared {
+    int sums[kSelectThreads / 64], chosen[2], counts[kPer][kSelectThreads / 64];
+};
+// Bins from the highest number down, EACH a thread in the order of threads; mine: how many rows this thread's have, `highest` its first.  The bin in
+// which the left-th row lies, and the how-manieth in it that is.
+template <int EACH>
+__device__ __forceinline__ void choose(Shared& sh, const int (&mine)[EACH], int highest, int& bin, int& left) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = x;
+    int sum = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) sum += mine[e];
+    int upto = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int below = __shfl_up(upto, o);
         if (lane >= o) upto += below;
     }
+    if (lane == 63) sh.sums[wave] = upto;
     __syncthreads();
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    before = upto - x, total = 0;
+    int before = upto - sum;
 #pragma unroll
-    for (int w = 0; w < kSelectThreads / 64; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
+    for (int w = 0; w < kSelectThreads / 64; ++w)
+        if (w < wave) before += sh.sums[w];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        if (before < left && left <= before + mine[e]) sh.chosen[0] = highest - e, sh.chosen[1] = left - before;
+        before += mine[e];
     }
+    __syncthreads();
+    bin = sh.chosen[0], left = sh.chosen[1];
+    __syncthreads();
+}
+// Places of flags among all of a block, in the order of rows: of this thread's j-th, how many lie before it; and how many there are.
+__device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], int (&at)[kPer]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned long long set[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        set[j] = __ballot(flag[j]);
+        if (lane == 0) sh.counts[j][wave] = __popcll(set[j]);
+    }
+    __syncthreads();
+    // every wavefront adds up all counts: a lane those of two
+    constexpr int kWavesOf = kSelectThreads / 64, kCounts = kPer * kWavesOf;
+    static_assert(kCounts == 128, "two counts a lane");
+    const int* const counts = &sh.counts[0][0];
+    const int c0 = counts[2 * lane], c1 = counts[2 * lane + 1];
+    int upto = c0 + c1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int below = __shfl_up(upto, o);
+        if (lane >= o) upto += below;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = j * kWavesOf + wave;
+        at[j] = __shfl(upto - c0 - c1, i >> 1) + (i & 1 ? __shfl(c0, i >> 1) : 0) + __popcll(set[j] & ((1ull << lane) - 1ull));
+    }
+    const int total = __shfl(upto, 63);
+    __syncthreads();
+    return total;
+}
+// What the rows of a block before it had: equal ones, places that become free, rows that move.
+struct Before {
+    int equal, holes, movers;
+};
+// The lists of a block, its rows x in registers: all greater than `found` stay, and the first `left` of those equal to it.
+__device__ __forceinline__ void list_block(const EvictArgs& a, Shared& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past) {
+    int32_t *to = a.to + (size_t)z.pair * (a.max_rows / 2), *from = a.from + (size_t)z.pair * (a.max_rows / 2);
+    int32_t* const kept = a.kept ? a.kept + (size_t)z.pair * a.max_rows : nullptr;
+    bool flag[kPer], stays[kPer];
+    int at[kPer];
+    const bool all = z.m == z.n;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * kSelectThreads + (int)threadIdx.x < z.n;
+    const int equal = places(sh, flag, at);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        stays[j] = i < z.n && (all || x[j] > found || (flag[j] && past.equal + at[j] < left));
+        flag[j] = i < z.m && !stays[j];
+    }
+    const int holes = places(sh, flag, at);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (flag[j]) to[past.holes + at[j]] = i0 + j * kSelectThreads + (int)threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) flag[j] = i0 + j * kSelectThreads + (int)threadIdx.x >= z.m && stays[j];
+    const int movers = places(sh, flag, at);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        if (flag[j]) from[past.movers + at[j]] = i;
+        if (i >= z.m || !stays[j]) continue;
+        if (kept) kept[i] = i;
+        if (a.weight != a.weight_in && (unsigned)page_at(a, z.b, i) < (unsigned)a.c.pages) {
+            const size_t row = row_at(a, z.b, z.hk, i);
+            a.weight[row] = a.weight_in[row];
+        }
+    }
+    past = Before{past.equal + equal, past.holes + holes, past.movers + movers};
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-    __shared__ int bins[kBins], sums[kSelectThreads / 64], chosen[2];
-    const int pair = blockIdx.x, b = pair / a.gm.Hkv, hk = pair - b * a.gm.Hkv;
-    const int n = rows_of(a, b), m = plan::clamp(a.keep[b], 0, n);
-    // the m-th greatest: from the highest 8 bits on, which value they have, and the how-manieth of those with it that is
-    uint32_t found = 0;
-    int left = m;
-    if (m > 0 && m < n) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < n; i += kSelectThreads) {
-                const uint32_t x = order(a.weight_in[row_at(a, b, hk, i)]);
-                if (shift == 24 || (x >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&bins[(x >> shift) & 255], 1);
-            }
-            __syncthreads();
-            // thread t: the bins above t
-            const int mine = threadIdx.x < kBins ? bins[kBins - 1 - threadIdx.x] : 0;
-            int before, total;
-            scan(mine, sums, before, total);
-            if (threadIdx.x < kBins && before < left && left <= before + mine) chosen[0] = kBins - 1 - (int)threadIdx.x, chosen[1] = left - before;
-            __syncthreads();
-            found |= (uint32_t)chosen[0] << shift, left = chosen[1];
-            __syncthreads();
-        }
+    constexpr int kBins = 256;
+    __shared__ Shared sh;
+    __shared__ int bins[kBins];
+    const Sizes z = sizes_of(a, blockIdx.x);
+    if (z.m == 0) {
+        if (threadIdx.x == 0) a.moves[z.pair] = 0;
+        return;
     }
-    // `left` rows with the weight found stay, the first ones, and all with a greater one
-    int32_t *to = a.to + (size_t)pair * (a.max_rows / 2), *from = a.from + (size_t)pair * (a.max_rows / 2);
-    int32_t* const kept = a.kept ? a.kept + (size_t)pair * a.max_rows : nullptr;
-    int equal = 0, holes = 0, movers = 0;
-    for (int i0 = 0; i0 < n && m > 0; i0 += kSelectThreads) {
-        const int i = i0 + (int)threadIdx.x;
-        float w = 0.f;
-        size_t at = 0;
-        if (i < n) at = row_at(a, b, hk, i), w = a.weight_in[at];
-        const uint32_t x = order(w);
-        int before, total;
-        const bool tie = i < n && m < n && x == found;
-        scan(tie, sums, before, total);
-        const bool stays = i < n && (m == n || x > found || (tie && equal + before < left));
-        equal += total;
-        const bool hole = i < m && !stays, mover = i >= m && stays;
-        scan((hole ? 1 : 0) + (mover ? 0x10000 : 0), sums, before, total);
-        if (hole) to[holes + (before & 0xffff)] = i;
-        if (mover) from[movers + (before >> 16)] = i;
-        holes += total & 0xffff, movers += total >> 16;
-        if (i < m && stays) {
-            if (a.weight != a.weight_in && (unsigned)page_at(a, b, i) < (unsigned)a.c.pages) a.weight[at] = w;
-            if (kept) kept[i] = i;
-        }
+    uint32_t x[kPer], found = 0;
+    load_block(a, z, 0, x);
+    int left = z.m;
+    for (int shift = 24; shift >= 0 && z.m < z.n; shift -= 8) {
+        if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (j * kSelectThreads + (int)threadIdx.x < z.n && (shift == 24 || (x[j] >> (shift + 8)) == (found >> (shift + 8)))) atomicAdd(&bins[(x[j] >> shift) & 255], 1);
+        __syncthreads();
+        const int mine[1] = {threadIdx.x < kBins ? bins[kBins - 1 - threadIdx.x] : 0};
+        int bin;
+        choose<1>(sh, mine, kBins - 1 - (int)threadIdx.x, bin, left);
+        found |= (uint32_t)bin << shift;
     }
-    if (threadIdx.x == 0) a.moves[pair] = holes;
+    Before past{0, 0, 0};
+    list_block(a, sh, z, 0, x, found, left, past);
+    if (threadIdx.x == 0) a.moves[z.pair] = past.holes;
 }
 
-// A group of lanes per move: 16 lanes K, 16 lanes V.
+// The workgroup's segment of its pair: rows i0 .. i1 - 1.
+struct Segment {
+    int i0, i1;
+};
+__device__ __forceinline__ Segment segment_of(const EvictArgs& a, const Sizes& z) {
+    const long long i0 = (long long)blockIdx.x * a.segment;
+    Segment g;
+    g.i0 = i0 < z.n ? (int)i0 : z.n, g.i1 = i0 + a.segment < z.n ? (int)(i0 + a.segment) : z.n;
+    return g;
+}
+__device__ __forceinline__ int32_t* bins_at(const EvictArgs& a, int32_t* bins, int pair, int segment) { return bins + ((size_t)pair * a.segments + segment) * kBins1; }
+// Segments that have rows.
+__device__ __forceinline__ int segments_of(const EvictArgs& a, const Sizes& z) { return (z.n + a.segment - 1) / a.segment; }
+// The bin of a pair's histograms, all segments together, in which the left-th row lies.
+__device__ __forceinline__ int choose_bin(const EvictArgs& a, Shared& sh, const Sizes& z, int32_t* bins, int& left) {
+    int mine[2] = {0, 0};
+    const int highest = kBins1 - 1 - 2 * (int)threadIdx.x, of = segments_of(a, z);
+#pragma unroll 8
+    for (int g = 0; g < of; ++g) {
+        const int32_t* const p = bins_at(a, bins, z.pair, g);
+        mine[0] += p[highest], mine[1] += p[highest - 1];
+    }
+    int bin;
+    choose<2>(sh, mine, highest, bin, left);
+    return bin;
+}
+static_assert(kBins1 == 2 * kSelectThreads && 2 * kBins3 == kBins1, "bins of a thread");
+
+// The highest 11 bits, and the order of all rows for the kernels behind.
+__global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a) {
+    __shared__ int bins[kBins1];
+    const Sizes z = sizes_of(a, blockIdx.y);
+    const Segment g = segment_of(a, z);
+    if (g.i0 >= g.i1) return;
+    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) bins[i] = 0;
+    __syncthreads();
+    for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
+        uint32_t x[kPer];
+        load_block(a, z, i0, x);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+            if (i < z.n) {
+                a.keys[(size_t)z.pair * a.max_rows + i] = x[j];
+                atomicAdd(&bins[x[j] >> 21], 1);
+            }
+        }
+    }
+    __syncthreads();
+    int32_t* const out = bins_at(a, a.bins1, z.pair, blockIdx.x);
+    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) out[i] = bins[i];
+}
+// The next 11 bits of rows in the bin found.
+__global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs a) {
+    __shared__ Shared sh;
+    __shared__ int bins[kBins1];
+    const Sizes z = sizes_of(a, blockIdx.y);
+    const Segment g = segment_of(a, z);
+    if (g.i0 >= g.i1 || z.m == 0 || z.m == z.n) return;
+    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) bins[i] = 0;
+    int left = z.m;
+    const uint32_t first = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
+    for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
+        uint32_t x[kPer];
+        load_keys(a, z, i0, x);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (i0 + j * kSelectThreads + (int)threadIdx.x < z.n && (x[j] >> 21) == first) atomicAdd(&bins[(x[j] >> 10) & (kBins1 - 1)], 1);
+    }
+    __syncthreads();
+    int32_t* const out = bins_at(a, a.bins2, z.pair, blockIdx.x);
+    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) out[i] = bins[i];
+}
+// The last 10, rows before the keep-th and behind apart, and how many of either stay for their higher bits.
+__global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(EvictArgs a) {
+    __shared__ Shared sh;
+    __shared__ int bins[2 * kBins3], above[2];
+    const Sizes z = sizes_of(a, blockIdx.y);
+    const Segment g = segment_of(a, z);
+    if (g.i0 >= g.i1 || z.m == 0 || z.m == z.n) return;
+    for (int i = threadIdx.x; i < 2 * kBins3; i += kSelectThreads) bins[i] = 0;
+    if (threadIdx.x < 2) above[threadIdx.x] = 0;
+    int left = z.m;
+    uint32_t upper = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
+    upper = upper << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
+    int mine[2] = {0, 0};
+    for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
+        uint32_t x[kPer];
+        load_keys(a, z, i0, x);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int i = i0 + j * kSelectThreads + (int)threadIdx.x, behind = i >= z.m;
+            if (i >= z.n) continue;
+            if ((x[j] >> 10) == upper) atomicAdd(&bins[behind * kBins3 + (int)(x[j] & (kBins3 - 1))], 1);
+            if ((x[j] >> 10) > upper) mine[0] += !behind, mine[1] += behind;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) mine[e] += __shfl_xor(mine[e], o);
+        if ((threadIdx.x & 63) == 0) atomicAdd(&above[e], mine[e]);
+    }
+    __syncthreads();
+    int32_t* const out = bins_at(a, a.bins3, z.pair, blockIdx.x);
+    for (int i = threadIdx.x; i < 2 * kBins3; i += kSelectThreads) out[i] = bins[i];
+    if (threadIdx.x < 2) a.above[((size_t)z.pair * a.segments + blockIdx.x) * 2 + threadIdx.x] = above[threadIdx.x];
+}
+// The lists.  What the segments before have of them follows from their histograms.
+__global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a) {
+    __shared__ Shared sh;
+    __shared__ int greater[kMostSegments][2], equal[kMostSegments][2];  // of each segment, before the keep-th row and behind
+    const Sizes z = sizes_of(a, blockIdx.y);
+    const Segment g = segment_of(a, z);
+    const int of = segments_of(a, z);
+    if (z.m == 0 || g.i0 >= g.i1) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.moves[z.pair] = 0;
+        return;
+    }
+    uint32_t found = 0;
+    int left = 0;
+    Before past{0, 0, 0};
+    if (z.m < z.n) {
+        left = z.m;
+        uint32_t upper = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
+        upper = upper << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
+        const int bin = kBins3 - 1 - (int)threadIdx.x;  // this thread's
+        int mine[1] = {0};
+#pragma unroll 8
+        for (int s = 0; s < of; ++s) {
+            const int32_t* const p = bins_at(a, a.bins3, z.pair, s);
+            mine[0] += p[bin] + p[kBins3 + bin];
+        }
+        int lowest;
+        choose<1>(sh, mine, bin, lowest, left);
+        found = upper << 10 | (uint32_t)lowest;
+        if (threadIdx.x < 2 * kMostSegments) (&greater[0][0])[threadIdx.x] = 0;
+        __syncthreads();
+        // (before this one: counts of all of these)
+        for (int s = 0; s < (int)blockIdx.x; ++s) {
+            const int32_t* const p = bins_at(a, a.bins3, z.pair, s);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int x = p[e * kBins3 + bin];
+                int more = bin > lowest ? x : 0;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
+                if ((threadIdx.x & 63) == 0 && more) atomicAdd(&greater[s][e], more);
+                if (bin == lowest) equal[s][e] = x;
+            }
+        }
+        __syncthreads();
+        for (int s = 0; s < (int)blockIdx.x; ++s) {
+            const int32_t* const up = a.above + ((size_t)z.pair * a.segments + s) * 2;
+            const int i0 = s * a.segment, i1 = i0 + a.segment, before = plan::clamp(z.m, i0, i1) - i0;  // rows of it before the keep-th
+            const int e0 = plan::clamp(left - past.equal, 0, equal[s][0]), e1 = plan::clamp(left - past.equal - equal[s][0], 0, equal[s][1]);
+            past.holes += before - up[0] - greater[s][0] - e0;
+            past.movers += up[1] + greater[s][1] + e1;
+            past.equal += equal[s][0] + equal[s][1];
+        }
+    }
+    for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
+        uint32_t x[kPer];
+        load_keys(a, z, i0, x);
+        list_block(a, sh, z, i0, x, found, left, past);
+    }
+    if ((int)blockIdx.x == of - 1 && threadIdx.x == 0) a.moves[z.pair] = past.holes;
+}
+
+// A group of lanes per move, 16 bytes a lane, K's and V's beside one another; kAhead moves of a group on their way together.
+template <int BITS>
 __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
+    constexpr int kLanes = 2 * BITS, kGroups = kThreads / kLanes, kAhead = 4, kRowBytes = kD * BITS / 8;
     const int pair = blockIdx.y, b = pair / a.gm.Hkv, hk = pair - b * a.gm.Hkv;
-    const int count = a.moves[pair], lane = threadIdx.x & 31, row_bytes = kD * a.c.bits / 8;
+    const int count = a.moves[pair], lane = threadIdx.x % kLanes, c = lane % (kLanes / 2);
     const size_t list = (size_t)pair * (a.max_rows / 2);
-    char* const pool = lane < 16 ? a.c.k : a.c.v;
-    unsigned char* const scales = lane < 16 ? a.c.ks : a.c.vs;
-    const int c = lane & 15;
-    for (int i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < count; i += gridDim.x * (kThreads / 32)) {
-        const int to = a.to[list + i], from = a.from[list + i];
-        if (lane == 0 && a.kept) a.kept[(size_t)pair * a.max_rows + to] = from;
-        // page numbers outside the pool are never followed
-        if ((unsigned)page_at(a, b, to) >= (unsigned)a.c.pages || (unsigned)page_at(a, b, from) >= (unsigned)a.c.pages) continue;
-        const size_t dst = row_at(a, b, hk, to), src = row_at(a, b, hk, from);
-        if (c * 16 < row_bytes) *reinterpret_cast<u32x4*>(pool + dst * row_bytes + c * 16) = *reinterpret_cast<const u32x4*>(pool + src * row_bytes + c * 16);
-        if (a.c.bits < 16 && c == 0) *reinterpret_cast<uint32_t*>(scales + dst * kRowScales) = *reinterpret_cast<const uint32_t*>(scales + src * kRowScales);
-        if (lane == 0) a.weight[dst] = a.weight_in[src];
+    char* const pool = (lane < kLanes / 2 ? a.c.k : a.c.v) + c * 16;
+    unsigned char* const scales = lane < kLanes / 2 ? a.c.ks : a.c.vs;
+    for (int i0 = (blockIdx.x * kGroups + (int)threadIdx.x / kLanes) * kAhead; i0 < count; i0 += gridDim.x * kGroups * kAhead) {
+        int to[kAhead], from[kAhead];
+        size_t dst[kAhead], src[kAhead];
+        bool on[kAhead];
+        u32x4 x[kAhead];
+        uint32_t e[kAhead];
+        float w[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) to[j] = a.to[list + min(i0 + j, count - 1)], from[j] = a.from[list + min(i0 + j, count - 1)];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int p = page_at(a, b, to[j]), q = page_at(a, b, from[j]);
+            on[j] = i0 + j < count && (unsigned)p < (unsigned)a.c.pages && (unsigned)q < (unsigned)a.c.pages;  // page numbers outside the pool are never followed
+            dst[j] = on[j] ? pool_row(a.c, a.gm.Hkv, p, hk, to[j]) : 0, src[j] = on[j] ? pool_row(a.c, a.gm.Hkv, q, hk, from[j]) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (on[j]) {
+                x[j] = *reinterpret_cast<const u32x4*>(pool + src[j] * kRowBytes);
+                if (BITS < 16 && c == 0) e[j] = *reinterpret_cast<const uint32_t*>(scales + src[j] * kRowScales);
+                if (lane == 1) w[j] = a.weight_in[src[j]];
+            }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (on[j]) {
+                *reinterpret_cast<u32x4*>(pool + dst[j] * kRowBytes) = x[j];
+                if (BITS < 16 && c == 0) *reinterpret_cast<uint32_t*>(scales + dst[j] * kRowScales) = e[j];
+                if (lane == 1) a.weight[dst[j]] = w[j];
+            }
+            if (lane == 2 && a.kept && i0 + j < count) a.kept[(size_t)pair * a.max_rows + to[j]] = from[j];
+        }
     }
 }
+
+constexpr int kMoveWorkgroups = 16384;
 
 size_t lay_out(EvictArgs& a, char* base) {
     size_t at = 0;
@@ -144,6 +439,14 @@ size_t lay_out(EvictArgs& a, char* base) {
     take(a.moves, pairs);
     take(a.to, pairs * (a.max_rows / 2));
     take(a.from, pairs * (a.max_rows / 2));
+    if (a.max_rows <= kBlock) return at;
+    a.segment = (a.max_rows + kMostSegments * kBlock - 1) / (kMostSegments * kBlock) * kBlock;
+    a.segments = (a.max_rows + a.segment - 1) / a.segment;
+    take(a.keys, pairs * a.max_rows);
+    take(a.bins1, pairs * a.segments * kBins1);
+    take(a.bins2, pairs * a.segments * kBins1);
+    take(a.bins3, pairs * a.segments * kBins1);
+    take(a.above, pairs * a.segments * 2);
     return at;
 }
 
@@ -160,14 +463,28 @@ int cache_evict(const Geom& g, const Pages& c, const int32_t* rows, const int32_
     EvictArgs a{g, c, rows, keep, max_rows, weight_in, weight, kept};
     lay_out(a, (char*)workspace);
     const int pairs = g.B * g.Hkv;
-    {
+    if (max_rows <= kBlock) {
         KernelTimer kt("evict_select", st);
         hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+    } else {
+        const dim3 grid(a.segments, pairs);
+        KernelTimer kt("evict_select", st);
+        hipLaunchKernelGGL(evict_first_kernel, grid, dim3(kSelectThreads), 0, st, a);
+        hipLaunchKernelGGL(evict_second_kernel, grid, dim3(kSelectThreads), 0, st, a);
+        hipLaunchKernelGGL(evict_third_kernel, grid, dim3(kSelectThreads), 0, st, a);
+        hipLaunchKernelGGL(evict_list_kernel, grid, dim3(kSelectThreads), 0, st, a);
     }
-    {
+    if (max_rows > 1) {
         KernelTimer kt("evict_move", st);
-        const int most = (max_rows / 2 + kThreads / 32 - 1) / (kThreads / 32), share = (4096 + pairs - 1) / pairs;
-        if (most) hipLaunchKernelGGL(evict_move_kernel, dim3(most < share ? most : share, pairs), dim3(kThreads), 0, st, a);
+        auto launch = [&](auto bits) {
+            constexpr int BITS = decltype(bits)::value;
+            constexpr int kEach = kThreads / (2 * BITS) * 4;  // moves of a workgroup
+            const int most = (max_rows / 2 + kEach - 1) / kEach, share = (kMoveWorkgroups + pairs - 1) / pairs;
+            hipLaunchKernelGGL(evict_move_kernel<BITS>, dim3(most < share ? most : share, pairs), dim3(kThreads), 0, st, a);
+        };
+        if (c.bits == 16) launch(std::integral_constant<int, 16>{});
+        else if (c.bits == 8) launch(std::integral_constant<int, 8>{});
+        else launch(std::integral_constant<int, 4>{});
     }
     return launch_status();
 }

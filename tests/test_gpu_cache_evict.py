@@ -106,6 +106,41 @@ def test_weights_of_all_kinds(name, rows, keep):
     check(make_step(8, [0], [rows], 2, 2, 4, 64, seed=2, tail=1), [rows], [keep], VALUES[name])
 
 
+@pytest.mark.parametrize("rows,keep,kinds", [(600001, 299999, 10 ** 9), (600001, 599990, 50), (530000, 17, 10 ** 9), (8193, 4000, 10 ** 9), (16385, 9000, 1)])
+def test_long_caches(rows, keep, kinds):
+    """More rows than a workgroup takes, and more than 64 times that many; ties across their shares."""
+    rng = np.random.default_rng(rows + keep)
+    page, Hkv = 128, 2
+    pages = -(-rows // page)
+    p = B.make_params(1, 1, Hkv, Hkv, 128, 4)
+    c = B.alloc_cache(p, pages, page, pages, fp4=True)
+    table = rng.permutation(pages).astype(np.int32)
+    c.tensors[4].copy_(up(table[None]))
+    for t in c.tensors[:4]:
+        t.copy_(torch.randint(0, 256, t.shape, dtype=torch.uint8, device="cuda"))
+    w = np.exp(rng.standard_normal((Hkv, rows)) * 4).astype(np.float32) if kinds > rows else rng.integers(0, kinds, (Hkv, rows)).astype(np.float32)
+    place = table[np.arange(rows) // page].astype(np.int64), np.arange(rows) % page
+    pool = np.zeros((pages, Hkv, page), np.float32)
+    for h in range(Hkv):
+        pool[place[0], h, place[1]] = w[h]
+    weight, kept = up(pool), torch.full((1, Hkv, rows), -9, dtype=torch.int32, device="cuda")
+    before = [t.cpu().numpy() for t in c.tensors[:4]]
+    B.l2a_cache_evict(p, c, up(np.array([rows], np.int32)), up(np.array([keep], np.int32)), rows, weight, weight, kept)
+    got, got_kept = weight.cpu().numpy(), kept.cpu().numpy()[0]
+    for h in range(Hkv):
+        stays = np.zeros(rows, bool)
+        stays[np.argsort(-w[h], kind="stable")[:keep]] = True
+        source = np.arange(keep)
+        source[~stays[:keep]] = keep + np.nonzero(stays[keep:])[0]
+        assert np.array_equal(got_kept[h, :keep], source) and (got_kept[h, keep:] == -9).all()
+        assert np.array_equal(got[place[0][:keep], h, place[1][:keep]], w[h][source])
+        assert np.array_equal(got[place[0][keep:], h, place[1][keep:]], w[h][keep:])
+        for t, x in zip(c.tensors[:4], before):
+            y = x.copy()
+            y[place[0][:keep], h, place[1][:keep]] = x[place[0][source], h, place[1][source]]
+            assert np.array_equal(t.cpu().numpy()[:, h], y[:, h])
+
+
 def test_sizes_out_of_range_are_clamped():
     s = make_step(16, [0, 0, 0], [40, 40, 40], 2, 2, 4, 16, seed=3, tail=1)
     check(s, [-5, 30, 2 ** 31 - 1], [7, -3, 16], spread, max_rows=40)
