@@ -7,9 +7,9 @@
 // Which rows stay is a radix selection over the weights' bits, ordered as whole numbers: the histogram of their highest bits says in which bin
 // the last row that stays lies, that of the bits below among the rows of this bin where in it, and so on.  Then the lists: places that become free, and
 // rows that move there, both ascending.
-//   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 8 bits a pass
+//   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 11, 11 and 10 bits
 //   evict_first_kernel, evict_second_kernel, evict_third_kernel, evict_list_kernel
-//                        more: a workgroup per 8192 rows (or 1/64), 11, 11 and 10 bits; each leaves its own histogram, and each workgroup of the next
+//                        more: a workgroup per 8192 rows (or 1/64); each leaves its own histogram, and each workgroup of the next
 //                        kernel adds up those of its KV head (no atomics on memory, nothing to clear)
 //   evict_move_kernel    the moves: K, V, exponents, weights
 #include "paged.hpp"
@@ -40,6 +40,7 @@ struct EvictArgs {
     int32_t *bins1, *bins2;  // [B * Hkv][segments][kBins1]
     int32_t* bins3;   // [B * Hkv][segments][2][kBins3]: of rows before the keep-th and behind
     int32_t* above;   // [B * Hkv][segments][2]: rows whose upper 22 bits say that they stay, before and behind
+    int32_t* chosen;  // [B * Hkv][4]: the bin of the first bits and the how-manieth in it, of the first two
 };
 
 __device__ __forceinline__ int rows_of(const EvictArgs& a, int b) { return plan::clamp(a.rows[b], 0, min(a.max_rows, a.c.capacity())); }
@@ -50,9 +51,6 @@ __device__ __forceinline__ uint32_t order(float w) {
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 __device__ __forceinline__ int page_at(const EvictArgs& a, int b, int row) { return a.c.table[(size_t)b * a.c.max_pages + (row >> a.c.page_log2)]; }
-__device__ __forceinline__ size_t row_at(const EvictArgs& a, int b, int hk, int row) {
-    return pool_row(a.c, a.gm.Hkv, plan::clamp(page_at(a, b, row), 0, a.c.pages - 1), hk, row);
-}
 
 struct Sizes {
     int pair, b, hk, n, m;
@@ -63,16 +61,26 @@ __device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int pair) {
     z.n = rows_of(a, z.b), z.m = plan::clamp(a.keep[z.b], 0, z.n);
     return z;
 }
-// Row i0 + 1024 j + thread of a block as order; 0 past the end.
+// Row i0 + 1024 j + thread of a block as order; 0 past the end.  Where the weights do not stay in place, those before the keep-th go to theirs (the moves
+// write over those that leave).
 __device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
     float w[kPer];
+    size_t row[kPer];
+    bool real[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = i0 + j * kSelectThreads + (int)threadIdx.x, page = i < z.n ? page_at(a, z.b, i) : 0;
+        real[j] = (unsigned)page < (unsigned)a.c.pages;
+        row[j] = pool_row(a.c, a.gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), z.hk, i);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) w[j] = i0 + j * kSelectThreads + (int)threadIdx.x < z.n ? a.weight_in[row[j]] : 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
-        w[j] = i < z.n ? a.weight_in[row_at(a, z.b, z.hk, i)] : 0.f;
+        x[j] = i < z.n ? order(w[j]) : 0u;
+        if (a.weight != a.weight_in && i < z.m && real[j]) a.weight[row[j]] = w[j];
     }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = i0 + j * kSelectThreads + (int)threadIdx.x < z.n ? order(w[j]) : 0u;
 }
 __device__ __forceinline__ void load_keys(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
     const uint32_t* const keys = a.keys + (size_t)z.pair * a.max_rows;
@@ -115,14 +123,16 @@ __device__ __forceinline__ void choose(Shared& sh, const int (&mine)[EACH], int 
     bin = sh.chosen[0], left = sh.chosen[1];
     __syncthreads();
 }
-// Places of flags among all of a block, in the order of rows: of this thread's j-th, how many lie before it; and how many there are.
-__device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], int (&at)[kPer]) {
+// Places of flags among all of a block, in the order of rows: of this thread's j-th, how many lie before it; and how many there are.  Two kinds of flags
+// at once, the second's numbers in the upper halves (a block has fewer than 2^16 rows).
+__device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], const bool (&other)[kPer], int (&at)[kPer]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    unsigned long long set[kPer];
+    const unsigned long long before = (1ull << lane) - 1ull;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        set[j] = __ballot(flag[j]);
-        if (lane == 0) sh.counts[j][wave] = __popcll(set[j]);
+        const unsigned long long set = __ballot(flag[j]), more = __ballot(other[j]);
+        at[j] = __popcll(set & before) + (__popcll(more & before) << 16);
+        if (lane == 0) sh.counts[j][wave] = __popcll(set) + (__popcll(more) << 16);
     }
     __syncthreads();
     // every wavefront adds up all counts: a lane those of two
@@ -139,7 +149,7 @@ __device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], int 
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = j * kWavesOf + wave;
-        at[j] = __shfl(upto - c0 - c1, i >> 1) + (i & 1 ? __shfl(c0, i >> 1) : 0) + __popcll(set[j] & ((1ull << lane) - 1ull));
+        at[j] += __shfl(upto - c0 - c1, i >> 1) + (i & 1 ? __shfl(c0, i >> 1) : 0);
     }
     const int total = __shfl(upto, 63);
     __syncthreads();
@@ -153,43 +163,32 @@ struct Before {
 __device__ __forceinline__ void list_block(const EvictArgs& a, Shared& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past) {
     int32_t *to = a.to + (size_t)z.pair * (a.max_rows / 2), *from = a.from + (size_t)z.pair * (a.max_rows / 2);
     int32_t* const kept = a.kept ? a.kept + (size_t)z.pair * a.max_rows : nullptr;
-    bool flag[kPer], stays[kPer];
+    bool flag[kPer], other[kPer], stays[kPer];
     int at[kPer];
     const bool all = z.m == z.n;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * kSelectThreads + (int)threadIdx.x < z.n;
-    const int equal = places(sh, flag, at);
+    for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * kSelectThreads + (int)threadIdx.x < z.n, other[j] = false;
+    const int equal = places(sh, flag, other, at);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
         stays[j] = i < z.n && (all || x[j] > found || (flag[j] && past.equal + at[j] < left));
-        flag[j] = i < z.m && !stays[j];
+        flag[j] = i < z.m && !stays[j], other[j] = i >= z.m && stays[j];
     }
-    const int holes = places(sh, flag, at);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-        if (flag[j]) to[past.holes + at[j]] = i0 + j * kSelectThreads + (int)threadIdx.x;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) flag[j] = i0 + j * kSelectThreads + (int)threadIdx.x >= z.m && stays[j];
-    const int movers = places(sh, flag, at);
+    const int both = places(sh, flag, other, at), holes = both & 0xffff, movers = both >> 16;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
-        if (flag[j]) from[past.movers + at[j]] = i;
-        if (i >= z.m || !stays[j]) continue;
-        if (kept) kept[i] = i;
-        if (a.weight != a.weight_in && (unsigned)page_at(a, z.b, i) < (unsigned)a.c.pages) {
-            const size_t row = row_at(a, z.b, z.hk, i);
-            a.weight[row] = a.weight_in[row];
-        }
+        if (flag[j]) to[past.holes + (at[j] & 0xffff)] = i;
+        if (other[j]) from[past.movers + (at[j] >> 16)] = i;
+        if (kept && i < z.m && stays[j]) kept[i] = i;
     }
     past = Before{past.equal + equal, past.holes + holes, past.movers + movers};
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-    constexpr int kBins = 256;
     __shared__ Shared sh;
-    __shared__ int bins[kBins];
+    __shared__ int bins[kBins1];
     const Sizes z = sizes_of(a, blockIdx.x);
     if (z.m == 0) {
         if (threadIdx.x == 0) a.moves[z.pair] = 0;
@@ -198,16 +197,21 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     uint32_t x[kPer], found = 0;
     load_block(a, z, 0, x);
     int left = z.m;
-    for (int shift = 24; shift >= 0 && z.m < z.n; shift -= 8) {
-        if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
+    const int highest = kBins1 - 1 - 2 * (int)threadIdx.x;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        if (z.m == z.n) break;
+        constexpr int kShift[3] = {21, 10, 0};
+        const int shift = kShift[pass], above = pass ? kShift[pass - 1] : 0;
+        bins[highest] = bins[highest - 1] = 0;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
-            if (j * kSelectThreads + (int)threadIdx.x < z.n && (shift == 24 || (x[j] >> (shift + 8)) == (found >> (shift + 8)))) atomicAdd(&bins[(x[j] >> shift) & 255], 1);
+            if (j * kSelectThreads + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins3 - 1 : kBins1 - 1)], 1);
         __syncthreads();
-        const int mine[1] = {threadIdx.x < kBins ? bins[kBins - 1 - threadIdx.x] : 0};
+        const int mine[2] = {bins[highest], bins[highest - 1]};
         int bin;
-        choose<1>(sh, mine, kBins - 1 - (int)threadIdx.x, bin, left);
+        choose<2>(sh, mine, highest, bin, left);
         found |= (uint32_t)bin << shift;
     }
     Before past{0, 0, 0};
@@ -267,7 +271,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a
     int32_t* const out = bins_at(a, a.bins1, z.pair, blockIdx.x);
     for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) out[i] = bins[i];
 }
-// The next 11 bits of rows in the bin found.
+// The next 11 bits of rows in the bin found.  (Its number is left for the kernels behind, by the first workgroup.)
 __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs a) {
     __shared__ Shared sh;
     __shared__ int bins[kBins1];
@@ -277,6 +281,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs 
     for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) bins[i] = 0;
     int left = z.m;
     const uint32_t first = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.chosen[z.pair * 4] = (int)first, a.chosen[z.pair * 4 + 1] = left;
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
         load_keys(a, z, i0, x);
@@ -297,9 +302,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(EvictArgs a
     if (g.i0 >= g.i1 || z.m == 0 || z.m == z.n) return;
     for (int i = threadIdx.x; i < 2 * kBins3; i += kSelectThreads) bins[i] = 0;
     if (threadIdx.x < 2) above[threadIdx.x] = 0;
-    int left = z.m;
-    uint32_t upper = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
-    upper = upper << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
+    int left = a.chosen[z.pair * 4 + 1];
+    const uint32_t upper = (uint32_t)a.chosen[z.pair * 4] << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.chosen[z.pair * 4 + 2] = (int)upper, a.chosen[z.pair * 4 + 3] = left;
     int mine[2] = {0, 0};
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
@@ -338,9 +343,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
     int left = 0;
     Before past{0, 0, 0};
     if (z.m < z.n) {
-        left = z.m;
-        uint32_t upper = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
-        upper = upper << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
+        const uint32_t upper = (uint32_t)a.chosen[z.pair * 4 + 2];
+        left = a.chosen[z.pair * 4 + 3];
         const int bin = kBins3 - 1 - (int)threadIdx.x;  // this thread's
         int mine[1] = {0};
 #pragma unroll 8
@@ -351,28 +355,23 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
         int lowest;
         choose<1>(sh, mine, bin, lowest, left);
         found = upper << 10 | (uint32_t)lowest;
-        if (threadIdx.x < 2 * kMostSegments) (&greater[0][0])[threadIdx.x] = 0;
-        __syncthreads();
-        // (before this one: counts of all of these)
-        for (int s = 0; s < (int)blockIdx.x; ++s) {
-            const int32_t* const p = bins_at(a, a.bins3, z.pair, s);
+        // a wavefront for each half of a segment before this one
+        const int lane = threadIdx.x & 63;
+        for (int i = threadIdx.x >> 6; i < 2 * (int)blockIdx.x; i += kSelectThreads / 64) {
+            const int32_t* const p = bins_at(a, a.bins3, z.pair, i >> 1) + (i & 1) * kBins3;
+            int more = lane == 0 ? a.above[((size_t)z.pair * a.segments + (i >> 1)) * 2 + (i & 1)] : 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int x = p[e * kBins3 + bin];
-                int more = bin > lowest ? x : 0;
+            for (int e = 0; e < kBins3 / 64; ++e) more += e * 64 + lane > lowest ? p[e * 64 + lane] : 0;
 #pragma unroll
-                for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
-                if ((threadIdx.x & 63) == 0 && more) atomicAdd(&greater[s][e], more);
-                if (bin == lowest) equal[s][e] = x;
-            }
+            for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
+            if (lane == 0) greater[i >> 1][i & 1] = more, equal[i >> 1][i & 1] = p[lowest];
         }
         __syncthreads();
         for (int s = 0; s < (int)blockIdx.x; ++s) {
-            const int32_t* const up = a.above + ((size_t)z.pair * a.segments + s) * 2;
             const int i0 = s * a.segment, i1 = i0 + a.segment, before = plan::clamp(z.m, i0, i1) - i0;  // rows of it before the keep-th
             const int e0 = plan::clamp(left - past.equal, 0, equal[s][0]), e1 = plan::clamp(left - past.equal - equal[s][0], 0, equal[s][1]);
-            past.holes += before - up[0] - greater[s][0] - e0;
-            past.movers += up[1] + greater[s][1] + e1;
+            past.holes += before - greater[s][0] - e0;
+            past.movers += greater[s][1] + e1;
             past.equal += equal[s][0] + equal[s][1];
         }
     }
@@ -447,6 +446,7 @@ size_t lay_out(EvictArgs& a, char* base) {
     take(a.bins2, pairs * a.segments * kBins1);
     take(a.bins3, pairs * a.segments * kBins1);
     take(a.above, pairs * a.segments * 2);
+    take(a.chosen, pairs * 4);
     return at;
 }
 
