@@ -306,14 +306,16 @@ def _token_rows(t: Optional[torch.Tensor], p: l2a_params, heads: int, device: in
     """-> address and token stride in elements of a tensor [B, T, heads, D] or [B T, heads, D] whose heads lie one behind the other."""
     if t is None:
         return None, 0
-    tokens = p.B * p.T
-    ok = t.dtype == torch_dtype(p) and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, p.D) and t.shape[0] == (tokens if t.dim() == 3 else p.B)
+    tokens, dtype = p.B * p.T, torch_dtype(p)
+    if t.is_contiguous() and t.dtype == dtype and t.numel() == tokens * heads * p.D and t.get_device() == device:
+        return t.data_ptr(), 0
+    ok = t.dtype == dtype and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, p.D) and t.shape[0] == (tokens if t.dim() == 3 else p.B)
     ok = ok and (t.dim() == 3 or t.shape[1] == p.T) and t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == p.D)
     if ok:
         stride = heads * p.D if tokens == 1 else t.stride(-3) if t.dim() == 3 or p.T > 1 else t.stride(0)
         ok = heads * p.D <= stride < 2 ** 31 and (t.dim() == 3 or p.B == 1 or p.T == 1 or t.stride(0) == p.T * stride)
     if not ok:
-        raise ValueError(f"{what} must be [{p.B}, {p.T}, {heads}, {p.D}] or [{tokens}, {heads}, {p.D}] {torch_dtype(p)} on the current device, with one stride from "
+        raise ValueError(f"{what} must be [{p.B}, {p.T}, {heads}, {p.D}] or [{tokens}, {heads}, {p.D}] {dtype} on the current device, with one stride from "
                          f"token to token and the heads of a token one behind the other; got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
     return t.data_ptr(), stride
 
@@ -324,12 +326,13 @@ def l2a_rope(p: l2a_params, r: l2a_rotary, q, k, pos, q_out, k_out) -> None:
     dev = torch.cuda.current_device()
     if r.device != dev:
         raise ValueError("the frequencies must be on the current device, whose stream the call is enqueued on")
-    call = l2a_rotary.from_buffer_copy(r)
-    q_at, call.q_stride = _token_rows(q, p, p.Hq, dev, "q")
-    k_at, call.k_stride = _token_rows(k, p, p.Hkv, dev, "k")
-    qo_at, call.q_out_stride = _token_rows(q_out, p, p.Hq, dev, "q_out")
-    ko_at, call.k_out_stride = _token_rows(k_out, p, p.Hkv, dev, "k_out")
-    rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(call), q_at, k_at, _packed(pos, torch.int32, r.axes * p.B * p.T, dev, "pos"), qo_at, ko_at,
+    q_at, qs = _token_rows(q, p, p.Hq, dev, "q")
+    k_at, ks = _token_rows(k, p, p.Hkv, dev, "k")
+    qo_at, qos = _token_rows(q_out, p, p.Hq, dev, "q_out")
+    ko_at, kos = _token_rows(k_out, p, p.Hkv, dev, "k_out")
+    if qs or ks or qos or kos:
+        r = l2a_rotary(r.axes, r.pairs, r.flags, qs, ks, qos, kos, r.freq)
+    rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(r), q_at, k_at, _packed(pos, torch.int32, r.axes * p.B * p.T, dev, "pos"), qo_at, ko_at,
                         torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         raise L2AError(rc, "l2a_rope")

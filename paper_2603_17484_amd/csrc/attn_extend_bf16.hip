@@ -622,23 +622,27 @@ __device__ __forceinline__ void store_sums(const ExtendArgs& a, const Out& o, in
 // A piece row by row and key by key: for those with keys that are not in every row's reach and with an infinity or a NaN in a sum.  It may
 // come from such a key's values, as a weight of zero does not keep it out of the other rows' sums.
 // (Looking for them among the values themselves, in the loops: 2.5 to 11 % of the main kernel's time.)
-template <int NW>
+template <int BITS, int NW>
 __device__ __forceinline__ void rows_alone(const ExtendArgs& a, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c4 = lane * 4;  // 32 lanes per row
     const int32_t* const table = a.c.table + (size_t)t.b * a.c.max_pages;
     const int b0 = (t.lo / kKeys + t.skip + piece.from) * kKeys, b1 = (t.lo / kKeys + t.skip + piece.to) * kKeys - 1;
     auto values = [&](const char* pool, const unsigned char* scales, size_t row) __attribute__((always_inline)) {
-        if (a.c.bits == 16) return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(pool + row * (kD * 2) + c4 * 2), f32x4);
-        const float e = exponent_value(scales[row * kRowScales + c4 / kScaleBlock]);
-        if (a.c.bits == 4) {
-            const uint32_t x = *reinterpret_cast<const uint16_t*>(pool + row * (kD / 2) + c4 / 2);
-            const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 0)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 1));
+        if constexpr (BITS == 16) {
+            return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(pool + row * (kD * 2) + c4 * 2), f32x4);
+        } else {
+            const float e = exponent_value(scales[row * kRowScales + c4 / kScaleBlock]);
+            bf16x2 lo, hi;
+            if constexpr (BITS == 8) {
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(pool + row * kD + c4);
+                lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, false)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, true));
+            } else {
+                const uint32_t x = *reinterpret_cast<const uint16_t*>(pool + row * (kD / 2) + c4 / 2);
+                lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 0)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, e, 1));
+            }
             return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
         }
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(pool + row * kD + c4);
-        const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, false)), hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, e, true));
-        return f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
     };
     for (int r = group; r < t.rows; r += 2 * NW) {
         const int code = row_code(a, t, t.first + r);
@@ -690,8 +694,11 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
     constexpr int kRows = 64 / BITS, kEach = kSub / kRows, kRowBytes = kD * BITS / 8;  // rows of an instruction, which lie in one page; instructions
     const int mine = load_row<BITS>(lane);
+    constexpr bool kDirect = BITS == 4;  // K goes straight into its operand: with 4 bits the way through shared memory took longer than the bytes
     u32x4 kx[BITS < 16 ? kEach : 1], vx[BITS < 16 ? kEach : 1];
     uint32_t kse[BITS < 16 ? kEach : 1], vse[BITS < 16 ? kEach : 1];
+    RawKeys<kDirect ? BITS : 16> keys_raw;
+    size_t key_row = 0;   // of this lane, in the pool
     size_t rows[kEach];   // where the instructions' rows begin in the pool, and how far behind that this lane's row is
     unsigned off[kEach];
     // keys out of the tile's repeat the nearest one in it (see Loader)
@@ -703,6 +710,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
                 const size_t row = pool_row(a.c, gm.Hkv, plan::clamp(table[(k0 + 16 * p) >> a.c.page_log2], 0, a.c.pages - 1), hk, k0 + 16 * p);
 #pragma unroll
                 for (int e = 0; e < kEach / 2; ++e) rows[p * (kEach / 2) + e] = row + e * kRows, off[p * (kEach / 2) + e] = mine;
+                if (kDirect && (n >> 4) == p) key_row = row + (n & 15);
             }
         } else {
 #pragma unroll
@@ -710,6 +718,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
                 const int first = plan::clamp(k0 + e * kRows, t.lo & -kRows, t.hi & -kRows);
                 rows[e] = pool_row(a.c, gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), hk, first);
                 off[e] = plan::clamp(k0 + e * kRows + mine, t.lo, t.hi) - first;
+                if (kDirect && n / kRows == e) key_row = rows[e] + plan::clamp(k0 + n, t.lo, t.hi) - first;
             }
         }
     };
@@ -730,15 +739,16 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     };
     if (sb0 < sb1) {
         find(sb0);
-        load(a.c.k, a.c.ks, kx, kse, k_to);
+        if constexpr (kDirect) keys_raw.load(a.c, key_row, h);
+        else load(a.c.k, a.c.ks, kx, kse, k_to);
         load(a.c.v, a.c.vs, vx, vse, v_to);
     }
     const int code = code_of(n), local_tok = code / G;
     const Range keys = plan::row_keys(t.kind, t.s.pos + local_tok, gm.W);
     bf16x8 qreg[8];
-    const __bf16* qp = a.q + ((size_t)(t.s.start + local_tok) * gm.Hq + hk * G + code - local_tok * G) * kD + 8 * h;
+    const __bf16* qp = a.q + ((size_t)(t.s.start + local_tok) * gm.Hq + hk * G + code - local_tok * G) * kD;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+    for (int ks = 0; ks < 8; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qp + (kDirect ? slot_channel<BITS>(ks, h) : ks * 16 + 8 * h));
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qreg[ks]));  // waited for here, and so not in the loop, behind its loads
     const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - gm.W - 1;
@@ -750,13 +760,18 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     for (int sb = sb0; sb < sb1; sb += NW) {
         const bool more = sb + NW < sb1;
         if (more) find(sb + NW);
-        if constexpr (BITS < 16) convert(kx, kse, k_to);
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
         bf16x8 op[8];
+        if constexpr (kDirect) keys_raw.get(h, op);
+        else if constexpr (BITS < 16) convert(kx, kse, k_to);
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");  // K; V, loaded after it, may be on its way still
+        if constexpr (kDirect) {
+            if (more) keys_raw.load(a.c, key_row, h);
+        } else {
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) op[ks] = k_operand(k_at, ks, 0);
-        if constexpr (BITS < 16) {
-            if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
+            for (int ks = 0; ks < 8; ++ks) op[ks] = k_operand(k_at, ks, 0);
+            if constexpr (BITS < 16) {
+                if (more) load(a.c.k, a.c.ks, kx, kse, k_to);
+            }
         }
         FENCE();
         f32x16 sc;
@@ -1106,7 +1121,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
         if (t.rows <= kSub) done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
         else if (t.rows <= kHalvesRows) done = some_rows<BITS, true>(a, lds, t, piece, w);
         else done = some_rows<BITS, false>(a, lds, t, piece, w);
-        if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
+        if (!__any(done)) rows_alone<BITS, kWaves>(a, t, piece, w);
     });
 }
 
@@ -1128,7 +1143,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
         bool done;
         if (FEW || t.rows <= kSub) done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
         else done = some_rows<BITS, true>(a, lds, t, piece, w);
-        if (!__any(done)) rows_alone<kWaves>(a, t, piece, w);
+        if (!__any(done)) rows_alone<BITS, kWaves>(a, t, piece, w);
     };
     if constexpr (!SELF) {
         for_pieces(a, rows);

@@ -57,40 +57,6 @@ struct WeightsArgs {
     int workgroups;
 };
 
-// Slot (ks, h) of the products over the channels: which eight channels it stands for, so that what a lane loads at once, 16 bytes of a row,
-// is whole slots of its own half h.
-template <int BITS>
-__device__ __forceinline__ int slot_channel(int ks, int h) {
-    constexpr int kVec = 128 / BITS, kSlots = kVec / 8;
-    return (ks / kSlots) * 2 * kVec + h * kVec + (ks % kSlots) * 8;
-}
-// A lane's bytes of its key, and the operand they become.
-template <int BITS>
-struct RawKeys {
-    static constexpr int kSlots = 16 / BITS, kLoads = 8 / kSlots;  // slots of a load
-    u32x4 x[kLoads];
-    uint32_t exponents;
-    __device__ __forceinline__ void load(const Pages& c, size_t row, int h) {
-        const char* const p = c.k + row * (kD * BITS / 8) + h * 16;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + i * 32);
-        if constexpr (BITS < 16) exponents = *reinterpret_cast<const uint32_t*>(c.ks + row * kRowScales);
-    }
-    __device__ __forceinline__ void get(int h, bf16x8 (&k)[8]) const {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if constexpr (BITS == 16) {
-                k[i] = __builtin_bit_cast(bf16x8, x[i]);
-            } else {
-                u32x4 y[kSlots];
-                dequantise<BITS>(x[i], exponent_value((exponents >> (BITS == 8 ? 8 * i : 8 * (2 * i + h))) & 0xffu), y);
-#pragma unroll
-                for (int j = 0; j < kSlots; ++j) k[i * kSlots + j] = __builtin_bit_cast(bf16x8, y[j]);
-            }
-        }
-    }
-};
-
 // ---------------------------------------------------------------------------------------
 // few rows
 // ---------------------------------------------------------------------------------------
@@ -259,8 +225,10 @@ __global__ __launch_bounds__(kPackThreads) void weights_pack_kernel(WeightsArgs 
         return total;
     };
     int earlier = 0;
-    for (int g = 0; g < G; ++g)
-        for (int t = threadIdx.x; t < t0; t += kPackThreads) earlier += counts(t, g);
+    for (int t = threadIdx.x; t < t0; t += kPackThreads) {
+#pragma unroll
+        for (int g = 0; g < 16; ++g) earlier += counts(t, min(g, G - 1)) && g < G;  // loads that do not wait for one another
+    }
     const int first = all(earlier);
     // a thread per row, in order
     const int t = t0 + (int)threadIdx.x / G, g = (int)threadIdx.x % G;
@@ -433,7 +401,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_many_kernel(WeightsArg
             if (count > 0) issue(0);
             if (count > 1) issue(1);
             float sum[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            // tiles whose rows all see the whole chunk: from the one behind the last whose first row does not, to the last whole one
+            // (The weights of a tile between the matrix instructions of the next, slot by slot, take as long: the chip's clock falls with what it does at once.)
             for (int t = 0; t < count; ++t) {
                 if (t + 1 < count) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
                 else dma_wait();

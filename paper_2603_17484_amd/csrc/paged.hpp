@@ -62,4 +62,38 @@ __device__ __forceinline__ void dequantise(const u32x4& x, float scale, u32x4 (&
     }
 }
 
+// Keys that go straight from memory into an operand of the matrix instructions, a lane a key's row (or, with h, half of it).  Slot (ks, h) of the
+// products over the channels stands for eight channels from here on, so that what a lane loads at once, 16 bytes of a row, is whole slots of its half.
+template <int BITS>
+__device__ __forceinline__ int slot_channel(int ks, int h) {
+    constexpr int kVec = 128 / BITS, kSlots = kVec / 8;
+    return (ks / kSlots) * 2 * kVec + h * kVec + (ks % kSlots) * 8;
+}
+// A lane's bytes of its key, and the operand they become.
+template <int BITS>
+struct RawKeys {
+    static constexpr int kSlots = 16 / BITS, kLoads = 8 / kSlots;  // slots of a load
+    u32x4 x[kLoads];
+    uint32_t exponents;
+    __device__ __forceinline__ void load(const Pages& c, size_t row, int h) {
+        const char* const p = c.k + row * (kD * BITS / 8) + h * 16;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + i * 32);
+        if constexpr (BITS < 16) exponents = *reinterpret_cast<const uint32_t*>(c.ks + row * kRowScales);
+    }
+    __device__ __forceinline__ void get(int h, bf16x8 (&k)[8]) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if constexpr (BITS == 16) {
+                k[i] = __builtin_bit_cast(bf16x8, x[i]);
+            } else {
+                u32x4 y[kSlots];
+                dequantise<BITS>(x[i], exponent_value((exponents >> (BITS == 8 ? 8 * i : 8 * (2 * i + h))) & 0xffu), y);
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) k[i * kSlots + j] = __builtin_bit_cast(bf16x8, y[j]);
+            }
+        }
+    }
+};
+
 }  // namespace l2a
