@@ -43,36 +43,49 @@ __device__ __forceinline__ int block_exponent(float amax) {
     return min(max(e, kMinExponent<BITS>), kMaxExponent<BITS>);
 }
 
-// A row is 16 lanes of 8 channels (bf16) or 8 of 16 (e4m3, e2m1); a group of them takes ROWS tokens of a KV head, whose loads are on their
+// A row is 16 lanes of 8 channels (bf16), 8 of 16 (e4m3), or 8 of twice 8, one in each half of the row (e2m1: what the lanes store of packed rows at once
+// are whole lines of memory, 75 us for 89 at 65536 tokens); a group of them takes ROWS tokens of a KV head, whose loads are on their
 // way together, and groups side by side the KV heads: packed rows are read or written as they lie, and ROWS rows of a page are one run.
 // blockIdx.y: K or V.  65536 tokens of 8 KV heads out of an e4m3 cache (407 MB) with ROWS = 1 and 8 channels a lane: 139 us.
 template <int BITS, bool READ, int ROWS>
 __global__ __launch_bounds__(kThreads) void cache_rows_kernel(RowsArgs a) {
-    constexpr int kLanes = BITS < 16 ? 8 : 16, kRowBytes = kD * BITS / 8, kMine = kRowBytes / kLanes;  // bytes of a row in the cache, a lane's
-    typedef std::conditional_t<BITS == 4, u32x2, u32x4> Mine;
+    constexpr int kLanes = BITS < 16 ? 8 : 16, kRowBytes = kD * BITS / 8;
     const Geom& gm = a.gm;
     const long long unit = (long long)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
     const int c = threadIdx.x % kLanes, block = (int)(unit / gm.Hkv), hk = (int)(unit - (long long)block * gm.Hkv);
-    char* const packed = (blockIdx.y ? a.v : a.k) + c * (BITS < 16 ? 32 : 16);
-    char* const pool = (blockIdx.y ? a.c.v : a.c.k) + c * kMine;
-    unsigned char* const scales = (blockIdx.y ? a.c.vs : a.c.ks) + (c >> 1);
+    char* const packed = (blockIdx.y ? a.v : a.k) + c * (BITS == 8 ? 32 : 16);
+    char* const pool = (blockIdx.y ? a.c.v : a.c.k) + c * (BITS == 4 ? 4 : 16);
+    unsigned char* const scales = (blockIdx.y ? a.c.vs : a.c.ks) + (BITS == 4 ? c >> 2 : c >> 1);
     size_t at[ROWS], row[ROWS];  // rows of the pool, and packed
     bool on[ROWS];
-    int b = -1;
+    long long place[ROWS];       // of the rows in their sequences
+    int page[ROWS];
+    // Most groups lie in one sequence, which is looked for once; the table's entries are then on their way together.  (One row's lookups behind the
+    // other's: 65536 tokens of 8 KV heads out of a cache in 4 bits 96 us for 89.)
+    int b = block * ROWS < gm.T ? seq_of(a, block * ROWS) : -1;
+    int start = 0, end = 0;
+    long long first = 0;
+    auto enter = [&]() __attribute__((always_inline)) {
+        if (b >= 0) start = a.seq_start[b], end = a.seq_start[b + 1], first = a.pos[b];
+    };
+    enter();
+    size_t entry[ROWS];
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
         const int tok = block * ROWS + j;
-        on[j] = false, at[j] = 0, row[j] = 0;
-        if (tok >= gm.T) continue;
-        if (b < 0 || tok >= a.seq_start[b + 1]) b = seq_of(a, tok);
-        if (b < 0) continue;
+        if (tok < gm.T && (b < 0 || tok >= end)) b = seq_of(a, tok), enter();
         // places outside the table, and page numbers outside the pool, are never followed
-        const long long t = (long long)a.pos[b] + tok - a.seq_start[b];
-        if (t < 0 || t >= a.c.capacity()) continue;
-        const int page = a.c.table[(size_t)b * a.c.max_pages + (int)(t >> a.c.page_log2)];
-        on[j] = page >= 0 && page < a.c.pages;
-        at[j] = on[j] ? pool_row(a.c, gm.Hkv, page, hk, (int)t) : 0;
+        place[j] = first + tok - start;
+        on[j] = tok < gm.T && b >= 0 && place[j] >= 0 && place[j] < a.c.capacity();
+        entry[j] = on[j] ? (size_t)b * a.c.max_pages + (int)(place[j] >> a.c.page_log2) : 0;
         row[j] = (size_t)tok * gm.Hkv + hk;
+    }
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) page[j] = a.c.table[entry[j]];
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        on[j] = on[j] && page[j] >= 0 && page[j] < a.c.pages;
+        at[j] = on[j] ? pool_row(a.c, gm.Hkv, page[j], hk, (int)place[j]) : 0;
     }
     if constexpr (BITS == 16) {
         u32x4 x[ROWS];
@@ -82,22 +95,62 @@ __global__ __launch_bounds__(kThreads) void cache_rows_kernel(RowsArgs a) {
 #pragma unroll
         for (int j = 0; j < ROWS; ++j)
             if (on[j]) *reinterpret_cast<u32x4*>(READ ? packed + row[j] * (kD * 2) : pool + at[j] * (kD * 2)) = x[j];
+    } else if constexpr (READ && BITS == 4) {
+        uint32_t y[ROWS][2];
+        unsigned e[ROWS][2];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+            if (on[j]) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) y[j][i] = *reinterpret_cast<const uint32_t*>(pool + at[j] * kRowBytes + i * (kRowBytes / 2)), e[j][i] = scales[at[j] * kRowScales + 2 * i];
+            }
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+            if (on[j]) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) dequantise8(y[j][i], exponent_value(e[j][i]), *reinterpret_cast<u32x4*>(packed + row[j] * (kD * 2) + i * kD));
+            }
+    } else if constexpr (BITS == 4) {
+        bf16x8 x[ROWS][2];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+            if (on[j]) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[j][i] = *reinterpret_cast<const bf16x8*>(packed + row[j] * (kD * 2) + i * kD);
+            }
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float f[8], amax = 0.f;
+                int none = 0;  // something that is no finite number
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] = on[j] ? (float)x[j][i][k] : 0.f, amax = fmaxf(amax, fabsf(f[k])), none |= !(fabsf(f[k]) < INFINITY);
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o)), none |= __shfl_xor(none, o);  // the block's other lanes
+                if (!on[j]) continue;
+                const int e = block_exponent<4>(amax);
+                const float inv = exponent_value(127 - e);  // (multiplied first: 2^-e itself rounds nothing, of subnormal numbers either)
+                // (magnitudes beyond 6 2^kMaxExponent become that)
+                uint32_t y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0] * inv, f[1] * inv, 1.f, 0);
+                y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, f[2] * inv, f[3] * inv, 1.f, 1);
+                y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, f[4] * inv, f[5] * inv, 1.f, 2);
+                y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, f[6] * inv, f[7] * inv, 1.f, 3);
+                *reinterpret_cast<uint32_t*>(pool + at[j] * kRowBytes + i * (kRowBytes / 2)) = y;
+                if ((c & 3) == 0) scales[at[j] * kRowScales + 2 * i] = (unsigned char)(none ? 255 : e + 127);
+            }
+        }
     } else if constexpr (READ) {
-        Mine y[ROWS];
+        u32x4 y[ROWS];
         unsigned e[ROWS];
 #pragma unroll
         for (int j = 0; j < ROWS; ++j)
-            if (on[j]) y[j] = *reinterpret_cast<const Mine*>(pool + at[j] * kRowBytes), e[j] = scales[at[j] * kRowScales];
+            if (on[j]) y[j] = *reinterpret_cast<const u32x4*>(pool + at[j] * kD), e[j] = scales[at[j] * kRowScales];
 #pragma unroll
         for (int j = 0; j < ROWS; ++j)
             if (on[j]) {
                 u32x4 x[2];
-                if constexpr (BITS == 8) {
-                    dequantise<8>(y[j], exponent_value(e[j]), x);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) dequantise8(y[j][i], exponent_value(e[j]), x[i]);
-                }
+                dequantise<8>(y[j], exponent_value(e[j]), x);
                 u32x4* const out = reinterpret_cast<u32x4*>(packed + row[j] * (kD * 2));
                 out[0] = x[0], out[1] = x[1];
             }
@@ -115,42 +168,21 @@ __global__ __launch_bounds__(kThreads) void cache_rows_kernel(RowsArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) f[i] = on[j] ? (float)x[j][i >> 3][i & 7] : 0.f, amax = fmaxf(amax, fabsf(f[i]));
             amax = fmaxf(amax, __shfl_xor(amax, 1));  // the block's other half
-            if constexpr (BITS == 4) {
-                int none = 0;  // an element that is no finite number
+            if (!on[j]) continue;
+            const int e = block_exponent<8>(amax);
+            const float inv = exponent_value(127 - e), most = 448.f * exponent_value(127 + kMaxExponent<8>);
+            if (e == kMaxExponent<8>) {  // bf16 reaches 2^128 (1 - 2^-8), beyond what an element stands for at most, 1.75 2^127
 #pragma unroll
-                for (int i = 0; i < 16; ++i) none |= !(fabsf(f[i]) < INFINITY);
-                none |= __shfl_xor(none, 1);
-                if (!on[j]) continue;
-                const int e = block_exponent<4>(amax);
-                const float inv = exponent_value(127 - e);  // (multiplied first: 2^-e itself rounds nothing, of subnormal numbers either)
-                u32x2 y;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {  // magnitudes beyond 6 2^kMaxExponent become that
-                    const float* const x = f + 8 * i;
-                    unsigned w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0] * inv, x[1] * inv, 1.f, 0);
-                    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.f, 1);
-                    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4] * inv, x[5] * inv, 1.f, 2);
-                    y[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inv, x[7] * inv, 1.f, 3);
-                }
-                *reinterpret_cast<u32x2*>(pool + at[j] * kRowBytes) = y;
-                if ((c & 1) == 0) scales[at[j] * kRowScales] = (unsigned char)(none ? 255 : e + 127);
-            } else {
-                if (!on[j]) continue;
-                const int e = block_exponent<8>(amax);
-                const float inv = exponent_value(127 - e), most = 448.f * exponent_value(127 + kMaxExponent<8>);
-                if (e == kMaxExponent<8>) {  // bf16 reaches 2^128 (1 - 2^-8), beyond what an element stands for at most, 1.75 2^127
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) f[i] = fabsf(f[i]) < INFINITY ? fminf(fmaxf(f[i], -most), most) : __builtin_nanf("");
-                }
-                u32x4 y;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i] * inv, f[4 * i + 1] * inv, 0, false);
-                    y[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2] * inv, f[4 * i + 3] * inv, w, true);
-                }
-                *reinterpret_cast<u32x4*>(pool + at[j] * kD) = y;
-                if ((c & 1) == 0) scales[at[j] * kRowScales] = (unsigned char)(e + 127);
+                for (int i = 0; i < 16; ++i) f[i] = fabsf(f[i]) < INFINITY ? fminf(fmaxf(f[i], -most), most) : __builtin_nanf("");
             }
+            u32x4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i] * inv, f[4 * i + 1] * inv, 0, false);
+                y[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2] * inv, f[4 * i + 3] * inv, w, true);
+            }
+            *reinterpret_cast<u32x4*>(pool + at[j] * kD) = y;
+            if ((c & 1) == 0) scales[at[j] * kRowScales] = (unsigned char)(e + 127);
         }
     }
 }
