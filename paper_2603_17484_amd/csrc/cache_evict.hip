@@ -8,9 +8,10 @@
 // the last row that stays lies, that of the bits below among the rows of this bin where in it, and so on.  Then the lists: places that become free, and
 // rows that move there, both ascending.
 //   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 11, 11 and 10 bits
-//   evict_first_kernel, evict_second_kernel, evict_third_kernel, evict_list_kernel
-//                        more: a workgroup per 8192 rows (or 1/64); each leaves its own histogram, and each workgroup of the next
-//                        kernel adds up those of its KV head (no atomics on memory, nothing to clear)
+//   evict_first_kernel, evict_second_kernel, evict_list_kernel
+//                        more: a workgroup per 8192 rows (or 1/64).  The first leaves the histogram of its rows' highest 11 bits; each of the second adds up
+//                        those of its KV head and lists its rows in the bin found; each of the third takes all of these into shared memory,
+//                        so that it knows by itself which rows stay and what comes before its own on the lists (no atomics on memory, nothing to clear)
 //   evict_move_kernel    the moves: K, V, exponents, weights
 #include "paged.hpp"
 
@@ -21,7 +22,14 @@ constexpr int kSelectThreads = 1024;
 constexpr int kPer = 8;                          // rows of a thread
 constexpr int kBlock = kSelectThreads * kPer;
 constexpr int kMostSegments = 64;                // workgroups of a KV head of a sequence
-constexpr int kBins1 = 2048, kBins3 = 1024;      // 11, 11 and 10 bits
+constexpr int kBins = 2 * kSelectThreads;        // 11 bits; the last 10 leave half of them empty
+constexpr int kCandidates = 6144;                // rows of a bin in shared memory
+
+struct Counts {
+    int bin, left;     // the bin of the first bits in which the last row that stays lies, and the how-manieth in it that is
+    int listed;        // rows of the segment in it
+    int greater[2];    // rows that stay for their first bits, before the keep-th row and behind
+};
 
 struct EvictArgs {
     Geom gm;
@@ -36,11 +44,11 @@ struct EvictArgs {
     int32_t *to, *from;  // [B * Hkv][max_rows / 2]
     // of calls with more than kBlock rows
     int segments, segment;  // of a KV head of a sequence; rows of each, whole blocks
-    uint32_t* keys;   // [B * Hkv][max_rows] order of the weights
-    int32_t *bins1, *bins2;  // [B * Hkv][segments][kBins1]
-    int32_t* bins3;   // [B * Hkv][segments][2][kBins3]: of rows before the keep-th and behind
-    int32_t* above;   // [B * Hkv][segments][2]: rows whose upper 22 bits say that they stay, before and behind
-    int32_t* chosen;  // [B * Hkv][4]: the bin of the first bits and the how-manieth in it, of the first two
+    int stride;       // of keys: segments x segment
+    uint32_t* keys;   // [B * Hkv][stride] order of the weights
+    int32_t* bins;    // [B * Hkv][segments][kBins]
+    Counts* counts;   // [B * Hkv][segments]
+    u32x2* listed;    // [B * Hkv][stride] a segment's rows in the bin of the first bits: order, row
 };
 
 __device__ __forceinline__ int rows_of(const EvictArgs& a, int b) { return plan::clamp(a.rows[b], 0, min(a.max_rows, a.c.capacity())); }
@@ -82,13 +90,10 @@ __device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, i
         if (a.weight != a.weight_in && i < z.m && real[j]) a.weight[row[j]] = w[j];
     }
 }
+// The same of a block whose order was left in memory (segments are whole blocks).
 __device__ __forceinline__ void load_keys(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
-    const uint32_t* const keys = a.keys + (size_t)z.pair * a.max_rows;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
-        x[j] = i < z.n ? keys[i] : 0u;
-    }
+    for (int j = 0; j < kPer; ++j) x[j] = a.keys[(size_t)z.pair * a.stride + i0 + j * kSelectThreads + (int)threadIdx.x];
 }
 
 struct Shared {
@@ -188,7 +193,7 @@ __device__ __forceinline__ void list_block(const EvictArgs& a, Shared& sh, const
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
     __shared__ Shared sh;
-    __shared__ int bins[kBins1];
+    __shared__ int bins[kBins];
     const Sizes z = sizes_of(a, blockIdx.x);
     if (z.m == 0) {
         if (threadIdx.x == 0) a.moves[z.pair] = 0;
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     uint32_t x[kPer], found = 0;
     load_block(a, z, 0, x);
     int left = z.m;
-    const int highest = kBins1 - 1 - 2 * (int)threadIdx.x;
+    const int highest = kBins - 1 - 2 * (int)threadIdx.x;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         if (z.m == z.n) break;
@@ -207,7 +212,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
-            if (j * kSelectThreads + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins3 - 1 : kBins1 - 1)], 1);
+            if (j * kSelectThreads + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins / 2 - 1 : kBins - 1)], 1);
         __syncthreads();
         const int mine[2] = {bins[highest], bins[highest - 1]};
         int bin;
@@ -225,35 +230,15 @@ struct Segment {
 };
 __device__ __forceinline__ Segment segment_of(const EvictArgs& a, const Sizes& z) {
     const long long i0 = (long long)blockIdx.x * a.segment;
-    Segment g;
-    g.i0 = i0 < z.n ? (int)i0 : z.n, g.i1 = i0 + a.segment < z.n ? (int)(i0 + a.segment) : z.n;
-    return g;
+    return Segment{i0 < z.n ? (int)i0 : z.n, i0 + a.segment < z.n ? (int)(i0 + a.segment) : z.n};
 }
-__device__ __forceinline__ int32_t* bins_at(const EvictArgs& a, int32_t* bins, int pair, int segment) { return bins + ((size_t)pair * a.segments + segment) * kBins1; }
-// Segments that have rows.
-__device__ __forceinline__ int segments_of(const EvictArgs& a, const Sizes& z) { return (z.n + a.segment - 1) / a.segment; }
-// The bin of a pair's histograms, all segments together, in which the left-th row lies.
-__device__ __forceinline__ int choose_bin(const EvictArgs& a, Shared& sh, const Sizes& z, int32_t* bins, int& left) {
-    int mine[2] = {0, 0};
-    const int highest = kBins1 - 1 - 2 * (int)threadIdx.x, of = segments_of(a, z);
-#pragma unroll 8
-    for (int g = 0; g < of; ++g) {
-        const int32_t* const p = bins_at(a, bins, z.pair, g);
-        mine[0] += p[highest], mine[1] += p[highest - 1];
-    }
-    int bin;
-    choose<2>(sh, mine, highest, bin, left);
-    return bin;
-}
-static_assert(kBins1 == 2 * kSelectThreads && 2 * kBins3 == kBins1, "bins of a thread");
 
-// The highest 11 bits, and the order of all rows for the kernels behind.
 __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a) {
-    __shared__ int bins[kBins1];
+    __shared__ int bins[kBins];
     const Sizes z = sizes_of(a, blockIdx.y);
     const Segment g = segment_of(a, z);
     if (g.i0 >= g.i1) return;
-    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) bins[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
     __syncthreads();
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
@@ -261,124 +246,160 @@ __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
-            if (i < z.n) {
-                a.keys[(size_t)z.pair * a.max_rows + i] = x[j];
-                atomicAdd(&bins[x[j] >> 21], 1);
-            }
+            a.keys[(size_t)z.pair * a.stride + i] = x[j];  // (a segment is whole blocks)
+            if (i < z.n) atomicAdd(&bins[x[j] >> 21], 1);
         }
     }
     __syncthreads();
-    int32_t* const out = bins_at(a, a.bins1, z.pair, blockIdx.x);
-    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) out[i] = bins[i];
+    int32_t* const out = a.bins + ((size_t)z.pair * a.segments + blockIdx.x) * kBins;
+    for (int i = threadIdx.x; i < kBins; i += kSelectThreads) out[i] = bins[i];
 }
-// The next 11 bits of rows in the bin found.  (Its number is left for the kernels behind, by the first workgroup.)
+
 __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs a) {
     __shared__ Shared sh;
-    __shared__ int bins[kBins1];
+    __shared__ int count, greater[2];
     const Sizes z = sizes_of(a, blockIdx.y);
     const Segment g = segment_of(a, z);
     if (g.i0 >= g.i1 || z.m == 0 || z.m == z.n) return;
-    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) bins[i] = 0;
-    int left = z.m;
-    const uint32_t first = (uint32_t)choose_bin(a, sh, z, a.bins1, left);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.chosen[z.pair * 4] = (int)first, a.chosen[z.pair * 4 + 1] = left;
-    for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
-        uint32_t x[kPer];
-        load_keys(a, z, i0, x);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j)
-            if (i0 + j * kSelectThreads + (int)threadIdx.x < z.n && (x[j] >> 21) == first) atomicAdd(&bins[(x[j] >> 10) & (kBins1 - 1)], 1);
+    if (threadIdx.x == 0) count = greater[0] = greater[1] = 0;
+    const int highest = kBins - 1 - 2 * (int)threadIdx.x, of = (z.n + a.segment - 1) / a.segment;
+    int sums[2] = {0, 0}, bin, left = z.m, mine[2] = {0, 0};
+#pragma unroll 8
+    for (int s = 0; s < of; ++s) {
+        const int32_t* const p = a.bins + ((size_t)z.pair * a.segments + s) * kBins;
+        sums[0] += p[highest], sums[1] += p[highest - 1];
     }
-    __syncthreads();
-    int32_t* const out = bins_at(a, a.bins2, z.pair, blockIdx.x);
-    for (int i = threadIdx.x; i < kBins1; i += kSelectThreads) out[i] = bins[i];
-}
-// The last 10, rows before the keep-th and behind apart, and how many of either stay for their higher bits.
-__global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(EvictArgs a) {
-    __shared__ Shared sh;
-    __shared__ int bins[2 * kBins3], above[2];
-    const Sizes z = sizes_of(a, blockIdx.y);
-    const Segment g = segment_of(a, z);
-    if (g.i0 >= g.i1 || z.m == 0 || z.m == z.n) return;
-    for (int i = threadIdx.x; i < 2 * kBins3; i += kSelectThreads) bins[i] = 0;
-    if (threadIdx.x < 2) above[threadIdx.x] = 0;
-    int left = a.chosen[z.pair * 4 + 1];
-    const uint32_t upper = (uint32_t)a.chosen[z.pair * 4] << 11 | (uint32_t)choose_bin(a, sh, z, a.bins2, left);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.chosen[z.pair * 4 + 2] = (int)upper, a.chosen[z.pair * 4 + 3] = left;
-    int mine[2] = {0, 0};
+    choose<2>(sh, sums, highest, bin, left);
+    u32x2* const listed = a.listed + (size_t)z.pair * a.stride + g.i0;
+    const int lane = threadIdx.x & 63;
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
         load_keys(a, z, i0, x);
+        unsigned long long set[kPer];
+        int all = 0, at = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            const int i = i0 + j * kSelectThreads + (int)threadIdx.x, behind = i >= z.m;
-            if (i >= z.n) continue;
-            if ((x[j] >> 10) == upper) atomicAdd(&bins[behind * kBins3 + (int)(x[j] & (kBins3 - 1))], 1);
-            if ((x[j] >> 10) > upper) mine[0] += !behind, mine[1] += behind;
+            const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+            const bool more = i < z.n && (int)(x[j] >> 21) > bin;
+            mine[0] += more && i < z.m, mine[1] += more && i >= z.m;
+            set[j] = __ballot(i < z.n && (int)(x[j] >> 21) == bin);
+            all += __popcll(set[j]);
+        }
+        if (lane == 0) at = atomicAdd(&count, all);
+        at = __shfl(at, 0);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {  // (in any order)
+            if (set[j] >> lane & 1) listed[at + __popcll(set[j] & ((1ull << lane) - 1ull))] = u32x2{x[j], (uint32_t)(i0 + j * kSelectThreads + (int)threadIdx.x)};
+            at += __popcll(set[j]);
         }
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) mine[e] += __shfl_xor(mine[e], o);
-        if ((threadIdx.x & 63) == 0) atomicAdd(&above[e], mine[e]);
+        if (lane == 0) atomicAdd(&greater[e], mine[e]);
     }
     __syncthreads();
-    int32_t* const out = bins_at(a, a.bins3, z.pair, blockIdx.x);
-    for (int i = threadIdx.x; i < 2 * kBins3; i += kSelectThreads) out[i] = bins[i];
-    if (threadIdx.x < 2) a.above[((size_t)z.pair * a.segments + blockIdx.x) * 2 + threadIdx.x] = above[threadIdx.x];
+    if (threadIdx.x == 0) a.counts[(size_t)z.pair * a.segments + blockIdx.x] = Counts{bin, left, count, {greater[0], greater[1]}};
 }
-// The lists.  What the segments before have of them follows from their histograms.
+
 __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a) {
     __shared__ Shared sh;
-    __shared__ int greater[kMostSegments][2], equal[kMostSegments][2];  // of each segment, before the keep-th row and behind
+    __shared__ int bins[kBins], ends[kMostSegments], past_counts[4];
+    __shared__ u32x2 candidates[kCandidates];
     const Sizes z = sizes_of(a, blockIdx.y);
     const Segment g = segment_of(a, z);
-    const int of = segments_of(a, z);
     if (z.m == 0 || g.i0 >= g.i1) {
         if (blockIdx.x == 0 && threadIdx.x == 0) a.moves[z.pair] = 0;
         return;
     }
+    const int of = (z.n + a.segment - 1) / a.segment, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t own[kPer];
+    load_keys(a, z, g.i0, own);  // (on their way until the lists)
     uint32_t found = 0;
     int left = 0;
     Before past{0, 0, 0};
     if (z.m < z.n) {
-        const uint32_t upper = (uint32_t)a.chosen[z.pair * 4 + 2];
-        left = a.chosen[z.pair * 4 + 3];
-        const int bin = kBins3 - 1 - (int)threadIdx.x;  // this thread's
-        int mine[1] = {0};
-#pragma unroll 8
-        for (int s = 0; s < of; ++s) {
-            const int32_t* const p = bins_at(a, a.bins3, z.pair, s);
-            mine[0] += p[bin] + p[kBins3 + bin];
-        }
-        int lowest;
-        choose<1>(sh, mine, bin, lowest, left);
-        found = upper << 10 | (uint32_t)lowest;
-        // a wavefront for each half of a segment before this one
-        const int lane = threadIdx.x & 63;
-        for (int i = threadIdx.x >> 6; i < 2 * (int)blockIdx.x; i += kSelectThreads / 64) {
-            const int32_t* const p = bins_at(a, a.bins3, z.pair, i >> 1) + (i & 1) * kBins3;
-            int more = lane == 0 ? a.above[((size_t)z.pair * a.segments + (i >> 1)) * 2 + (i & 1)] : 0;
+        const Counts* const counts = a.counts + (size_t)z.pair * a.segments;
+        left = counts[0].left;
+        found = (uint32_t)counts[0].bin << 21;
+        if (wave == 0) {  // a lane a segment
+            const bool on = lane < of, before = lane < (int)blockIdx.x;
+            int upto = on ? counts[lane].listed : 0, greater[2] = {before ? counts[lane].greater[0] : 0, before ? counts[lane].greater[1] : 0};
 #pragma unroll
-            for (int e = 0; e < kBins3 / 64; ++e) more += e * 64 + lane > lowest ? p[e * 64 + lane] : 0;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
-            if (lane == 0) greater[i >> 1][i & 1] = more, equal[i >> 1][i & 1] = p[lowest];
+            for (int o = 1; o < 64; o <<= 1) {
+                const int below = __shfl_up(upto, o);
+                if (lane >= o) upto += below;
+                greater[0] += __shfl_xor(greater[0], o), greater[1] += __shfl_xor(greater[1], o);
+            }
+            if (on) ends[lane] = upto;
+            if (lane < 2) past_counts[lane] = greater[lane], past_counts[2 + lane] = 0;
         }
         __syncthreads();
-        for (int s = 0; s < (int)blockIdx.x; ++s) {
-            const int i0 = s * a.segment, i1 = i0 + a.segment, before = plan::clamp(z.m, i0, i1) - i0;  // rows of it before the keep-th
-            const int e0 = plan::clamp(left - past.equal, 0, equal[s][0]), e1 = plan::clamp(left - past.equal - equal[s][0], 0, equal[s][1]);
-            past.holes += before - greater[s][0] - e0;
-            past.movers += greater[s][1] + e1;
-            past.equal += equal[s][0] + equal[s][1];
+        const int in = ends[of - 1];
+        // the rows in the bin, a wavefront a segment: f(order and row, place among all)
+        auto all = [&](auto&& f) __attribute__((always_inline)) {
+            constexpr int kAhead = 4;
+            for (int s = wave; s < of; s += kSelectThreads / 64) {
+                const u32x2* const listed = a.listed + (size_t)z.pair * a.stride + (size_t)s * a.segment;
+                const int first = s ? ends[s - 1] : 0, n = ends[s] - first;
+                for (int k0 = lane; k0 < n; k0 += 64 * kAhead) {
+                    u32x2 x[kAhead];
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j) x[j] = listed[min(k0 + 64 * j, n - 1)];
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)
+                        if (k0 + 64 * j < n) f(x[j], first + k0 + 64 * j);
+                }
+            }
+        };
+        const bool fits = in <= kCandidates;  // (else: many rows of nearly the same weight)
+        if (fits) all([&](const u32x2& x, int at) __attribute__((always_inline)) { candidates[at] = x; });
+        __syncthreads();
+        auto some = [&](auto&& f) __attribute__((always_inline)) {
+            if (fits) {
+                for (int at = threadIdx.x; at < in; at += kSelectThreads) f(candidates[at][0], (int)candidates[at][1]);
+            } else {
+                all([&](const u32x2& x, int) __attribute__((always_inline)) { f(x[0], (int)x[1]); });
+            }
+        };
+        const int highest = kBins - 1 - 2 * (int)threadIdx.x;
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+            const int above = pass ? 10 : 21, shift = pass ? 0 : 10;
+            bins[highest] = bins[highest - 1] = 0;
+            __syncthreads();
+            some([&](uint32_t x, int) __attribute__((always_inline)) {
+                if ((x >> above) == (found >> above)) atomicAdd(&bins[(x >> shift) & ((1u << (above - shift)) - 1u)], 1);
+            });
+            __syncthreads();
+            const int here[2] = {bins[highest], bins[highest - 1]};
+            int bin;
+            choose<2>(sh, here, highest, bin, left);
+            found |= (uint32_t)bin << shift;
         }
+        int greater[2] = {0, 0}, equal[2] = {0, 0};  // of the segments before, before the keep-th row and behind
+        some([&](uint32_t x, int i) __attribute__((always_inline)) {
+            if (i >= g.i0) return;
+            if (x > found) greater[0] += i < z.m, greater[1] += i >= z.m;
+            if (x == found) equal[0] += i < z.m, equal[1] += i >= z.m;
+        });
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            int x = e < 2 ? greater[e] : equal[e - 2];
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+            if (lane == 0 && x) atomicAdd(&past_counts[e], x);
+        }
+        __syncthreads();
+        const int e0 = min(left, past_counts[2]), e1 = min(left - e0, past_counts[3]);  // equal ones that stay
+        past.equal = past_counts[2] + past_counts[3];
+        past.holes = min(z.m, g.i0) - past_counts[0] - e0;
+        past.movers = past_counts[1] + e1;
     }
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
-        uint32_t x[kPer];
-        load_keys(a, z, i0, x);
-        list_block(a, sh, z, i0, x, found, left, past);
+        if (i0 > g.i0) load_keys(a, z, i0, own);
+        list_block(a, sh, z, i0, own, found, left, past);
     }
     if ((int)blockIdx.x == of - 1 && threadIdx.x == 0) a.moves[z.pair] = past.holes;
 }
@@ -441,12 +462,11 @@ size_t lay_out(EvictArgs& a, char* base) {
     if (a.max_rows <= kBlock) return at;
     a.segment = (a.max_rows + kMostSegments * kBlock - 1) / (kMostSegments * kBlock) * kBlock;
     a.segments = (a.max_rows + a.segment - 1) / a.segment;
-    take(a.keys, pairs * a.max_rows);
-    take(a.bins1, pairs * a.segments * kBins1);
-    take(a.bins2, pairs * a.segments * kBins1);
-    take(a.bins3, pairs * a.segments * kBins1);
-    take(a.above, pairs * a.segments * 2);
-    take(a.chosen, pairs * 4);
+    a.stride = a.segments * a.segment;
+    take(a.keys, pairs * a.stride);
+    take(a.bins, pairs * a.segments * kBins);
+    take(a.counts, pairs * a.segments);
+    take(a.listed, pairs * a.stride);
     return at;
 }
 
@@ -471,7 +491,6 @@ int cache_evict(const Geom& g, const Pages& c, const int32_t* rows, const int32_
         KernelTimer kt("evict_select", st);
         hipLaunchKernelGGL(evict_first_kernel, grid, dim3(kSelectThreads), 0, st, a);
         hipLaunchKernelGGL(evict_second_kernel, grid, dim3(kSelectThreads), 0, st, a);
-        hipLaunchKernelGGL(evict_third_kernel, grid, dim3(kSelectThreads), 0, st, a);
         hipLaunchKernelGGL(evict_list_kernel, grid, dim3(kSelectThreads), 0, st, a);
     }
     if (max_rows > 1) {
