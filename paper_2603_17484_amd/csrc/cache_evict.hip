@@ -191,6 +191,57 @@ __device__ __forceinline__ void list_block(const EvictArgs& a, Shared& sh, const
     past = Before{past.equal + equal, past.holes + holes, past.movers + movers};
 }
 
+// The moves of a pair, from the first-th group of lanes' on: a group per move, 16 bytes a lane, K's and V's beside one another; kAhead moves of a
+// group on their way together.
+constexpr int kAhead = 4;
+template <int BITS>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const Sizes& z, int count, int first, int groups) {
+    constexpr int kLanes = 2 * BITS, kRowBytes = kD * BITS / 8;
+    const int lane = threadIdx.x % kLanes, c = lane % (kLanes / 2);
+    const size_t list = (size_t)z.pair * (a.max_rows / 2);
+    char* const pool = (lane < kLanes / 2 ? a.c.k : a.c.v) + c * 16;
+    unsigned char* const scales = lane < kLanes / 2 ? a.c.ks : a.c.vs;
+    for (int i0 = first * kAhead; i0 < count; i0 += groups * kAhead) {
+        int to[kAhead], from[kAhead];
+        size_t dst[kAhead], src[kAhead];
+        bool on[kAhead];
+        u32x4 x[kAhead];
+        uint32_t e[kAhead];
+        float w[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) to[j] = a.to[list + min(i0 + j, count - 1)], from[j] = a.from[list + min(i0 + j, count - 1)];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int p = page_at(a, z.b, to[j]), q = page_at(a, z.b, from[j]);
+            on[j] = i0 + j < count && (unsigned)p < (unsigned)a.c.pages && (unsigned)q < (unsigned)a.c.pages;  // page numbers outside the pool are never followed
+            dst[j] = on[j] ? pool_row(a.c, a.gm.Hkv, p, z.hk, to[j]) : 0, src[j] = on[j] ? pool_row(a.c, a.gm.Hkv, q, z.hk, from[j]) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (on[j]) {
+                x[j] = *reinterpret_cast<const u32x4*>(pool + src[j] * kRowBytes);
+                if (BITS < 16 && c == 0) e[j] = *reinterpret_cast<const uint32_t*>(scales + src[j] * kRowScales);
+                if (lane == 1) w[j] = a.weight_in[src[j]];
+            }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (on[j]) {
+                *reinterpret_cast<u32x4*>(pool + dst[j] * kRowBytes) = x[j];
+                if (BITS < 16 && c == 0) *reinterpret_cast<uint32_t*>(scales + dst[j] * kRowScales) = e[j];
+                if (lane == 1) a.weight[dst[j]] = w[j];
+            }
+            if (lane == 2 && a.kept && i0 + j < count) a.kept[(size_t)z.pair * a.max_rows + to[j]] = from[j];
+        }
+    }
+}
+template <int BITS>
+__global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
+    constexpr int kGroups = kThreads / (2 * BITS);
+    move_rows<BITS>(a, sizes_of(a, blockIdx.y), a.moves[blockIdx.y], blockIdx.x * kGroups + (int)threadIdx.x / (2 * BITS), gridDim.x * kGroups);
+}
+
+// MOVE: BITS of the elements, or 0: the moves are another kernel's.
+template <int MOVE>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
     __shared__ Shared sh;
     __shared__ int bins[kBins];
@@ -221,7 +272,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     }
     Before past{0, 0, 0};
     list_block(a, sh, z, 0, x, found, left, past);
-    if (threadIdx.x == 0) a.moves[z.pair] = past.holes;
+    if constexpr (MOVE) {
+        __syncthreads();  // (the lists, by this workgroup for itself)
+        move_rows<MOVE>(a, z, past.holes, threadIdx.x / (2 * MOVE), kSelectThreads / (2 * MOVE));
+    } else {
+        if (threadIdx.x == 0) a.moves[z.pair] = past.holes;
+    }
 }
 
 // The workgroup's segment of its pair: rows i0 .. i1 - 1.
@@ -404,50 +460,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
     if ((int)blockIdx.x == of - 1 && threadIdx.x == 0) a.moves[z.pair] = past.holes;
 }
 
-// A group of lanes per move, 16 bytes a lane, K's and V's beside one another; kAhead moves of a group on their way together.
-template <int BITS>
-__global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
-    constexpr int kLanes = 2 * BITS, kGroups = kThreads / kLanes, kAhead = 4, kRowBytes = kD * BITS / 8;
-    const int pair = blockIdx.y, b = pair / a.gm.Hkv, hk = pair - b * a.gm.Hkv;
-    const int count = a.moves[pair], lane = threadIdx.x % kLanes, c = lane % (kLanes / 2);
-    const size_t list = (size_t)pair * (a.max_rows / 2);
-    char* const pool = (lane < kLanes / 2 ? a.c.k : a.c.v) + c * 16;
-    unsigned char* const scales = lane < kLanes / 2 ? a.c.ks : a.c.vs;
-    for (int i0 = (blockIdx.x * kGroups + (int)threadIdx.x / kLanes) * kAhead; i0 < count; i0 += gridDim.x * kGroups * kAhead) {
-        int to[kAhead], from[kAhead];
-        size_t dst[kAhead], src[kAhead];
-        bool on[kAhead];
-        u32x4 x[kAhead];
-        uint32_t e[kAhead];
-        float w[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) to[j] = a.to[list + min(i0 + j, count - 1)], from[j] = a.from[list + min(i0 + j, count - 1)];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int p = page_at(a, b, to[j]), q = page_at(a, b, from[j]);
-            on[j] = i0 + j < count && (unsigned)p < (unsigned)a.c.pages && (unsigned)q < (unsigned)a.c.pages;  // page numbers outside the pool are never followed
-            dst[j] = on[j] ? pool_row(a.c, a.gm.Hkv, p, hk, to[j]) : 0, src[j] = on[j] ? pool_row(a.c, a.gm.Hkv, q, hk, from[j]) : 0;
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (on[j]) {
-                x[j] = *reinterpret_cast<const u32x4*>(pool + src[j] * kRowBytes);
-                if (BITS < 16 && c == 0) e[j] = *reinterpret_cast<const uint32_t*>(scales + src[j] * kRowScales);
-                if (lane == 1) w[j] = a.weight_in[src[j]];
-            }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (on[j]) {
-                *reinterpret_cast<u32x4*>(pool + dst[j] * kRowBytes) = x[j];
-                if (BITS < 16 && c == 0) *reinterpret_cast<uint32_t*>(scales + dst[j] * kRowScales) = e[j];
-                if (lane == 1) a.weight[dst[j]] = w[j];
-            }
-            if (lane == 2 && a.kept && i0 + j < count) a.kept[(size_t)pair * a.max_rows + to[j]] = from[j];
-        }
-    }
-}
-
 constexpr int kMoveWorkgroups = 16384;
+constexpr int kAlone = 256;  // pairs
 
 size_t lay_out(EvictArgs& a, char* base) {
     size_t at = 0;
@@ -483,28 +497,30 @@ int cache_evict(const Geom& g, const Pages& c, const int32_t* rows, const int32_
     EvictArgs a{g, c, rows, keep, max_rows, weight_in, weight, kept};
     lay_out(a, (char*)workspace);
     const int pairs = g.B * g.Hkv;
-    if (max_rows <= kBlock) {
-        KernelTimer kt("evict_select", st);
-        hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, st, a);
-    } else {
-        const dim3 grid(a.segments, pairs);
-        KernelTimer kt("evict_select", st);
-        hipLaunchKernelGGL(evict_first_kernel, grid, dim3(kSelectThreads), 0, st, a);
-        hipLaunchKernelGGL(evict_second_kernel, grid, dim3(kSelectThreads), 0, st, a);
-        hipLaunchKernelGGL(evict_list_kernel, grid, dim3(kSelectThreads), 0, st, a);
-    }
-    if (max_rows > 1) {
-        KernelTimer kt("evict_move", st);
-        auto launch = [&](auto bits) {
-            constexpr int BITS = decltype(bits)::value;
-            constexpr int kEach = kThreads / (2 * BITS) * 4;  // moves of a workgroup
+    auto launch = [&](auto bits) {
+        constexpr int BITS = decltype(bits)::value;
+        const bool alone = max_rows <= kBlock && pairs >= kAlone;
+        if (max_rows <= kBlock) {
+            KernelTimer kt("evict_select", st);
+            if (alone) hipLaunchKernelGGL(evict_select_kernel<BITS>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+            else hipLaunchKernelGGL(evict_select_kernel<0>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+        } else {
+            const dim3 grid(a.segments, pairs);
+            KernelTimer kt("evict_select", st);
+            hipLaunchKernelGGL(evict_first_kernel, grid, dim3(kSelectThreads), 0, st, a);
+            hipLaunchKernelGGL(evict_second_kernel, grid, dim3(kSelectThreads), 0, st, a);
+            hipLaunchKernelGGL(evict_list_kernel, grid, dim3(kSelectThreads), 0, st, a);
+        }
+        if (!alone && max_rows > 1) {
+            KernelTimer kt("evict_move", st);
+            constexpr int kEach = kThreads / (2 * BITS) * kAhead;  // moves of a workgroup
             const int most = (max_rows / 2 + kEach - 1) / kEach, share = (kMoveWorkgroups + pairs - 1) / pairs;
             hipLaunchKernelGGL(evict_move_kernel<BITS>, dim3(most < share ? most : share, pairs), dim3(kThreads), 0, st, a);
-        };
-        if (c.bits == 16) launch(std::integral_constant<int, 16>{});
-        else if (c.bits == 8) launch(std::integral_constant<int, 8>{});
-        else launch(std::integral_constant<int, 4>{});
-    }
+        }
+    };
+    if (c.bits == 16) launch(std::integral_constant<int, 16>{});
+    else if (c.bits == 8) launch(std::integral_constant<int, 8>{});
+    else launch(std::integral_constant<int, 4>{});
     return launch_status();
 }
 
