@@ -7,12 +7,16 @@
 // Which rows stay is a radix selection over the weights' bits, ordered as whole numbers: the histogram of their highest bits says in which bin
 // the last row that stays lies, that of the bits below among the rows of this bin where in it, and so on.  Then the lists: places that become free, and
 // rows that move there, both ascending.
-//   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 11, 11 and 10 bits
+//   evict_select_kernel  up to 8192 rows: a workgroup per KV head of a sequence, the weights in its registers, 11, 11 and 10 bits; where there are
+//                        many, it makes the moves too
 //   evict_first_kernel, evict_second_kernel, evict_list_kernel
 //                        more: a workgroup per 8192 rows (or 1/64).  The first leaves the histogram of its rows' highest 11 bits; each of the second adds up
 //                        those of its KV head and lists its rows in the bin found; each of the third takes all of these into shared memory,
 //                        so that it knows by itself which rows stay and what comes before its own on the lists (no atomics on memory, nothing to clear)
 //   evict_move_kernel    the moves: K, V, exponents, weights
+//
+// Selection is bound by chains of launches and of dependent loads, moves by their bytes.  Half of 114688 rows of 4 KV heads in bf16 (120 MB) 61 us: 7, 9 and 15 of
+// selection, 28 of moves (4.2 TB/s; a copy of 4 GiB: 4.8).  A quarter of 1792 to 3584 rows of 32 x 8 KV heads in e4m3 (74 MB) 36.
 #include "paged.hpp"
 
 namespace l2a {
@@ -461,7 +465,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
 }
 
 constexpr int kMoveWorkgroups = 16384;
-constexpr int kAlone = 256;  // pairs
+// KV heads of sequences from which on each one's moves are made by the workgroup that selects its rows, us for those of another kernel: 256 of 3000 rows in
+// e4m3, 3/4 kept, 27.6 for 34.3; 1024 of 500 in e2m1 49.5 for 59.6; 256 of 8000 in bf16 136 for 131.  Fewer: 128 of 8000 104 for 63, 4 of 3000 26 for 16.
+constexpr int kAlone = 256;
 
 size_t lay_out(EvictArgs& a, char* base) {
     size_t at = 0;

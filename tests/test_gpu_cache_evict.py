@@ -75,6 +75,9 @@ CASES = {  # bits, lengths, Hkv, page, rows, keep
     "a round of the selection and one more": (8, [1025, 1024, 1023], 1, 256, [1025, 1024, 1023], [512, 511, 1022]),
     "long": (16, [9000], 2, 64, [8960], [4032]),
     "longer": (4, [40000, 3], 1, 128, [39936, 2], [20096, 1]),
+    "more heads than CUs": (16, [40 + i % 7 for i in range(40)], 8, 16, [32 + i % 9 for i in range(40)], [16 + i % 13 for i in range(40)]),
+    "more heads than CUs, e4m3": (8, [400 + 16 * (i % 5) for i in range(33)], 8, 16, [400 - i for i in range(33)], [180 + 5 * i for i in range(33)]),
+    "more heads than CUs, e2m1": (4, [2100, 3, 16] + [30] * 30, 8, 16, [2099, 3, 16] + [30] * 30, [1000, 1, 16] + [i for i in range(30)]),
     "many": (8, [33 + 5 * i for i in range(60)], 2, 16, [32 + 5 * i for i in range(60)], [16 + i for i in range(60)]),
 }
 
