@@ -23,6 +23,7 @@ namespace l2a {
 namespace {
 
 constexpr int kSelectThreads = 1024;
+constexpr int kFewThreads = 256;                 // of up to 2048 rows each of many pairs
 constexpr int kPer = 8;                          // rows of a thread
 constexpr int kBlock = kSelectThreads * kPer;
 constexpr int kMostSegments = 64;                // workgroups of a KV head of a sequence
@@ -73,40 +74,43 @@ __device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int pair) {
     z.n = rows_of(a, z.b), z.m = plan::clamp(a.keep[z.b], 0, z.n);
     return z;
 }
-// Row i0 + 1024 j + thread of a block as order; 0 past the end.  Where the weights do not stay in place, those before the keep-th go to theirs (the moves
+// Row i0 + T j + thread of a block (of T threads) as order; 0 past the end.  Where the weights do not stay in place, those before the keep-th go to theirs (the moves
 // write over those that leave).
+template <int T>
 __device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
     float w[kPer];
     size_t row[kPer];
     bool real[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * kSelectThreads + (int)threadIdx.x, page = i < z.n ? page_at(a, z.b, i) : 0;
+        const int i = i0 + j * T + (int)threadIdx.x, page = i < z.n ? page_at(a, z.b, i) : 0;
         real[j] = (unsigned)page < (unsigned)a.c.pages;
         row[j] = pool_row(a.c, a.gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), z.hk, i);
     }
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) w[j] = i0 + j * kSelectThreads + (int)threadIdx.x < z.n ? a.weight_in[row[j]] : 0.f;
+    for (int j = 0; j < kPer; ++j) w[j] = i0 + j * T + (int)threadIdx.x < z.n ? a.weight_in[row[j]] : 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        const int i = i0 + j * T + (int)threadIdx.x;
         x[j] = i < z.n ? order(w[j]) : 0u;
         if (a.weight != a.weight_in && i < z.m && real[j]) a.weight[row[j]] = w[j];
     }
 }
 // The same of a block whose order was left in memory (segments are whole blocks).
+template <int T>
 __device__ __forceinline__ void load_keys(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = a.keys[(size_t)z.pair * a.stride + i0 + j * kSelectThreads + (int)threadIdx.x];
+    for (int j = 0; j < kPer; ++j) x[j] = a.keys[(size_t)z.pair * a.stride + i0 + j * T + (int)threadIdx.x];
 }
 
+template <int T>
 struct Shared {
-    int sums[kSelectThreads / 64], chosen[2], counts[kPer][kSelectThreads / 64];
+    int sums[T / 64], chosen[2], counts[kPer][T / 64];
 };
 // Bins from the highest number down, EACH a thread in the order of threads; mine: how many rows this thread's have, `highest` its first.  The bin in
 // which the left-th row lies, and the how-manieth in it that is.
-template <int EACH>
-__device__ __forceinline__ void choose(Shared& sh, const int (&mine)[EACH], int highest, int& bin, int& left) {
+template <int EACH, int T>
+__device__ __forceinline__ void choose(Shared<T>& sh, const int (&mine)[EACH], int highest, int& bin, int& left) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int sum = 0;
 #pragma unroll
@@ -121,7 +125,7 @@ __device__ __forceinline__ void choose(Shared& sh, const int (&mine)[EACH], int 
     __syncthreads();
     int before = upto - sum;
 #pragma unroll
-    for (int w = 0; w < kSelectThreads / 64; ++w)
+    for (int w = 0; w < T / 64; ++w)
         if (w < wave) before += sh.sums[w];
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
@@ -134,7 +138,8 @@ __device__ __forceinline__ void choose(Shared& sh, const int (&mine)[EACH], int 
 }
 // Places of flags among all of a block, in the order of rows: of this thread's j-th, how many lie before it; and how many there are.  Two kinds of flags
 // at once, the second's numbers in the upper halves (a block has fewer than 2^16 rows).
-__device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], const bool (&other)[kPer], int (&at)[kPer]) {
+template <int T>
+__device__ __forceinline__ int places(Shared<T>& sh, const bool (&flag)[kPer], const bool (&other)[kPer], int (&at)[kPer]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned long long before = (1ull << lane) - 1ull;
 #pragma unroll
@@ -145,10 +150,10 @@ __device__ __forceinline__ int places(Shared& sh, const bool (&flag)[kPer], cons
     }
     __syncthreads();
     // every wavefront adds up all counts: a lane those of two
-    constexpr int kWavesOf = kSelectThreads / 64, kCounts = kPer * kWavesOf;
-    static_assert(kCounts == 128, "two counts a lane");
+    constexpr int kWavesOf = T / 64, kCounts = kPer * kWavesOf;
+    static_assert(kCounts <= 128, "two counts a lane");
     const int* const counts = &sh.counts[0][0];
-    const int c0 = counts[2 * lane], c1 = counts[2 * lane + 1];
+    const int c0 = 2 * lane < kCounts ? counts[2 * lane] : 0, c1 = 2 * lane < kCounts ? counts[2 * lane + 1] : 0;
     int upto = c0 + c1;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -169,25 +174,26 @@ struct Before {
     int equal, holes, movers;
 };
 // The lists of a block, its rows x in registers: all greater than `found` stay, and the first `left` of those equal to it.
-__device__ __forceinline__ void list_block(const EvictArgs& a, Shared& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past) {
+template <int T>
+__device__ __forceinline__ void list_block(const EvictArgs& a, Shared<T>& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past) {
     int32_t *to = a.to + (size_t)z.pair * (a.max_rows / 2), *from = a.from + (size_t)z.pair * (a.max_rows / 2);
     int32_t* const kept = a.kept ? a.kept + (size_t)z.pair * a.max_rows : nullptr;
     bool flag[kPer], other[kPer], stays[kPer];
     int at[kPer];
     const bool all = z.m == z.n;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * kSelectThreads + (int)threadIdx.x < z.n, other[j] = false;
+    for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * T + (int)threadIdx.x < z.n, other[j] = false;
     const int equal = places(sh, flag, other, at);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        const int i = i0 + j * T + (int)threadIdx.x;
         stays[j] = i < z.n && (all || x[j] > found || (flag[j] && past.equal + at[j] < left));
         flag[j] = i < z.m && !stays[j], other[j] = i >= z.m && stays[j];
     }
     const int both = places(sh, flag, other, at), holes = both & 0xffff, movers = both >> 16;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
+        const int i = i0 + j * T + (int)threadIdx.x;
         if (flag[j]) to[past.holes + (at[j] & 0xffff)] = i;
         if (other[j]) from[past.movers + (at[j] >> 16)] = i;
         if (kept && i < z.m && stays[j]) kept[i] = i;
@@ -245,9 +251,9 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
 }
 
 // MOVE: BITS of the elements, or 0: the moves are another kernel's.
-template <int MOVE>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-    __shared__ Shared sh;
+template <int MOVE, int T>
+__global__ __launch_bounds__(T) void evict_select_kernel(EvictArgs a) {
+    __shared__ Shared<T> sh;
     __shared__ int bins[kBins];
     const Sizes z = sizes_of(a, blockIdx.x);
     if (z.m == 0) {
@@ -255,30 +261,32 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
         return;
     }
     uint32_t x[kPer], found = 0;
-    load_block(a, z, 0, x);
+    load_block<T>(a, z, 0, x);
     int left = z.m;
-    const int highest = kBins - 1 - 2 * (int)threadIdx.x;
+    constexpr int kEach = kBins / T;  // bins of a thread
+    const int highest = kBins - 1 - kEach * (int)threadIdx.x;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         if (z.m == z.n) break;
         constexpr int kShift[3] = {21, 10, 0};
         const int shift = kShift[pass], above = pass ? kShift[pass - 1] : 0;
-        bins[highest] = bins[highest - 1] = 0;
+        for (int i = threadIdx.x; i < kBins; i += T) bins[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
-            if (j * kSelectThreads + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins / 2 - 1 : kBins - 1)], 1);
+            if (j * T + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins / 2 - 1 : kBins - 1)], 1);
         __syncthreads();
-        const int mine[2] = {bins[highest], bins[highest - 1]};
-        int bin;
-        choose<2>(sh, mine, highest, bin, left);
+        int mine[kEach], bin;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) mine[e] = bins[highest - e];
+        choose(sh, mine, highest, bin, left);
         found |= (uint32_t)bin << shift;
     }
     Before past{0, 0, 0};
     list_block(a, sh, z, 0, x, found, left, past);
     if constexpr (MOVE) {
         __syncthreads();  // (the lists, by this workgroup for itself)
-        move_rows<MOVE>(a, z, past.holes, threadIdx.x / (2 * MOVE), kSelectThreads / (2 * MOVE));
+        move_rows<MOVE>(a, z, past.holes, threadIdx.x / (2 * MOVE), T / (2 * MOVE));
     } else {
         if (threadIdx.x == 0) a.moves[z.pair] = past.holes;
     }
@@ -302,7 +310,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a
     __syncthreads();
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
-        load_block(a, z, i0, x);
+        load_block<kSelectThreads>(a, z, i0, x);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
@@ -316,7 +324,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs a) {
-    __shared__ Shared sh;
+    __shared__ Shared<kSelectThreads> sh;
     __shared__ int count, greater[2];
     const Sizes z = sizes_of(a, blockIdx.y);
     const Segment g = segment_of(a, z);
@@ -329,12 +337,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs 
         const int32_t* const p = a.bins + ((size_t)z.pair * a.segments + s) * kBins;
         sums[0] += p[highest], sums[1] += p[highest - 1];
     }
-    choose<2>(sh, sums, highest, bin, left);
+    choose(sh, sums, highest, bin, left);
     u32x2* const listed = a.listed + (size_t)z.pair * a.stride + g.i0;
     const int lane = threadIdx.x & 63;
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
-        load_keys(a, z, i0, x);
+        load_keys<kSelectThreads>(a, z, i0, x);
         unsigned long long set[kPer];
         int all = 0, at = 0;
 #pragma unroll
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(EvictArgs 
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a) {
-    __shared__ Shared sh;
+    __shared__ Shared<kSelectThreads> sh;
     __shared__ int bins[kBins], ends[kMostSegments], past_counts[4];
     __shared__ u32x2 candidates[kCandidates];
     const Sizes z = sizes_of(a, blockIdx.y);
@@ -375,7 +383,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
     }
     const int of = (z.n + a.segment - 1) / a.segment, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t own[kPer];
-    load_keys(a, z, g.i0, own);  // (on their way until the lists)
+    load_keys<kSelectThreads>(a, z, g.i0, own);  // (on their way until the lists)
     uint32_t found = 0;
     int left = 0;
     Before past{0, 0, 0};
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
             __syncthreads();
             const int here[2] = {bins[highest], bins[highest - 1]};
             int bin;
-            choose<2>(sh, here, highest, bin, left);
+            choose(sh, here, highest, bin, left);
             found |= (uint32_t)bin << shift;
         }
         int greater[2] = {0, 0}, equal[2] = {0, 0};  // of the segments before, before the keep-th row and behind
@@ -458,7 +466,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
         past.movers = past_counts[1] + e1;
     }
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
-        if (i0 > g.i0) load_keys(a, z, i0, own);
+        if (i0 > g.i0) load_keys<kSelectThreads>(a, z, i0, own);
         list_block(a, sh, z, i0, own, found, left, past);
     }
     if ((int)blockIdx.x == of - 1 && threadIdx.x == 0) a.moves[z.pair] = past.holes;
@@ -468,6 +476,9 @@ constexpr int kMoveWorkgroups = 16384;
 // KV heads of sequences from which on each one's moves are made by the workgroup that selects its rows, us for those of another kernel: 256 of 3000 rows in
 // e4m3, 3/4 kept, 27.6 for 34.3; 1024 of 500 in e2m1 49.5 for 59.6; 256 of 8000 in bf16 136 for 131.  Fewer: 128 of 8000 104 for 63, 4 of 3000 26 for 16.
 constexpr int kAlone = 256;
+// And from which on, where they have up to 2048 rows, by one of 256 threads, of which a CU holds more, us for those of 1024 threads: 1024 of 1792 in e4m3 77 for 102, of 500 in
+// e2m1 21.5 for 49.4, of 100 15 for 47; 512 of 2000 in e4m3 39 for 47.  256 of 2000 31 for 26.
+constexpr int kMany = 512;
 
 size_t lay_out(EvictArgs& a, char* base) {
     size_t at = 0;
@@ -508,8 +519,9 @@ int cache_evict(const Geom& g, const Pages& c, const int32_t* rows, const int32_
         const bool alone = max_rows <= kBlock && pairs >= kAlone;
         if (max_rows <= kBlock) {
             KernelTimer kt("evict_select", st);
-            if (alone) hipLaunchKernelGGL(evict_select_kernel<BITS>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
-            else hipLaunchKernelGGL(evict_select_kernel<0>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+            if (pairs >= kMany && max_rows <= kFewThreads * kPer) hipLaunchKernelGGL((evict_select_kernel<BITS, kFewThreads>), dim3(pairs), dim3(kFewThreads), 0, st, a);
+            else if (alone) hipLaunchKernelGGL((evict_select_kernel<BITS, kSelectThreads>), dim3(pairs), dim3(kSelectThreads), 0, st, a);
+            else hipLaunchKernelGGL((evict_select_kernel<0, kSelectThreads>), dim3(pairs), dim3(kSelectThreads), 0, st, a);
         } else {
             const dim3 grid(a.segments, pairs);
             KernelTimer kt("evict_select", st);

@@ -78,6 +78,8 @@ CASES = {  # bits, lengths, Hkv, page, rows, keep
     "more heads than CUs": (16, [40 + i % 7 for i in range(40)], 8, 16, [32 + i % 9 for i in range(40)], [16 + i % 13 for i in range(40)]),
     "more heads than CUs, e4m3": (8, [400 + 16 * (i % 5) for i in range(33)], 8, 16, [400 - i for i in range(33)], [180 + 5 * i for i in range(33)]),
     "more heads than CUs, e2m1": (4, [2100, 3, 16] + [30] * 30, 8, 16, [2099, 3, 16] + [30] * 30, [1000, 1, 16] + [i for i in range(30)]),
+    "twice as many": (4, [5 + 3 * i for i in range(66)], 8, 16, [4 + 3 * i for i in range(66)], [2 + i for i in range(66)]),
+    "twice as many, long": (8, [2048, 2047, 1] + [20] * 61, 8, 64, [2048, 2046, 1] + [19] * 61, [1024, 2000, 0] + [i % 20 for i in range(61)]),
     "many": (8, [33 + 5 * i for i in range(60)], 2, 16, [32 + 5 * i for i in range(60)], [16 + i for i in range(60)]),
 }
 
