@@ -473,11 +473,18 @@ __global__ __launch_bounds__(kChunk) void weights_join_kernel(WeightsArgs a) {
     if (o.pair < 0) return;
     float sum = a.slots[((size_t)w * 2 + 1) * kChunk + threadIdx.x];
     const long long end = o.start + o.tiles + kStart<BITS>;
-    for (int v = w + 1; v < a.workgroups; ++v) {
-        const long long x0 = v * o.per, x1 = x0 + o.per;
-        const int from = tiles_before<BITS>(x0, o.start, o.tiles), to = x1 >= end ? o.tiles : tiles_before<BITS>(x1, o.start, o.tiles);
-        if (from < to) sum += a.slots[(size_t)v * 2 * kChunk + threadIdx.x];
-        if (to == o.tiles) break;
+    constexpr int kAhead = 8;  // loads on their way together
+    for (int v = w + 1, to = 0; to < o.tiles && v < a.workgroups; v += kAhead) {
+        float x[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const long long x0 = (v + e) * o.per, x1 = x0 + o.per;
+            const int from = x0 >= end ? o.tiles : tiles_before<BITS>(x0, o.start, o.tiles);
+            to = x1 >= end ? o.tiles : tiles_before<BITS>(x1, o.start, o.tiles);
+            x[e] = from < to && v + e < a.workgroups ? a.slots[(size_t)(v + e) * 2 * kChunk + threadIdx.x] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) sum += x[e];
     }
     const int b = o.pair / a.gm.Hkv, hk = o.pair - b * a.gm.Hkv, key = o.chunk * kChunk + (int)threadIdx.x;
     const Seq s = seq_at(a.gm, a.c, a.seq_start, a.pos, b, a.max_new);
