@@ -133,6 +133,8 @@ class PagedCache:
 
     def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", fp4: bool = False,
                  decay: Optional[float] = None):
+        if decay is not None and not 0.0 <= decay < float("inf"):
+            raise ValueError(f"weights fade by a finite number that is not negative; got {decay}")
         self.p, self.page_size, self.decay = B.l2a_params.from_buffer_copy(p), page_size, decay
         self.cache = B.alloc_cache(p, pages, page_size, max_pages, fp8, device, **({"fp4": True} if fp4 else {}))
         self.weight = None if decay is None else torch.zeros(pages, p.Hkv, page_size, dtype=torch.float32, device=device)

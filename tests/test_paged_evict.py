@@ -92,6 +92,9 @@ def test_what_is_refused_changes_nothing(calls):
         assert after[0] == before[0] and np.array_equal(after[1], before[1]) and after[2] == before[2] and np.array_equal(cache.evicted, evicted)
     with pytest.raises(ValueError, match="no attention weights"):
         make(decay=None).evict(40)
+    for decay in (-0.5, float("nan"), float("inf")):
+        with pytest.raises(ValueError, match="fade"):
+            make(decay=decay)
 
 
 def test_without_windows_all_rows_may_go(calls):
