@@ -360,7 +360,7 @@ int l2a_cache_weights(const l2a_params* p, const l2a_cache* c, const void* q, co
  *   kept_opt    out optional [B, Hkv, max_rows] int32: which row each of rows 0 .. keep[b] - 1 was before; entries behind are left as they were
  *   workspace   l2a_evict_workspace_bytes(p, c, max_rows) bytes
  * Of p: B, Hkv and D count (the other fields must still be valid).  Rows in pages outside the pool are not moved.  Sequences that share pages must not
- * be evicted from in one call, nor may one of them while the other still needs them.  Errors as for the other calls; L2A_ERR_SHAPE for max_rows.
+ * be evicted from in one call, nor may one of them while the other still needs them, nor may a page stand twice in a sequence's table.  Errors as for the other calls; L2A_ERR_SHAPE for max_rows.
  */
 size_t l2a_evict_workspace_bytes(const l2a_params* p, const l2a_cache* c, int32_t max_rows);
 int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows, const int32_t* keep, int32_t max_rows,

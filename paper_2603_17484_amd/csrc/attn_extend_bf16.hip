@@ -17,7 +17,7 @@
 // makes the plan for itself (extend_short_kernel, extend_combine_short_kernel): two launches instead of four, 25 us for a token behind 32K.
 //
 // Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 126 (main 118: 5.3
-// TB/s); 16 x 5 behind 32K 106; a token behind 32K 24 (18); 2048 behind 32K 338 (331), 4096 behind 124K 1697 (1642: 1.04 PFLOP/s, 1577 to 1734 from
+// TB/s), in e2m1, 315 MB, 86 (80: 3.9); 16 x 5 behind 32K 106; a token behind 32K 24 (18); 2048 behind 32K 338 (331), 4096 behind 124K 1697 (1642: 1.04 PFLOP/s, 1577 to 1734 from
 // card to card; products of 8192 x 8192 matrices reach 1.28 with nothing between them); 128 behind 64K 98; 1000 beside 31 single ones at 16K 169 (142);
 // 3 x 777 first tokens 61 (38).  Before the main kernel: lists 5 to 11, plan 7 to 14; behind it: sums joined, 6 to 27.
 #include "paged.hpp"
@@ -694,7 +694,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
     constexpr int kRows = 64 / BITS, kEach = kSub / kRows, kRowBytes = kD * BITS / 8;  // rows of an instruction, which lie in one page; instructions
     const int mine = load_row<BITS>(lane);
-    constexpr bool kDirect = BITS == 4;  // K goes straight into its operand: with 4 bits the way through shared memory took longer than the bytes
+    constexpr bool kDirect = BITS == 4;  // K goes straight into its operand (64 sequences of 8K tokens 86 us, through shared memory 92)
     u32x4 kx[BITS < 16 ? kEach : 1], vx[BITS < 16 ? kEach : 1];
     uint32_t kse[BITS < 16 ? kEach : 1], vse[BITS < 16 ? kEach : 1];
     RawKeys<kDirect ? BITS : 16> keys_raw;

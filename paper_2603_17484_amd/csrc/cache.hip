@@ -7,7 +7,7 @@
 //   read    x = y 2^e, exact in bf16.
 //
 // Memory-bound: every byte of the new rows and of their cache rows is moved once.  65536 tokens of 8 KV heads read out of an e4m3 cache (407 MB)
-// 95 us, 4.3 TB/s (a copy of 4 GiB: 4.75); 8192 written into one (51 MB) 11 us; 7500 of 4 read in bf16 (34 MB) 9.5; 64 written 3.4.
+// 95 us, 4.3 TB/s (a copy of 4 GiB: 4.75), out of one in 4 bits (340 MB) 75; 8192 written into an e4m3 cache (51 MB) 11 us; 7500 of 4 read in bf16 (34 MB) 9.5; 64 written 3.4.
 #include "paged.hpp"
 
 namespace l2a {

@@ -12,6 +12,9 @@
 // workgroup takes an equal stretch of it, and what it does not finish of a chunk of keys meets the rest in a last kernel.
 //
 // Nothing is added by atomics: the order of every sum is fixed.
+//
+// Measured (us): 64 tokens behind 8K of 32 / 8 heads in bf16 (831 MB) 171, 4.9 TB/s (a copy of 4 GiB: 4.8), in e4m3 106, in e2m1 67; one behind 32K 10, of which 6 are
+// the call's; 2048 behind 32K of 28 / 4 heads, half of them routed (248 GFLOP), 250: 10 packing, 235 the products (1.05 PFLOP/s; 8192 x 8192 matrices 1.22), 5 joining.
 #include "paged.hpp"
 #include "tiles.hpp"
 
@@ -62,7 +65,7 @@ struct WeightsArgs {
 // ---------------------------------------------------------------------------------------
 constexpr int kMostSeqs = 1024;  // of a launch: their lengths are summed in shared memory
 
-// Key blocks of all sequences up to and with each, in ends; -> of all.  THREADS threads.
+// Key blocks of all sequences up to and with each, in ends; -> of all.
 template <typename F>
 __device__ __forceinline__ int sum_up(int n, int* ends, int* sums, F&& count) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -129,7 +129,7 @@ class PagedCache:
     about them on the host.  A step uploads the table and its index arrays, which waits for the stream's earlier work, and allocates its output (and
     its workspace, where none is given).  Steps of one cache are ordered, on one stream or by the caller.
     fp8, fp4: elements of 8 or 4 bits.  decay: a number keeps the attention weights that rows receive (`weight`), which fade by it in every step of
-    their sequence; evict() goes by them.  Rows of a sequence that was evicted from are no longer its positions: positions() has those."""
+    their sequence (extend's; steps made by hand from begin_step on call l2a_cache_weights themselves); evict() goes by them.  Rows of a sequence that was evicted from are no longer its positions: positions() has those."""
 
     def __init__(self, p: B.l2a_params, pages: int, page_size: int, max_pages: int, fp8: bool = False, device="cuda", fp4: bool = False,
                  decay: Optional[float] = None):
