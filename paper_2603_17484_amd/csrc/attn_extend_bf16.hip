@@ -17,7 +17,7 @@
 // makes the plan for itself (extend_short_kernel, extend_combine_short_kernel): two launches instead of four, 25 us for a token behind 32K.
 //
 // Measured (us; one call among others on one card, "main" the kernel that attends): 64 tokens behind 8K in e4m3, 610 MB of cache, 126 (main 118: 5.3
-// TB/s), in e2m1, 315 MB, 86 (80: 3.9); 16 x 5 behind 32K 106; a token behind 32K 24 (18); 2048 behind 32K 338 (331), 4096 behind 124K 1697 (1642: 1.04 PFLOP/s, 1577 to 1734 from
+// TB/s), in e2m1, 315 MB, 79 (73: 4.3); 16 x 5 behind 32K 106; a token behind 32K 24 (18); 2048 behind 32K 338 (331), 4096 behind 124K 1697 (1642: 1.04 PFLOP/s, 1577 to 1734 from
 // card to card; products of 8192 x 8192 matrices reach 1.28 with nothing between them); 128 behind 64K 98; 1000 beside 31 single ones at 16K 169 (142);
 // 3 x 777 first tokens 61 (38).  Before the main kernel: lists 5 to 11, plan 7 to 14; behind it: sums joined, 6 to 27.
 #include "paged.hpp"
@@ -677,6 +677,32 @@ template <int NW>
 struct FewLds {
     static constexpr unsigned block = kSub / 4 * kFour, keys = NW * 2 * block, sums = NW * 32 * kPart * 4, votes = keys > sums ? keys : sums, used = votes + 64;
 };
+// A tile's rows, whose sums the wavefronts of a workgroup have left in sums [wave][ROWS][kPart], joined and sent on: 16 threads per row, eight channels each.
+template <int ROWS, int NW>
+__device__ __forceinline__ void join_sums(const ExtendArgs& a, const float* sums, const Tile& t, const plan::Piece& piece, int w) {
+    const int c8 = (threadIdx.x & 15) * 8;
+    for (int r = threadIdx.x >> 4; r < t.rows; r += NW * 4) {
+        float m = kNone, l = 0.f;
+        f32x2 ml[NW];
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            ml[v] = *reinterpret_cast<const f32x2*>(sums + (v * ROWS + r) * kPart);
+            m = fmaxf(m, ml[v][0]);
+        }
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            const float by = fast_exp2(ml[v][0] - m);
+            const f32x4* const at = reinterpret_cast<const f32x4*>(sums + (v * ROWS + r) * kPart + 4 + c8);
+            l = fmaf(ml[v][1], by, l);
+            x += at[0] * by, y += at[1] * by;
+        }
+        const int out_code = row_code(a, t, t.first + r);
+        const Out o = out_of(a, t, piece, w, r, out_code, code_routed(a, t, out_code));
+        store_sums(a, o, c8, m, l, x);
+        store_sums(a, o, c8 + 4, m, l, y);
+    }
+}
 template <int BITS, int NW>
 __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const Tile& t, const plan::Piece& piece, int w) {
     const Geom& gm = a.gm;
@@ -694,7 +720,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
     const lds_cptr k_at = (lds_cptr)(uintptr_t)(k_to + k_lane(lane)), v_at = (lds_cptr)(uintptr_t)(v_to + v_lane(lane));
     constexpr int kRows = 64 / BITS, kEach = kSub / kRows, kRowBytes = kD * BITS / 8;  // rows of an instruction, which lie in one page; instructions
     const int mine = load_row<BITS>(lane);
-    constexpr bool kDirect = BITS == 4;  // K goes straight into its operand (64 sequences of 8K tokens 86 us, through shared memory 92)
+    constexpr bool kDirect = BITS == 4;  // K goes straight into its operand (64 sequences of 8K tokens, all by this function, 86 us, through shared memory 92)
     u32x4 kx[BITS < 16 ? kEach : 1], vx[BITS < 16 ? kEach : 1];
     uint32_t kse[BITS < 16 ? kEach : 1], vse[BITS < 16 ? kEach : 1];
     RawKeys<kDirect ? BITS : 16> keys_raw;
@@ -812,7 +838,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
         for (int i = 0; i < 8; ++i) row.o[i & 3] = mfma32(op[i], __builtin_bit_cast(bf16x8, p[i >> 2]), row.o[i & 3]);
     }
 
-    // ---- the eight wavefronts' sums, joined: 16 threads per row, eight channels each
+    // ---- the eight wavefronts' sums, joined
     row.l += __shfl_xor(row.l, 32);
     float* const sums = reinterpret_cast<float*>(lds);  // [wave][row][kPart]
     const bool some_masked = masked(sb0 - wave) || masked(sb1 - 1);
@@ -828,30 +854,196 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
                 *reinterpret_cast<f32x4*>(at + 4 + d * 32 + c_row(e, h)) = f32x4{row.o[d][e], row.o[d][e + 1], row.o[d][e + 2], row.o[d][e + 3]};
     }
     __syncthreads();
-    const int c8 = (threadIdx.x & 15) * 8;
-    for (int r = threadIdx.x >> 4; r < t.rows; r += NW * 4) {
-        float m = kNone, l = 0.f;
-        f32x2 ml[NW];
-#pragma unroll
-        for (int v = 0; v < NW; ++v) {
-            ml[v] = *reinterpret_cast<const f32x2*>(sums + (v * 32 + r) * kPart);
-            m = fmaxf(m, ml[v][0]);
-        }
-        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-#pragma unroll
-        for (int v = 0; v < NW; ++v) {
-            const float by = fast_exp2(ml[v][0] - m);
-            const f32x4* const at = reinterpret_cast<const f32x4*>(sums + (v * 32 + r) * kPart + 4 + c8);
-            l = fmaf(ml[v][1], by, l);
-            x += at[0] * by, y += at[1] * by;
-        }
-        const int out_code = code_of(r);
-        const Out o = out_of(a, t, piece, w, r, out_code, code_routed(a, t, out_code));
-        store_sums(a, o, c8, m, l, x);
-        store_sums(a, o, c8 + 4, m, l, y);
-    }
+    join_sums<32, NW>(a, sums, t, piece, w);
     return true;
 }
+
+// A tile of up to 16 rows and a cache in 4 bits, where conversions and weights take as long as the bytes: tiles of 16 x 16, which do half of what 32 rows
+// do.  K goes straight from memory into its operand: a lane has 32 channels of a key, the part of a row that has one exponent, and the channels are
+// contracted in that order.  V becomes bf16 in shared memory.  Both are read alike: lane (n, g) key n of 16, quarter g of its row.
+// S^T = K Q^T leaves lane (n, g) with keys 4 g .. 4 g + 3 of either 16 for row n: eight slots of the weights as the next product's operand.
+// (64 sequences of 8K tokens of 32 / 8 heads 79 us for 87, 128 of 1K 61 for 70, one of 32K 17.9 for 19.2.  Two such tiles for up to 32 rows: 16 x 5 rows
+// behind 32K 61 for 55.)
+struct RowSums16 {
+    f32x4 o[8];  // channels 16 d + 4 g .. 16 d + 4 g + 3 of row n
+    float m = kNone, l = 0.f;
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = kNone, l = 0.f;
+    }
+    // (see RowSums)
+    __device__ __forceinline__ void look(float mx) {
+        if (!__any(mx > m + kSlack)) return;
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        const float mnew = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32))), by = fast_exp2(m - mnew);
+        m = mnew, l *= by;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[d] *= by;
+    }
+    __device__ __forceinline__ bool finite() const {
+        float z = 0.f;
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z = fmaf(o[d][e], 0.f, z);
+        return z == 0.f || l * 0.f != 0.f;
+    }
+};
+template <int NW>
+struct Rows16 {
+    struct Raw {
+        u32x4 x[2];  // of either 16 keys
+        uint32_t e[2];
+    };
+    const ExtendArgs& a;
+    const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    Raw k, v;  // the next 32 keys
+    bf16x8 q[4];
+
+    // Sub-blocks of a piece: from + wave, from + wave + NW, .. below to.
+    struct Subs {
+        int from, to;
+    };
+    static __device__ __forceinline__ Subs subs_of(const Tile& t, const plan::Piece& piece) {
+        const int jb0 = t.lo / kKeys + t.skip + piece.from, jb1 = t.lo / kKeys + t.skip + piece.to;
+        return Subs{max(2 * jb0, t.lo / kSub), min(2 * jb1, t.hi / kSub + 1)};
+    }
+    struct Place {
+        size_t rows[2];   // where the 16 keys begin in the pool, and how far behind that this lane's is
+        unsigned off[2];
+    };
+    // keys out of the tile's repeat the nearest one in it (see Loader)
+    __device__ __forceinline__ Place find(const Tile& t, int sb) const {
+        const scalar int32_t* const table = (const scalar int32_t*)(a.c.table + (size_t)t.b * a.c.max_pages);
+        const int k0 = sb * kSub;
+        const bool inside = k0 >= t.lo && k0 + kSub - 1 <= t.hi;
+        Place at;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int first = inside ? k0 + 16 * p : plan::clamp(k0 + 16 * p, t.lo & -16, t.hi & -16);
+            at.rows[p] = pool_row(a.c, a.gm.Hkv, plan::clamp(table[first >> a.c.page_log2], 0, a.c.pages - 1), t.hk, first);
+            at.off[p] = inside ? n : plan::clamp(k0 + 16 * p + n, t.lo, t.hi) - first;
+        }
+        return at;
+    }
+    __device__ __forceinline__ void load(const char* pool, const unsigned char* scales, const Place& at, Raw& x) const {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            x.x[p] = *reinterpret_cast<const u32x4*>(pool + at.rows[p] * (kD / 2) + (at.off[p] * (kD / 2) + g * 16));
+            x.e[p] = scales[at.rows[p] * kRowScales + (at.off[p] * kRowScales + g)];
+        }
+    }
+    __device__ __forceinline__ int code_of(const Tile& t) const { return row_code(a, t, t.first + min(n, t.rows - 1)); }
+    // A piece's first loads.
+    __device__ __forceinline__ void begin(const Tile& t, const plan::Piece& piece) {
+        const Subs sub = subs_of(t, piece);
+        const int code = code_of(t), tok = code / a.gm.G;
+        const __bf16* const qp = a.q + ((size_t)(t.s.start + tok) * a.gm.Hq + t.hk * a.gm.G + code - tok * a.gm.G) * kD + g * 32;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qp + 8 * s);
+        if (sub.from + wave >= sub.to) return;
+        const Place at = find(t, sub.from + wave);
+        load(a.c.k, a.c.ks, at, k);
+        load(a.c.v, a.c.vs, at, v);
+    }
+    // The piece that has begun.  next(), before its sums are joined, begins the next one.  (Without that 82 us for 79.)
+    template <typename F>
+    __device__ __forceinline__ bool run(char* lds, const Tile& t, const plan::Piece& piece, int w, F&& next) {
+        const Subs sub = subs_of(t, piece);
+        const int sb0 = sub.from + wave, sb1 = sub.to;
+        const float c2 = a.gm.scale_log2;
+
+        __syncthreads();  // LDS is free
+        // V in shared memory: as elsewhere, but 32 bytes apart behind 4 rows: a transposing read's four tiles, of 4 keys by 16 channels, touch every bank once
+        constexpr unsigned kApart = 1024 + 32, kBlock = kSub / 4 * kApart;
+        static_assert(NW * kBlock <= FewLds<NW>::votes, "room for every wavefront's block");
+        const lds_ptr v_to = (lds_ptr)(uintptr_t)(wave * kBlock + (n >> 2) * kApart + (n & 3) * 64 + g * 256);
+        const lds_cptr v_at = (lds_cptr)(uintptr_t)(wave * kBlock + g * kApart + (n >> 2) * 64 + (n & 3) * 8);
+        const Range keys = plan::row_keys(t.kind, t.s.pos + code_of(t) / a.gm.G, a.gm.W);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(q[s]));  // waited for here, and so not in the loop, behind its loads
+        const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - a.gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - a.gm.W - 1;
+        auto masked = [&](int sb) __attribute__((always_inline)) { return sb * kSub < lo_max || sb * kSub + kSub - 1 > hi_min; };
+        const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+        const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+        RowSums16 row;
+        row.clear();
+        for (int sb = sb0; sb < sb1; sb += NW) {
+            const bool more = sb + NW < sb1;
+            Place at;
+            if (more) at = find(t, sb + NW);
+            f32x4 sc[2];
+            {
+                bf16x8 op[2][4];
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    u32x4 y[4];
+                    dequantise<4>(k.x[p], exponent_value(k.e[p]), y);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) op[p][s] = __builtin_bit_cast(bf16x8, y[s]);
+                }
+                if (more) load(a.c.k, a.c.ks, at, k);
+                FENCE();
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) sc[p] = mfma16(op[p][s], q[s], s == 0 ? zero4 : sc[p]);
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                u32x4 y[4];
+                dequantise<4>(v.x[p], exponent_value(v.e[p]), y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(__attribute__((address_space(3))) u32x4*)(v_to + 4 * p * kApart + i * 16) = y[i];
+            }
+            if (more) load(a.c.v, a.c.vs, at, v);
+            bf16x8 op[8];
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+                typedef s16x4 __attribute__((address_space(3)))* tr_ptr;
+                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(v_at + (d >> 1) * 256 + (d & 1) * 32));
+                const s16x4 v2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(v_at + (d >> 1) * 256 + (d & 1) * 32 + 4 * kApart));
+                op[d] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+            FENCE();
+            if (masked(sb)) {
+                const int first = keys.lo - sb * kSub - 4 * g, last = keys.hi - sb * kSub - 4 * g;
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[p][e] = 16 * p + e >= first && 16 * p + e <= last ? sc[p][e] : -INFINITY;
+            }
+            const f32x4 x = sc[0], y = sc[1];
+            row.look(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * c2);
+            u32x4 weights;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const f32x2 f = {fast_exp2(fmaf(sc[e >> 2][e & 3], c2, -row.m)), fast_exp2(fmaf(sc[e >> 2][(e & 3) + 1], c2, -row.m))};
+                const bf16x2 pb = __builtin_convertvector(f, bf16x2);
+                row.l = __builtin_amdgcn_fdot2_f32_bf16(pb, one2, row.l, false);
+                weights[e >> 1] = __builtin_bit_cast(uint32_t, pb);
+            }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) row.o[d] = mfma16(op[d], __builtin_bit_cast(bf16x8, weights), row.o[d]);
+        }
+        next();
+
+        // ---- the wavefronts' sums, joined
+        row.l += __shfl_xor(row.l, 16), row.l += __shfl_xor(row.l, 32);
+        float* const sums = reinterpret_cast<float*>(lds);  // [wave][row][kPart]
+        const bool some_masked = masked(sub.from) || masked(sb1 - 1);
+        if (vote<NW>(reinterpret_cast<int*>(lds + FewLds<NW>::votes), some_masked && !row.finite())) return false;
+        // (every wavefront is done with its part of LDS)
+        float* const at = sums + (wave * 16 + n) * kPart;
+        if (g == 0) *reinterpret_cast<f32x2*>(at) = f32x2{row.m, row.l};
+#pragma unroll
+        for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4*>(at + 4 + 16 * d + 4 * g) = row.o[d];
+        __syncthreads();
+        join_sums<16, NW>(a, sums, t, piece, w);
+        return true;
+    }
+};
 
 // Workgroups are dealt round-robin to the 8 XCDs: each XCD takes neighbouring segments and stretches.
 __device__ __forceinline__ int workgroup(const ExtendArgs& a) { return (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3); }
@@ -1125,24 +1317,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_kernel(ExtendArgs a) {
     });
 }
 
-// Calls whose sequences all have up to 128 rows per KV head, a tile for each part of its keys; FEW: up to 32.  SELF: every workgroup makes the plan
+// Calls whose sequences all have up to 128 rows per KV head, a tile for each part of its keys; ROWS: up to how many, 128, 32 or 16.  SELF: every workgroup makes the plan
 // for itself, a thread per KV head of a sequence (at most as many as threads), and the first one leaves it for the last kernel: a
 // launch less.
-constexpr int kShortPairs = 64 * kWaves;
+constexpr int kShortPairs = 64 * kWaves, kSixteen = 16;
 struct ShortPlan {
     int start[2 * kShortPairs], of[2 * kShortPairs];  // of a tile: its place in the line; twice its pair, plus its kind
     Seq seq[kShortPairs];
     int sums[kWaves], first;
 };
-template <int BITS, bool FEW, bool SELF>
+template <int BITS, int ROWS, bool SELF>
 __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs a) {
-    constexpr unsigned kLds = FEW ? FewLds<kWaves>::used : TileLds<BITS>::used;
+    constexpr unsigned kLds = ROWS <= kSub ? FewLds<kWaves>::used : TileLds<BITS>::used;
     __shared__ __attribute__((aligned(1024))) char lds[kLds + (SELF ? sizeof(ShortPlan) : 0)];
     by_address(lds);
     auto rows = [&](const Tile& t, const plan::Piece& piece, int w) __attribute__((always_inline)) {
         bool done;
-        if (FEW || t.rows <= kSub) done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
-        else done = some_rows<BITS, true>(a, lds, t, piece, w);
+        if constexpr (ROWS == kSixteen) {
+            Rows16<kWaves> few{a};
+            few.begin(t, piece);
+            done = few.run(lds, t, piece, w, [] {});
+        } else if (ROWS <= kSub || t.rows <= kSub) {
+            done = few_rows<BITS, kWaves>(a, lds, t, piece, w);
+        } else {
+            done = some_rows<BITS, true>(a, lds, t, piece, w);
+        }
         if (!__any(done)) rows_alone<BITS, kWaves>(a, t, piece, w);
     };
     if constexpr (!SELF) {
@@ -1172,7 +1371,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
         scan<64 * kWaves>(on[0] + on[1], plan_.sums, T, tiles);
         scan<64 * kWaves>(length[0] + length[1], plan_.sums, at, total);
         total = same(total), tiles = same(tiles);
-        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(FEW ? kSub : kHalvesRows, BITS < 16))), x0 = w * per;
+        const int per = same(plan::stretch(total, a.workgroups, plan::block_cost(ROWS <= kSub ? kSub : kHalvesRows, BITS < 16))), x0 = w * per;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (on[kind]) {
@@ -1192,15 +1391,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void extend_short_kernel(ExtendArgs
         }
         __syncthreads();
         if (x0 >= total) return;
-        for (int i = same(plan_.first); i < tiles; ++i) {
-            const int start = same(plan_.start[i]), of = same(plan_.of[i]);
-            if (start >= x0 + per) break;
-            const int p = of >> 1, tb = same(p / gm.Hkv);
-            const Seq ts{same(plan_.seq[p].start), same(plan_.seq[p].n), same(plan_.seq[p].pos)};
-            Tile tile = make_tile(a, ts, tb, p - tb * gm.Hkv, of & 1, 0, ts.n * gm.G);
-            tile.start = start, tile.pos0 = same(tile.pos0), tile.pos1 = same(tile.pos1), tile.lo = same(tile.lo), tile.hi = same(tile.hi), tile.blocks = same(tile.blocks);
-            const plan::Piece piece = plan::piece(place_of(a, tile), per, w);
-            if (piece.from != piece.to) rows(tile, piece, w);
+        int i = same(plan_.first);
+        // the next piece, as far as there is one
+        auto next = [&](Tile& tile, plan::Piece& piece) __attribute__((always_inline)) {
+            while (i < tiles) {
+                const int start = same(plan_.start[i]), of = same(plan_.of[i]);
+                if (start >= x0 + per) return false;
+                const int p = of >> 1, tb = same(p / gm.Hkv);
+                const Seq ts{same(plan_.seq[p].start), same(plan_.seq[p].n), same(plan_.seq[p].pos)};
+                tile = make_tile(a, ts, tb, p - tb * gm.Hkv, of & 1, 0, ts.n * gm.G);
+                tile.start = start, tile.pos0 = same(tile.pos0), tile.pos1 = same(tile.pos1), tile.lo = same(tile.lo), tile.hi = same(tile.hi), tile.blocks = same(tile.blocks);
+                piece = plan::piece(place_of(a, tile), per, w);
+                piece = plan::Piece{same(piece.from), same(piece.to), same(piece.first), same(piece.last)};
+                ++i;
+                if (piece.from != piece.to) return true;
+            }
+            return false;
+        };
+        Tile tile;
+        plan::Piece piece;
+        if constexpr (ROWS == kSixteen) {
+            Rows16<kWaves> few{a};
+            bool on = next(tile, piece);
+            if (on) few.begin(tile, piece);
+            while (on) {
+                Tile then;
+                plan::Piece its;
+                const bool done = few.run(lds, tile, piece, w, [&]() __attribute__((always_inline)) {
+                    on = next(then, its);
+                    if (on) few.begin(then, its);
+                });
+                if (!__any(done)) rows_alone<BITS, kWaves>(a, tile, piece, w);
+                tile = then, piece = its;
+            }
+        } else {
+            while (next(tile, piece)) rows(tile, piece, w);
         }
     }
 }
@@ -1422,14 +1647,18 @@ int mfma_extend(const Geom& g, const Pages& c, const void* q, const int32_t* seq
     }
     {
         KernelTimer kt("extend", st);
+        const dim3 grid(a.workgroups), threads(64 * kWaves);
+        auto launch_short = [&](auto bits, auto rows) {
+            constexpr int BITS = decltype(bits)::value, ROWS = decltype(rows)::value;
+            if (self) hipLaunchKernelGGL((extend_short_kernel<BITS, ROWS, true>), grid, threads, 0, st, a);
+            else hipLaunchKernelGGL((extend_short_kernel<BITS, ROWS, false>), grid, threads, 0, st, a);
+        };
         auto launch = [&](auto bits) {
             constexpr int BITS = decltype(bits)::value;
-            const dim3 grid(a.workgroups), threads(64 * kWaves);
             if (!a.few) hipLaunchKernelGGL(extend_kernel<BITS>, grid, threads, 0, st, a);
-            else if (a.tile_rows == kSub && self) hipLaunchKernelGGL((extend_short_kernel<BITS, true, true>), grid, threads, 0, st, a);
-            else if (a.tile_rows == kSub) hipLaunchKernelGGL((extend_short_kernel<BITS, true, false>), grid, threads, 0, st, a);
-            else if (self) hipLaunchKernelGGL((extend_short_kernel<BITS, false, true>), grid, threads, 0, st, a);
-            else hipLaunchKernelGGL((extend_short_kernel<BITS, false, false>), grid, threads, 0, st, a);
+            else if (BITS == 4 && (long long)max_new * g.G <= kSixteen) launch_short(std::integral_constant<int, 4>{}, std::integral_constant<int, kSixteen>{});
+            else if (a.tile_rows == kSub) launch_short(bits, std::integral_constant<int, kSub>{});
+            else launch_short(bits, std::integral_constant<int, kHalvesRows>{});
         };
         if (c.bits == 16) launch(std::integral_constant<int, 16>{});
         else if (c.bits == 8) launch(std::integral_constant<int, 8>{});

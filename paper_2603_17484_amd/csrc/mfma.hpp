@@ -47,6 +47,10 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// The smaller one, D[16x16] += A[16x32] B[32x16].  Per lane (n = l & 15, g = l >> 4): A row n and B column n, k-slots 8 g .. 8 g + 7;
+// C/D column n, register r holds row 4 g + r.
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Tile orders of the forward and dQ kernels: tokens x (b, KV head) up to which the tiles of all heads

@@ -139,6 +139,33 @@ def test_blocks_that_are_nan_reach_the_rows_that_see_them_and_no_others(check, n
     check(s)
 
 
+# up to 16 rows per KV head, for which there are tiles of 16 x 16: new, cached, Hq, Hkv, W, page and more
+SIXTEEN = {
+    "as many rows as fit": ([2, 1, 2], [300, 77, 0], 16, 2, 40, 16, dict(Hm=16, f=0.5)),
+    "one head each, sixteen tokens": ([16, 3, 0, 16], [33, 1, 50, 200], 2, 2, 21, 32, dict(f=0.5, lead=2, tail=3)),
+    "no window": ([4, 1], [95, 17], 4, 1, 0, 1024, dict(f=0.6)),
+    "several tiles a workgroup": ([1] * 64, [(37 * i) % 150 for i in range(64)], 16, 8, 16, 16, dict(f=0.7)),
+    "more KV heads than a plan of its own": ([1, 0, 2, 1] * 35, [(53 * i) % 170 for i in range(140)], 8, 4, 30, 16, dict(f=0.6)),
+    "long and short": ([1] * 12, [0, 5000, 31, 32, 33, 1, 64, 2900, 16, 15, 17, 127], 4, 1, 100, 64, dict(f=0.8)),
+}
+
+
+@pytest.mark.parametrize("name", SIXTEEN)
+def test_up_to_sixteen_rows(check, name):
+    new, cached, Hq, Hkv, W, page, more = SIXTEEN[name]
+    check(Step4(new, cached, Hq, Hkv, W, page, seed=len(name), **more))
+
+
+def test_tiles_behind_one_with_nan_are_what_they_would_be(check):
+    """Rows with a masked NaN among their keys are worked out one by one, while the workgroup's next tile has begun."""
+    s = Step4([3] * 64, [(41 * i) % 90 for i in range(64)], 16, 8, 12, 16, f=0.6, seed=11)
+    for b in range(0, 64, 3):
+        s.v[b][-1, b % 8, 70] = np.nan      # the last token's, which the two before it must not see
+        s.k[b][s.cached[b] + 1, (b + 1) % 8, 3] = np.inf
+        s.v[b][s.cached[b] // 2, (b + 2) % 8, 127] = np.inf
+    check(s)
+
+
 def test_rows_outside_the_table_or_the_pool_are_skipped():
     p = B.make_params(2, 8, 2, 2, D, 4)
     c = B.alloc_cache(p, 3, 16, 2, fp4=True)
