@@ -16,7 +16,7 @@
 //   evict_move_kernel    the moves: K, V, exponents, weights
 //
 // Selection is bound by chains of launches and of dependent loads, moves by their bytes.  Half of 114688 rows of 4 KV heads in bf16 (120 MB) 61 us: 7, 9 and 15 of
-// selection, 28 of moves (4.2 TB/s; a copy of 4 GiB: 4.8).  A quarter of 1792 to 3584 rows of 32 x 8 KV heads in e4m3 (74 MB) 36.
+// selection, 28 of moves (4.2 TB/s; a copy of 4 GiB: 4.8).  A quarter of 1792 to 3584 rows of 32 x 8 KV heads in e4m3 (74 MB) 33.
 #include "paged.hpp"
 
 namespace l2a {
@@ -74,16 +74,19 @@ __device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int pair) {
     z.n = rows_of(a, z.b), z.m = plan::clamp(a.keep[z.b], 0, z.n);
     return z;
 }
+// The pair's lists in the workspace.
+__device__ __forceinline__ int32_t* to_of(const EvictArgs& a, const Sizes& z) { return a.to + (size_t)z.pair * (a.max_rows / 2); }
+__device__ __forceinline__ int32_t* from_of(const EvictArgs& a, const Sizes& z) { return a.from + (size_t)z.pair * (a.max_rows / 2); }
 // Row i0 + T j + thread of a block (of T threads) as order; 0 past the end.  Where the weights do not stay in place, those before the keep-th go to theirs (the moves
-// write over those that leave).
-template <int T>
-__device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer]) {
+// write over those that leave).  page_of(row): its page.
+template <int T, typename Page>
+__device__ __forceinline__ void load_block(const EvictArgs& a, const Sizes& z, int i0, uint32_t (&x)[kPer], Page&& page_of) {
     float w[kPer];
     size_t row[kPer];
     bool real[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int i = i0 + j * T + (int)threadIdx.x, page = i < z.n ? page_at(a, z.b, i) : 0;
+        const int i = i0 + j * T + (int)threadIdx.x, page = i < z.n ? page_of(i) : 0;
         real[j] = (unsigned)page < (unsigned)a.c.pages;
         row[j] = pool_row(a.c, a.gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), z.hk, i);
     }
@@ -105,10 +108,10 @@ __device__ __forceinline__ void load_keys(const EvictArgs& a, const Sizes& z, in
 
 template <int T>
 struct Shared {
-    int sums[T / 64], chosen[2], counts[kPer][T / 64];
+    int sums[T / 64], chosen[2], counts[2][kPer][T / 64];
 };
 // Bins from the highest number down, EACH a thread in the order of threads; mine: how many rows this thread's have, `highest` its first.  The bin in
-// which the left-th row lies, and the how-manieth in it that is.
+// which the left-th row lies, and the how-manieth in it that is.  (Before it is called again there has to be a barrier.)
 template <int EACH, int T>
 __device__ __forceinline__ void choose(Shared<T>& sh, const int (&mine)[EACH], int highest, int& bin, int& left) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -134,25 +137,24 @@ __device__ __forceinline__ void choose(Shared<T>& sh, const int (&mine)[EACH], i
     }
     __syncthreads();
     bin = sh.chosen[0], left = sh.chosen[1];
-    __syncthreads();
 }
 // Places of flags among all of a block, in the order of rows: of this thread's j-th, how many lie before it; and how many there are.  Two kinds of flags
-// at once, the second's numbers in the upper halves (a block has fewer than 2^16 rows).
+// at once, the second's numbers in the upper halves (a block has fewer than 2^16 rows).  turn: 0 and 1 by turns.
 template <int T>
-__device__ __forceinline__ int places(Shared<T>& sh, const bool (&flag)[kPer], const bool (&other)[kPer], int (&at)[kPer]) {
+__device__ __forceinline__ int places(Shared<T>& sh, int turn, const bool (&flag)[kPer], const bool (&other)[kPer], int (&at)[kPer]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned long long before = (1ull << lane) - 1ull;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const unsigned long long set = __ballot(flag[j]), more = __ballot(other[j]);
         at[j] = __popcll(set & before) + (__popcll(more & before) << 16);
-        if (lane == 0) sh.counts[j][wave] = __popcll(set) + (__popcll(more) << 16);
+        if (lane == 0) sh.counts[turn][j][wave] = __popcll(set) + (__popcll(more) << 16);
     }
     __syncthreads();
     // every wavefront adds up all counts: a lane those of two
     constexpr int kWavesOf = T / 64, kCounts = kPer * kWavesOf;
     static_assert(kCounts <= 128, "two counts a lane");
-    const int* const counts = &sh.counts[0][0];
+    const int* const counts = &sh.counts[turn][0][0];
     const int c0 = 2 * lane < kCounts ? counts[2 * lane] : 0, c1 = 2 * lane < kCounts ? counts[2 * lane + 1] : 0;
     int upto = c0 + c1;
 #pragma unroll
@@ -165,37 +167,35 @@ __device__ __forceinline__ int places(Shared<T>& sh, const bool (&flag)[kPer], c
         const int i = j * kWavesOf + wave;
         at[j] += __shfl(upto - c0 - c1, i >> 1) + (i & 1 ? __shfl(c0, i >> 1) : 0);
     }
-    const int total = __shfl(upto, 63);
-    __syncthreads();
-    return total;
+    return __shfl(upto, 63);
 }
 // What the rows of a block before it had: equal ones, places that become free, rows that move.
 struct Before {
     int equal, holes, movers;
 };
 // The lists of a block, its rows x in registers: all greater than `found` stay, and the first `left` of those equal to it.
-template <int T>
-__device__ __forceinline__ void list_block(const EvictArgs& a, Shared<T>& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past) {
-    int32_t *to = a.to + (size_t)z.pair * (a.max_rows / 2), *from = a.from + (size_t)z.pair * (a.max_rows / 2);
+template <int T, typename Index>
+__device__ __forceinline__ void list_block(const EvictArgs& a, Shared<T>& sh, const Sizes& z, int i0, const uint32_t (&x)[kPer], uint32_t found, int left, Before& past,
+                                           Index* to, Index* from) {
     int32_t* const kept = a.kept ? a.kept + (size_t)z.pair * a.max_rows : nullptr;
     bool flag[kPer], other[kPer], stays[kPer];
     int at[kPer];
     const bool all = z.m == z.n;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) flag[j] = !all && x[j] == found && i0 + j * T + (int)threadIdx.x < z.n, other[j] = false;
-    const int equal = places(sh, flag, other, at);
+    const int equal = places(sh, 0, flag, other, at);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = i0 + j * T + (int)threadIdx.x;
         stays[j] = i < z.n && (all || x[j] > found || (flag[j] && past.equal + at[j] < left));
         flag[j] = i < z.m && !stays[j], other[j] = i >= z.m && stays[j];
     }
-    const int both = places(sh, flag, other, at), holes = both & 0xffff, movers = both >> 16;
+    const int both = places(sh, 1, flag, other, at), holes = both & 0xffff, movers = both >> 16;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int i = i0 + j * T + (int)threadIdx.x;
-        if (flag[j]) to[past.holes + (at[j] & 0xffff)] = i;
-        if (other[j]) from[past.movers + (at[j] >> 16)] = i;
+        if (flag[j]) to[past.holes + (at[j] & 0xffff)] = (Index)i;
+        if (other[j]) from[past.movers + (at[j] >> 16)] = (Index)i;
         if (kept && i < z.m && stays[j]) kept[i] = i;
     }
     past = Before{past.equal + equal, past.holes + holes, past.movers + movers};
@@ -204,11 +204,10 @@ __device__ __forceinline__ void list_block(const EvictArgs& a, Shared<T>& sh, co
 // The moves of a pair, from the first-th group of lanes' on: a group per move, 16 bytes a lane, K's and V's beside one another; kAhead moves of a
 // group on their way together.
 constexpr int kAhead = 4;
-template <int BITS>
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const Sizes& z, int count, int first, int groups) {
+template <int BITS, typename Index, typename Page>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const Sizes& z, int count, int first, int groups, const Index* to_list, const Index* from_list, Page&& page_of) {
     constexpr int kLanes = 2 * BITS, kRowBytes = kD * BITS / 8;
     const int lane = threadIdx.x % kLanes, c = lane % (kLanes / 2);
-    const size_t list = (size_t)z.pair * (a.max_rows / 2);
     char* const pool = (lane < kLanes / 2 ? a.c.k : a.c.v) + c * 16;
     unsigned char* const scales = lane < kLanes / 2 ? a.c.ks : a.c.vs;
     for (int i0 = first * kAhead; i0 < count; i0 += groups * kAhead) {
@@ -219,10 +218,10 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const Sizes& z, in
         uint32_t e[kAhead];
         float w[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) to[j] = a.to[list + min(i0 + j, count - 1)], from[j] = a.from[list + min(i0 + j, count - 1)];
+        for (int j = 0; j < kAhead; ++j) to[j] = to_list[min(i0 + j, count - 1)], from[j] = from_list[min(i0 + j, count - 1)];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int p = page_at(a, z.b, to[j]), q = page_at(a, z.b, from[j]);
+            const int p = page_of(to[j]), q = page_of(from[j]);
             on[j] = i0 + j < count && (unsigned)p < (unsigned)a.c.pages && (unsigned)q < (unsigned)a.c.pages;  // page numbers outside the pool are never followed
             dst[j] = on[j] ? pool_row(a.c, a.gm.Hkv, p, z.hk, to[j]) : 0, src[j] = on[j] ? pool_row(a.c, a.gm.Hkv, q, z.hk, from[j]) : 0;
         }
@@ -247,21 +246,30 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const Sizes& z, in
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
     constexpr int kGroups = kThreads / (2 * BITS);
-    move_rows<BITS>(a, sizes_of(a, blockIdx.y), a.moves[blockIdx.y], blockIdx.x * kGroups + (int)threadIdx.x / (2 * BITS), gridDim.x * kGroups);
+    const Sizes z = sizes_of(a, blockIdx.y);
+    move_rows<BITS>(a, z, a.moves[z.pair], blockIdx.x * kGroups + (int)threadIdx.x / (2 * BITS), gridDim.x * kGroups, to_of(a, z), from_of(a, z),
+                    [&](int row) { return page_at(a, z.b, row); });
 }
 
-// MOVE: BITS of the elements, or 0: the moves are another kernel's.
+// MOVE: BITS of the elements, or 0: the moves are another kernel's.  Page numbers, and where it makes the moves its lists, stay in shared memory: nothing it
+// moves waits for more than its own row.
 template <int MOVE, int T>
 __global__ __launch_bounds__(T) void evict_select_kernel(EvictArgs a) {
+    constexpr int kPages = T * kPer / 16, kList = MOVE ? T * kPer / 2 : 1;
     __shared__ Shared<T> sh;
-    __shared__ int bins[kBins];
+    __shared__ int bins[kBins], pages[kPages];
+    __shared__ uint16_t to[kList], from[kList];
     const Sizes z = sizes_of(a, blockIdx.x);
+    for (int i = threadIdx.x; i < kBins; i += T) bins[i] = 0;
+    for (int i = threadIdx.x; i < min(kPages, a.c.max_pages); i += T) pages[i] = a.c.table[(size_t)z.b * a.c.max_pages + i];
+    auto page_of = [&](int row) { return pages[row >> a.c.page_log2]; };
     if (z.m == 0) {
         if (threadIdx.x == 0) a.moves[z.pair] = 0;
         return;
     }
+    __syncthreads();
     uint32_t x[kPer], found = 0;
-    load_block<T>(a, z, 0, x);
+    load_block<T>(a, z, 0, x, page_of);
     int left = z.m;
     constexpr int kEach = kBins / T;  // bins of a thread
     const int highest = kBins - 1 - kEach * (int)threadIdx.x;
@@ -270,24 +278,23 @@ __global__ __launch_bounds__(T) void evict_select_kernel(EvictArgs a) {
         if (z.m == z.n) break;
         constexpr int kShift[3] = {21, 10, 0};
         const int shift = kShift[pass], above = pass ? kShift[pass - 1] : 0;
-        for (int i = threadIdx.x; i < kBins; i += T) bins[i] = 0;
-        __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
             if (j * T + (int)threadIdx.x < z.n && (pass == 0 || (x[j] >> above) == (found >> above))) atomicAdd(&bins[(x[j] >> shift) & (pass == 2 ? kBins / 2 - 1 : kBins - 1)], 1);
         __syncthreads();
         int mine[kEach], bin;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) mine[e] = bins[highest - e];
+        for (int e = 0; e < kEach; ++e) mine[e] = bins[highest - e], bins[highest - e] = 0;  // (for the next pass)
         choose(sh, mine, highest, bin, left);
         found |= (uint32_t)bin << shift;
     }
     Before past{0, 0, 0};
-    list_block(a, sh, z, 0, x, found, left, past);
     if constexpr (MOVE) {
-        __syncthreads();  // (the lists, by this workgroup for itself)
-        move_rows<MOVE>(a, z, past.holes, threadIdx.x / (2 * MOVE), T / (2 * MOVE));
+        list_block(a, sh, z, 0, x, found, left, past, to, from);
+        __syncthreads();  // (the lists, and weights that did not stay in place)
+        move_rows<MOVE>(a, z, past.holes, threadIdx.x / (2 * MOVE), T / (2 * MOVE), to, from, page_of);
     } else {
+        list_block(a, sh, z, 0, x, found, left, past, to_of(a, z), from_of(a, z));
         if (threadIdx.x == 0) a.moves[z.pair] = past.holes;
     }
 }
@@ -310,7 +317,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(EvictArgs a
     __syncthreads();
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         uint32_t x[kPer];
-        load_block<kSelectThreads>(a, z, i0, x);
+        load_block<kSelectThreads>(a, z, i0, x, [&](int row) { return page_at(a, z.b, row); });
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int i = i0 + j * kSelectThreads + (int)threadIdx.x;
@@ -421,7 +428,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
                 }
             }
         };
+        const int highest = kBins - 1 - 2 * (int)threadIdx.x;
         const bool fits = in <= kCandidates;  // (else: many rows of nearly the same weight)
+        bins[highest] = bins[highest - 1] = 0;
         if (fits) all([&](const u32x2& x, int at) __attribute__((always_inline)) { candidates[at] = x; });
         __syncthreads();
         auto some = [&](auto&& f) __attribute__((always_inline)) {
@@ -431,17 +440,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
                 all([&](const u32x2& x, int) __attribute__((always_inline)) { f(x[0], (int)x[1]); });
             }
         };
-        const int highest = kBins - 1 - 2 * (int)threadIdx.x;
 #pragma unroll
         for (int pass = 0; pass < 2; ++pass) {
             const int above = pass ? 10 : 21, shift = pass ? 0 : 10;
-            bins[highest] = bins[highest - 1] = 0;
-            __syncthreads();
             some([&](uint32_t x, int) __attribute__((always_inline)) {
                 if ((x >> above) == (found >> above)) atomicAdd(&bins[(x >> shift) & ((1u << (above - shift)) - 1u)], 1);
             });
             __syncthreads();
             const int here[2] = {bins[highest], bins[highest - 1]};
+            bins[highest] = bins[highest - 1] = 0;  // (for the next pass)
             int bin;
             choose(sh, here, highest, bin, left);
             found |= (uint32_t)bin << shift;
@@ -467,18 +474,19 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
     }
     for (int i0 = g.i0; i0 < g.i1; i0 += kBlock) {
         if (i0 > g.i0) load_keys<kSelectThreads>(a, z, i0, own);
-        list_block(a, sh, z, i0, own, found, left, past);
+        list_block(a, sh, z, i0, own, found, left, past, to_of(a, z), from_of(a, z));
     }
     if ((int)blockIdx.x == of - 1 && threadIdx.x == 0) a.moves[z.pair] = past.holes;
 }
 
 constexpr int kMoveWorkgroups = 16384;
 // KV heads of sequences from which on each one's moves are made by the workgroup that selects its rows, us for those of another kernel: 256 of 3000 rows in
-// e4m3, 3/4 kept, 27.6 for 34.3; 1024 of 500 in e2m1 49.5 for 59.6; 256 of 8000 in bf16 136 for 131.  Fewer: 128 of 8000 104 for 63, 4 of 3000 26 for 16.
+// e4m3, 3/4 kept, 27 for 34; 1024 of 500 in e2m1 47 for 58; 256 of 8000 in bf16 142 for 130.  Fewer: 128 of 8000 106 for 63, 4 of 3000 24 for 16.
 constexpr int kAlone = 256;
-// And from which on, where they have up to 2048 rows, by one of 256 threads, of which a CU holds more, us for those of 1024 threads: 1024 of 1792 in e4m3 77 for 102, of 500 in
-// e2m1 21.5 for 49.4, of 100 15 for 47; 512 of 2000 in e4m3 39 for 47.  256 of 2000 31 for 26.
+// And from which on, where they have up to 2048 rows, by one of 256 threads, of which a CU holds more, us for those of 1024 threads: 1024 of 1792 in e4m3 73 for 96, of 500 in
+// e2m1 19.5 for 47, of 100 14.5 for 45; 512 of 2000 in e4m3 34 for 46.  256 of 2000 27.2 for 25.5.
 constexpr int kMany = 512;
+static_assert(kMany >= kAlone, "who selects with few threads makes the moves too, and leaves no list for another kernel");
 
 size_t lay_out(EvictArgs& a, char* base) {
     size_t at = 0;
