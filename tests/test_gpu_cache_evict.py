@@ -111,6 +111,19 @@ def test_weights_of_all_kinds(name, rows, keep):
     check(make_step(8, [0], [rows], 2, 2, 4, 64, seed=2, tail=1), [rows], [keep], VALUES[name])
 
 
+@pytest.mark.parametrize("name", VALUES)
+@pytest.mark.parametrize("sequences", [33, 65])  # times 8 KV heads
+def test_weights_of_all_kinds_where_a_workgroup_does_it_all(name, sequences):
+    rows = [1500] + [40 + i % 50 for i in range(sequences - 1)]
+    check(make_step(4, [0] * sequences, rows, 8, 8, 4, 16, seed=3, tail=1), rows, [700] + [i % 60 for i in range(sequences - 1)], VALUES[name], in_place=sequences == 65)
+
+
+@pytest.mark.parametrize("page", [16, 1024])
+def test_as_many_rows_as_a_workgroup_takes(page):
+    lengths = [8192, 8191] + [5] * 126
+    check(make_step(8, [0] * 128, lengths, 2, 2, 4, page, seed=4, tail=1, more_pages=0), lengths, [4096, 8000] + [3] * 126, spread, in_place=False)
+
+
 @pytest.mark.parametrize("rows,keep,kinds", [(600001, 299999, 10 ** 9), (600001, 599990, 50), (530000, 17, 10 ** 9), (8193, 4000, 10 ** 9), (16385, 9000, 1)])
 def test_long_caches(rows, keep, kinds):
     """More rows than a workgroup takes, and more than 64 times that many; ties across their shares."""
