@@ -5,7 +5,8 @@
 //
 // Few rows (decoding): bound by the keys' bytes.  A wavefront holds a sequence's rows as an operand of the matrix instructions (A) and takes a
 // stretch of the keys, 32 at a time as the other operand (B: a lane owns a key), whose loads are on their way while the 32 before are at
-// work.  S = Q K^T leaves a lane with 16 rows' scores of its key, whose exponentials it adds up.
+// work.  S = Q K^T leaves a lane with 16 rows' scores of its key, whose exponentials it adds up.  (Loads under a condition, in the loop: 172 us for 170 in bf16, one
+// behind 32K 10.6 for 10.0.)
 //
 // Many rows: bound by the matrix cores and the exponentials.  The rows that count are packed first.  Then a workgroup holds 256 keys in
 // registers, 64 a wavefront, and their tiles of 32 rows come through shared memory, once for all four wavefronts.  All work laid end to end is a line; every
@@ -13,7 +14,7 @@
 //
 // Nothing is added by atomics: the order of every sum is fixed.
 //
-// Measured (us): 64 tokens behind 8K of 32 / 8 heads in bf16 (831 MB) 171, 4.9 TB/s (a copy of 4 GiB: 4.8), in e4m3 106, in e2m1 67; one behind 32K 10, of which 6 are
+// Measured (us): 64 tokens behind 8K of 32 / 8 heads in bf16 (831 MB) 170, 4.9 TB/s (a copy of 4 GiB: 4.8), in e4m3 93, in e2m1 57; one behind 32K 10, of which 6 are
 // the call's; 2048 behind 32K of 28 / 4 heads, half of them routed (248 GFLOP), 250: 10 packing, 235 the products (1.05 PFLOP/s; 8192 x 8192 matrices 1.22), 5 joining.
 #include "paged.hpp"
 #include "tiles.hpp"
@@ -105,11 +106,186 @@ __device__ __forceinline__ int behind(const int* ends, int n, int x) {
 __device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int page_of(const WeightsArgs& a, int b, int key) { return a.c.table[(size_t)b * a.c.max_pages + (key >> a.c.page_log2)]; }
 
+// A wavefront's part of a KV head of a sequence: `count` blocks of 32 keys from block0 on.
+struct Part {
+    Seq s;
+    int b, hk, block0, count;
+};
 template <int BITS>
+__device__ __forceinline__ void few_part(const WeightsArgs& a, const Part& part) {
+    const Geom& gm = a.gm;
+    const Seq s = part.s;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, G = gm.G, b = part.b, hk = part.hk, block0 = part.block0, count = part.count;
+    const int last = s.pos + s.n - 1, rows = s.n * G;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // the rows: an operand, and what their scores are told apart by
+    const int r = min(n, rows - 1), tok = r / G;
+    const __bf16* const qp = a.q + ((size_t)(s.start + tok) * gm.Hq + hk * G + r - tok * G) * kD;
+    bf16x8 q[8];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(qp + slot_channel<BITS>(ks, h));
+    const float lse = a.lse[(size_t)(hk * G + r - tok * G) * gm.T + s.start + tok];
+    const bool counts = n < rows && fabsf(lse) < INFINITY;
+    const float my_bias = counts ? -lse * kLog2e : 0.f;
+    const int my_limit = counts ? s.pos + tok : -1;
+    float bias[16];
+    int limit[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) bias[e] = __shfl(my_bias, c_row(e, h)), limit[e] = __shfl(my_limit, c_row(e, h));
+    auto key_at = [&](int j) { return (block0 + j) * kSub + n; };
+    auto page_at = [&](int j) { return page_of(a, b, min(key_at(min(j, count - 1)), last)); };
+    auto row_at = [&](int j, int page) { return pool_row(a.c, gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), hk, min(key_at(j), last)); };
+    int page = page_at(0), coming = page_at(1);
+    size_t row = row_at(0, page);
+    RawKeys<BITS> raw;
+    raw.load(a.c, row, h);
+    const float* const old_weights = a.weight_in ? a.weight_in : a.weight;
+    auto old_at = [&](size_t at) { return old_weights[a.weight_in ? at : 0]; };
+    float old = old_at(row);
+    // (The last block by itself, and no load under a condition: what is on its way is then known, and waited for no earlier than it is needed.)
+    auto step = [&](auto next, int j) __attribute__((always_inline)) {
+        bf16x8 k[8];
+        raw.get(h, k);
+        const size_t row_here = row;
+        const int page_here = page;
+        const float old_here = old;
+        if constexpr (decltype(next)::value) {
+            page = coming, row = row_at(j + 1, coming);
+            raw.load(a.c, row, h);
+            old = old_at(row);
+            coming = page_at(j + 2);
+        }
+        f32x16 sc = zero16;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) sc = mfma32(q[ks], k[ks], sc);
+        const int key = key_at(j);
+        float sum = 0.f, more = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float x = fast_exp2(fmaf(sc[e], gm.scale_log2, bias[e])), y = fast_exp2(fmaf(sc[e + 1], gm.scale_log2, bias[e + 1]));
+            sum += key <= limit[e] ? x : 0.f;
+            more += key <= limit[e + 1] ? y : 0.f;
+        }
+        sum += more;
+        sum += __shfl_xor(sum, 32);
+        if (h == 0 && key <= last && (unsigned)page_here < (unsigned)a.c.pages) a.weight[row_here] = a.weight_in && key < s.pos ? fmaf(a.decay, old_here, sum) : sum;
+    };
+    for (int j = 0; j < count - 1; ++j) step(std::true_type{}, j);
+    step(std::false_type{}, count - 1);
+}
+
+// Up to 16 rows of a cache of 8 or 4 bits, in tiles of 16 x 16, which do half of what 32 rows do in fewer registers.  (64 tokens behind 8K of 32 / 8 heads in e4m3 93 us for
+// 105, in e2m1 57 for 67.)  Lane (n, g) holds key n of either 16
+// (and row n), channels 32 g .., which have one exponent; S = Q K^T leaves it with rows 4 g .. 4 g + 3.
+template <int BITS>
+struct Raw16 {
+    u32x4 x[BITS / 4];
+    uint32_t exponent;
+    __device__ __forceinline__ void load(const Pages& c, size_t row, int g) {
+        const char* const p = c.k + row * (kD * BITS / 8) + g * (4 * BITS);
+#pragma unroll
+        for (int i = 0; i < BITS / 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + i * 16);
+        if constexpr (BITS < 16) exponent = c.ks[row * kRowScales + g];
+    }
+    __device__ __forceinline__ void get(bf16x8 (&k)[4]) const {
+        constexpr int kSlots = 16 / BITS;  // slots of a load
+#pragma unroll
+        for (int i = 0; i < BITS / 4; ++i) {
+            if constexpr (BITS == 16) {
+                k[i] = __builtin_bit_cast(bf16x8, x[i]);
+            } else {
+                u32x4 y[kSlots];
+                dequantise<BITS>(x[i], exponent_value(exponent), y);
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) k[i * kSlots + j] = __builtin_bit_cast(bf16x8, y[j]);
+            }
+        }
+    }
+};
+template <int BITS>
+__device__ __forceinline__ void sixteen_part(const WeightsArgs& a, const Part& part) {
+    const Geom& gm = a.gm;
+    const Seq s = part.s;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, G = gm.G, b = part.b, hk = part.hk, last = s.pos + s.n - 1, rows = s.n * G;
+    const bool second = g & 1;  // the own key, whose weight lanes below 32 write: of the second 16
+    auto own_of = [second](auto x, auto y) { return second ? y : x; };
+    const int r = min(n, rows - 1), tok = r / G;
+    const __bf16* const qp = a.q + ((size_t)(s.start + tok) * gm.Hq + hk * G + r - tok * G) * kD + g * 32;
+    bf16x8 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const bf16x8*>(qp + 8 * i);
+    const float lse = a.lse[(size_t)(hk * G + r - tok * G) * gm.T + s.start + tok];
+    const bool counts = n < rows && fabsf(lse) < INFINITY;
+    const float my_bias = counts ? -lse * kLog2e : 0.f;
+    const int my_limit = counts ? s.pos + tok : -1;
+    float bias[4];
+    int limit[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = __shfl(my_bias, 4 * g + e), limit[e] = __shfl(my_limit, 4 * g + e);
+    struct Keys {
+        size_t row0, row1;
+        int page0, page1;
+    };
+    auto key_at = [&](int j, int p) { return (part.block0 + j) * kSub + 16 * p + n; };
+    auto in_reach = [&](int j, int p) { return min(key_at(min(j, part.count - 1), p), last); };
+    auto find_pages = [&](int j, Keys& at) { at.page0 = page_of(a, b, in_reach(j, 0)), at.page1 = page_of(a, b, in_reach(j, 1)); };
+    auto row_at = [&](int page, int key) { return pool_row(a.c, gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), hk, key); };
+    auto find_rows = [&](int j, Keys& at) { at.row0 = row_at(at.page0, in_reach(j, 0)), at.row1 = row_at(at.page1, in_reach(j, 1)); };
+    Keys here, coming;
+    Raw16<BITS> raw[2];
+    float old;
+    const float* const old_weights = a.weight_in ? a.weight_in : a.weight;
+    auto load = [&]() {
+        raw[0].load(a.c, here.row0, g), raw[1].load(a.c, here.row1, g);
+        old = old_weights[a.weight_in ? own_of(here.row0, here.row1) : 0];
+    };
+    find_pages(0, here), find_pages(1, coming);
+    find_rows(0, here);
+    load();
+    const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+    // (The last block by itself, and no load under a condition: what is on its way is then known, and waited for no earlier than it is needed.)
+    auto step = [&](auto more, int j) __attribute__((always_inline)) {
+        bf16x8 k[2][4];
+        raw[0].get(k[0]), raw[1].get(k[1]);
+        const float old_here = old;
+        const Keys own = here;
+        if constexpr (decltype(more)::value) {
+            here = coming;
+            find_rows(j + 1, here);
+            find_pages(j + 2, coming);
+            load();
+        }
+        float sum[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            f32x4 sc = zero4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc = mfma16(q[i], k[p][i], sc);
+            const int key = key_at(j, p);
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float y = fast_exp2(fmaf(sc[e], gm.scale_log2, bias[e]));
+                x[e] = key <= limit[e] ? y : 0.f;
+            }
+            sum[p] = (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        float all = own_of(sum[0], sum[1]) + __shfl_xor(own_of(sum[1], sum[0]), 16);
+        all += __shfl_xor(all, 32);
+        const int key = key_at(j, second), page = own_of(own.page0, own.page1);
+        if (g < 2 && key <= last && (unsigned)page < (unsigned)a.c.pages)
+            a.weight[own_of(own.row0, own.row1)] = a.weight_in && key < s.pos ? fmaf(a.decay, old_here, all) : all;
+    };
+    for (int j = 0; j < part.count - 1; ++j) step(std::true_type{}, j);
+    step(std::false_type{}, part.count - 1);
+}
+
+// ROWS: how many a KV head of a sequence has at most, 16 or 32.
+template <int BITS, int ROWS>
 __global__ __launch_bounds__(64 * kWaves, 2) void weights_few_kernel(WeightsArgs a, int b0) {
     __shared__ int ends[kMostSeqs], sums[kWaves];
     const Geom& gm = a.gm;
-    const int seqs = min(gm.B - b0, kMostSeqs), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, G = gm.G;
+    const int seqs = min(gm.B - b0, kMostSeqs);
     const int blocks = sum_up(seqs, ends, sums, [&](int i) {
         const Seq s = seq_at(gm, a.c, a.seq_start, a.pos, b0 + i, a.max_new);
         return s.n ? (s.pos + s.n + kSub - 1) / kSub : 0;
@@ -121,68 +297,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_few_kernel(WeightsArgs
     const long long end = u + per < units ? u + per : units;
     if (u >= end) return;
     int i = behind(ends, seqs, (int)(u / gm.Hkv));
-    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (; u < end; ++i) {
         // sequence i's part of the stretch
         const int first = i ? ends[i - 1] : 0, its = ends[i] - first, b = b0 + i;
         if (its == 0) continue;
         Seq s = seq_at(gm, a.c, a.seq_start, a.pos, b, a.max_new);
         s = Seq{same(s.start), same(s.n), same(s.pos)};
-        const int last = s.pos + s.n - 1, rows = s.n * G;
         while (u < end && u < (long long)ends[i] * gm.Hkv) {
             const int local = same((int)(u - (long long)first * gm.Hkv)), hk = local / its, block0 = local - hk * its;
-            const int count = same((int)(end - u < its - block0 ? end - u : its - block0));  // blocks of this KV head
-            // the rows: an operand, and what their scores are told apart by
-            const int r = min(n, rows - 1), tok = r / G;
-            const __bf16* const qp = a.q + ((size_t)(s.start + tok) * gm.Hq + hk * G + r - tok * G) * kD;
-            bf16x8 q[8];
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(qp + slot_channel<BITS>(ks, h));
-            const float lse = a.lse[(size_t)(hk * G + r - tok * G) * gm.T + s.start + tok];
-            const bool counts = n < rows && fabsf(lse) < INFINITY;
-            const float my_bias = counts ? -lse * kLog2e : 0.f;
-            const int my_limit = counts ? s.pos + tok : -1;
-            float bias[16];
-            int limit[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) bias[e] = __shfl(my_bias, c_row(e, h)), limit[e] = __shfl(my_limit, c_row(e, h));
-            auto key_at = [&](int j) { return (block0 + j) * kSub + n; };
-            auto page_at = [&](int j) { return page_of(a, b, min(key_at(min(j, count - 1)), last)); };
-            auto row_at = [&](int j, int page) { return pool_row(a.c, gm.Hkv, plan::clamp(page, 0, a.c.pages - 1), hk, min(key_at(j), last)); };
-            int page = page_at(0), coming = page_at(1);
-            size_t row = row_at(0, page);
-            RawKeys<BITS> raw;
-            raw.load(a.c, row, h);
-            auto old_at = [&](size_t at, int key) { return a.weight_in && h == 0 && key < s.pos ? a.weight_in[at] : 0.f; };
-            float old = old_at(row, key_at(0));
-            for (int j = 0; j < count; ++j) {
-                bf16x8 k[8];
-                raw.get(h, k);
-                const size_t row_next = row_at(min(j + 1, count - 1), coming);
-                const int page_next = coming;
-                const float old_here = old;
-                if (j + 1 < count) {
-                    raw.load(a.c, row_next, h);
-                    old = old_at(row_next, key_at(j + 1));
-                    coming = page_at(j + 2);
-                }
-                f32x16 sc = zero16;
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) sc = mfma32(q[ks], k[ks], sc);
-                const int key = key_at(j);
-                float sum = 0.f, more = 0.f;
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float x = fast_exp2(fmaf(sc[e], gm.scale_log2, bias[e])), y = fast_exp2(fmaf(sc[e + 1], gm.scale_log2, bias[e + 1]));
-                    sum += key <= limit[e] ? x : 0.f;
-                    more += key <= limit[e + 1] ? y : 0.f;
-                }
-                sum += more;
-                sum += __shfl_xor(sum, 32);
-                if (h == 0 && key <= last && (unsigned)page < (unsigned)a.c.pages) a.weight[row] = key < s.pos ? fmaf(a.decay, old_here, sum) : sum;
-                row = row_next, page = page_next;
-            }
-            u += count;
+            const Part part{s, b, hk, block0, same((int)(end - u < its - block0 ? end - u : its - block0))};
+            if constexpr (ROWS == 16) sixteen_part<BITS>(a, part);
+            else few_part<BITS>(a, part);
+            u += part.count;
         }
     }
 }
@@ -499,8 +625,11 @@ __global__ __launch_bounds__(kChunk) void weights_join_kernel(WeightsArgs a) {
     a.weight[row] = sum;
 }
 
-// Two on a CU, and three: few rows in bf16 take 171 us with two, 180 with three (their registers), many rows 267 with two, 251 with three.
-constexpr int kFewWorkgroups = 512, kManyWorkgroups = 768;
+// Two to four on a CU.  Few rows, 64 tokens behind 8K of 32 / 8 heads (4 rows) by 512, 768 and 1024 workgroups: in e4m3 101, 93 and 96 us, in e2m1 68, 59 and 57; in bf16 with
+// tiles of 16 rows 187, 175 and 175, of 32, by 512, 170.  20 rows, 30 sequences of 15K of 16 / 4 heads, by 512 and 768: in e4m3 50 and 48, in e2m1 30 and 29.  Many rows 267 with two, 251 with three.
+constexpr int kManyWorkgroups = 768;
+template <int BITS, int ROWS>
+constexpr int kFewWorkgroups = BITS == 16 ? 512 : BITS == 4 && ROWS == 16 ? 1024 : 768;
 bool few(const Geom& g, int max_new) { return (long long)(max_new < g.T ? max_new : g.T) * g.G <= kRows; }
 
 // The workspace: sub-buffers at multiples of 256 bytes.
@@ -541,8 +670,13 @@ int cache_weights(const Geom& g, const Pages& c, const void* q, const int32_t* s
         constexpr int BITS = decltype(bits)::value;
         if (few(g, max_new)) {
             KernelTimer kt("cache_weights", st);
-            for (int b0 = 0; b0 < g.B; b0 += kMostSeqs)
-                hipLaunchKernelGGL(weights_few_kernel<BITS>, dim3(kFewWorkgroups), dim3(64 * kWaves), 0, st, a, b0);
+            auto launch_few = [&](auto rows) {
+                constexpr int ROWS = decltype(rows)::value;
+                for (int b0 = 0; b0 < g.B; b0 += kMostSeqs)
+                    hipLaunchKernelGGL((weights_few_kernel<BITS, ROWS>), dim3(kFewWorkgroups<BITS, ROWS>), dim3(64 * kWaves), 0, st, a, b0);
+            };
+            if (BITS < 16 && (long long)max_new * g.G <= 16) launch_few(std::integral_constant<int, BITS < 16 ? 16 : kRows>{});
+            else launch_few(std::integral_constant<int, kRows>{});
             return;
         }
         {

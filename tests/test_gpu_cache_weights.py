@@ -131,6 +131,12 @@ def test_old_weights(new, decay, with_old, in_place):
     check(make_step(16, new, [70, 33], 4, 2, 10, 16, seed=1), 0.5, decay, with_old, in_place)
 
 
+@pytest.mark.parametrize("decay,with_old,in_place", [(0.0, True, False), (0.5, True, True), (1.0, False, False), (0.0, False, True), (0.9, True, False)])
+@pytest.mark.parametrize("bits,new,Hq,Hkv,page", [(4, [1, 0, 2], 16, 2, 16), (8, [2, 1, 1], 16, 2, 1024), (8, [8, 1, 5], 10, 5, 32), (4, [16, 9, 16], 3, 3, 64), (4, [1, 1, 1], 16, 1, 16)])
+def test_up_to_sixteen_rows(bits, new, Hq, Hkv, page, decay, with_old, in_place):
+    check(make_step(bits, new, [70, 129, 0], Hq, Hkv, 10, page, seed=page, lead=1, tail=2), 0.6, decay, with_old, in_place)
+
+
 @pytest.mark.parametrize("new", [[2, 1], [90, 3]])
 def test_what_must_not_matter(new):
     """Old weights of the new tokens' rows, and all of them where nothing of them stays; log-sum-exps that are no finite numbers count as not routed."""

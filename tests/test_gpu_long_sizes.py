@@ -60,7 +60,9 @@ def test_a_pool_in_four_bits_beyond_four_gigabytes():
 @pytest.mark.parametrize("new,cached,Hq,Hkv,f,dtype", [
     ([700, 1, 1, 40], [9000, 30000, 511, 3000], 28, 4, 0.5, "fp4"), ([3000], [0], 12, 1, 1.0, "bf16"), ([1, 2000, 1], [70000, 5000, 300], 8, 2, 0.2, "fp8"),
     ([1] * 60, [37 * i * i % 20000 for i in range(60)], 32, 8, 0.7, "bf16"), ([5] * 30, [911 * i % 15000 for i in range(30)], 16, 16, 1.0, "fp8"), ([9] * 200, [100 + i for i in range(200)], 64, 8, 0.9, "fp4"),
-    ([1500], [40000], 28, 4, 0.003, "bf16"), ([64] * 20, [256 * i for i in range(20)], 8, 8, 0.5, "fp4")])
+    ([1500], [40000], 28, 4, 0.003, "bf16"), ([64] * 20, [256 * i for i in range(20)], 8, 8, 0.5, "fp4"),
+    ([1] * 60, [37 * i * i % 20000 for i in range(60)], 32, 8, 0.7, "fp4"), ([4, 2, 1] * 10, [911 * i % 15000 for i in range(30)], 32, 8, 0.8, "fp4"), ([1] * 40, [701 * i % 18000 for i in range(40)], 16, 1, 0.9, "fp8"),
+    ([5] * 30, [911 * i % 15000 for i in range(30)], 32, 8, 0.9, "fp4"), ([7] * 20, [911 * i % 15000 for i in range(20)], 32, 8, 0.9, "fp8")])
 def test_weights_of_long_caches(new, cached, Hq, Hkv, f, dtype):
     """Against the formula in 64 bits on the GPU; log-sum-exps of random numbers' size (weights are then below 2^10 / keys)."""
     page, scale, G = 64, D ** -0.5, Hq // Hkv
