@@ -966,7 +966,6 @@ struct Rows16 {
         for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(q[s]));  // waited for here, and so not in the loop, behind its loads
         const int lo_max = t.kind == plan::kWindow ? max(t.pos1 - a.gm.W, 0) : 0, hi_min = t.kind == plan::kWindow ? t.pos0 : t.pos0 - a.gm.W - 1;
         auto masked = [&](int sb) __attribute__((always_inline)) { return sb * kSub < lo_max || sb * kSub + kSub - 1 > hi_min; };
-        const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
         const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
         RowSums16 row;
         row.clear();
@@ -974,7 +973,7 @@ struct Rows16 {
             const bool more = sb + NW < sb1;
             Place at;
             if (more) at = find(t, sb + NW);
-            f32x4 sc[2];
+            f32x4 sc[2];  // (V's conversion lies between their products and what reads them)
             {
                 bf16x8 op[2][4];
 #pragma unroll
@@ -986,10 +985,7 @@ struct Rows16 {
                 }
                 if (more) load(a.c.k, a.c.ks, at, k);
                 FENCE();
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) sc[p] = mfma16(op[p][s], q[s], s == 0 ? zero4 : sc[p]);
+                mfma16_vgpr_pair<false>(sc[0], sc[1], op[0], q, op[1], q);
             }
 #pragma unroll
             for (int p = 0; p < 2; ++p) {

@@ -242,7 +242,6 @@ __device__ __forceinline__ void sixteen_part(const WeightsArgs& a, const Part& p
     find_pages(0, here), find_pages(1, coming);
     find_rows(0, here);
     load();
-    const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
     // (The last block by itself, and no load under a condition: what is on its way is then known, and waited for no earlier than it is needed.)
     auto step = [&](auto more, int j) __attribute__((always_inline)) {
         bf16x8 k[2][4];
@@ -255,17 +254,16 @@ __device__ __forceinline__ void sixteen_part(const WeightsArgs& a, const Part& p
             find_pages(j + 2, coming);
             load();
         }
+        f32x4 sc[2];
+        mfma16_vgpr_pair<true>(sc[0], sc[1], q, k[0], q, k[1]);
         float sum[2];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            f32x4 sc = zero4;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc = mfma16(q[i], k[p][i], sc);
             const int key = key_at(j, p);
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float y = fast_exp2(fmaf(sc[e], gm.scale_log2, bias[e]));
+                const float y = fast_exp2(fmaf(sc[p][e], gm.scale_log2, bias[e]));
                 x[e] = key <= limit[e] ? y : 0.f;
             }
             sum[p] = (x[0] + x[1]) + (x[2] + x[3]);

@@ -168,5 +168,27 @@ __device__ __forceinline__ void mfma32_vgpr_from(f32x16& d, bf16x8 a, bf16x8 b, 
 __device__ __forceinline__ void mfma32_vgpr_acc(f32x16& d, bf16x8 a, bf16x8 b) {
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
+// Two 16 x 16 tiles over 128 channels, x = A0 B0 and y = A1 B1, for the VALU.  (Of the small instruction the compiler's own chains change registers from step to
+// step, which leans on its count of wait states; these accumulate in place.)  One block, so that it keeps both ends itself: two wait
+// states before the first step, as operands may come straight from the VALU, and with SETTLE eleven behind the last.  Without, the caller has as many
+// instructions between the block and what reads x or y, behind a scheduling barrier.
+template <bool SETTLE>
+__device__ __forceinline__ void mfma16_vgpr_pair(f32x4& x, f32x4& y, const bf16x8 (&a0)[4], const bf16x8 (&b0)[4], const bf16x8 (&a1)[4], const bf16x8 (&b1)[4]) {
+    asm volatile(
+        "s_nop 1\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %2, %6, 0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %10, %14, 0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %3, %7, %0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %11, %15, %1\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %4, %8, %0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %12, %16, %1\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %5, %9, %0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %13, %17, %1\n\t"
+        "s_nop %18"
+        : "=&v"(x), "=&v"(y)
+        : "v"(a0[0]), "v"(a0[1]), "v"(a0[2]), "v"(a0[3]), "v"(b0[0]), "v"(b0[1]), "v"(b0[2]), "v"(b0[3]), "v"(a1[0]), "v"(a1[1]), "v"(a1[2]), "v"(a1[3]),
+          "v"(b1[0]), "v"(b1[1]), "v"(b1[2]), "v"(b1[3]), "n"(SETTLE ? 10 : 0));
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 }  // namespace l2a

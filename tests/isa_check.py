@@ -31,8 +31,9 @@ import tempfile
 
 from paper_2603_17484_amd.build import CSRC, FLAGS, HIPCC
 
-ASM_FREE_SOURCES = ["attn_fp32.hip", "util.hip", "cache_weights.hip", "attn_extend_bf16.hip"]
-KERNEL_SOURCES = ["attn_fwd_bf16.hip", "attn_bwd_dq_bf16.hip", "attn_bwd_dkdv_bf16.hip", "attn_decode_bf16.hip"] + ASM_FREE_SOURCES
+ASM_FREE_SOURCES = ["attn_fp32.hip", "util.hip"]
+KERNEL_SOURCES = ["attn_fwd_bf16.hip", "attn_bwd_dq_bf16.hip", "attn_bwd_dkdv_bf16.hip", "attn_decode_bf16.hip", "attn_extend_bf16.hip",
+                  "cache_weights.hip"] + ASM_FREE_SOURCES
 WAIT_STATES = 11      # 8-pass matrix instruction -> read of its result by another unit
 WAIT_STATES_F32 = 10  # the same for v_mfma_f32_*_f32
 MAX_BRANCH_DEPTH = 6
