@@ -372,12 +372,13 @@ int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows
  * axis 0, the next pairs[1] to axis 1, and so on; n is their sum.  Pair i is channels i and n + i, or 2 i and 2 i + 1 with
  * L2A_ROTARY_ADJACENT; channels from 2 n on are copied.  L2A_ROTARY_INVERSE turns back, which is the gradient's way too: dq = inverse(d q_out).
  * For the layer's inputs before l2a_attn_fwd, for new tokens before l2a_cache_write and l2a_attn_extend (B = 1, T = packed tokens), and for
- * the gradients behind l2a_attn_bwd.  bf16 or fp32; angles are formed in fp64, results are rounded once.
+ * the gradients behind l2a_attn_bwd.  bf16 or fp32, D = 64 or 128; angles are formed in fp64, results are rounded once.
  *
  *   q      in  [B,T,Hq,D], k in [B,T,Hkv,D]; either may be NULL.  Heads of a token lie one behind the other, tokens q_stride (k_stride) elements apart
  *              over all B T, so that both may be parts of the rows of a fused projection; 0: contiguous
  *   pos    in  [axes, B*T] int32, device memory, any values
  *   q_out, k_out  out, as q and k; each may be its input (with the same stride).  Other overlaps are not allowed
+ * Of p: B, T, Hq, Hkv, D and dtype count (the other fields must still be valid; L2A_FLAG_SCALAR is not asked for here).
  * Errors: L2A_ERR_SHAPE for axes outside 1..4, pairs < 0, n not a positive multiple of 8 or 2 n > D, a stride smaller than a token's row or not a multiple of 16
  * bytes; L2A_ERR_UNSUPPORTED for unknown flags, in place with two strides.
  */

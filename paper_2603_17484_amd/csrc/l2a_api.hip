@@ -424,7 +424,10 @@ int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows
 
 int l2a_rope(const l2a_params* p, const l2a_rotary* r, const void* q, const void* k, const int32_t* pos, void* q_out, void* k_out,
              void* stream) {
-    const int rc = check_params(p);
+    if (!p) return L2A_ERR_NULL;
+    l2a_params any = *p;
+    if (any.D == 64) any.flags |= L2A_FLAG_SCALAR;  // (which heads of 64 channels in bf16 need for the attention only)
+    const int rc = check_params(&any);
     if (rc != L2A_OK) return rc;
     if (!r || !r->freq || !pos || (!q && !k) || (q && !q_out) || (k && !k_out)) return L2A_ERR_NULL;
     if (r->axes < 1 || r->axes > 4) return L2A_ERR_SHAPE;
