@@ -303,10 +303,12 @@ def make_rotary(freq: torch.Tensor, pairs, adjacent: bool = False, inverse: bool
 
 
 def _token_rows(t: Optional[torch.Tensor], p: l2a_params, dtype, tokens: int, heads: int, D: int, device: int, what: str):
-    """-> address and token stride in elements (0: contiguous) of a tensor [B, T, heads, D] or [B T, heads, D] whose heads lie one behind the other."""
+    """-> address and token stride in elements (0: contiguous) of a tensor [B, T, heads, D] or [B T, heads, D] whose heads lie one behind the other.  (Heads
+    may be flattened into a token's row.  Other shapes with as many entries are other layouts, such as one with the heads before the tokens.)"""
     if t is None:
         return None, 0
-    if t.dtype == dtype and t.numel() == tokens * heads * D and t.is_contiguous() and t.get_device() == device:
+    if t.dtype == dtype and t.is_contiguous() and t.get_device() == device and tuple(t.shape) in (
+            (p.B, p.T, heads, D), (tokens, heads, D), (p.B, p.T, heads * D), (tokens, heads * D), (tokens * heads * D,)):
         return t.data_ptr(), 0
     ok = t.dtype == dtype and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, D) and t.shape[0] == (tokens if t.dim() == 3 else p.B)
     ok = ok and (t.dim() == 3 or t.shape[1] == p.T) and t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == D)
