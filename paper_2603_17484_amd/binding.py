@@ -332,7 +332,7 @@ def l2a_rope(p: l2a_params, r: l2a_rotary, q, k, pos, q_out, k_out) -> None:
     k_at, ks = _token_rows(k, p, dtype, tokens, Hkv, D, dev, "k")
     qo_at, qos = _token_rows(q_out, p, dtype, tokens, Hq, D, dev, "q_out")
     ko_at, kos = _token_rows(k_out, p, dtype, tokens, Hkv, D, dev, "k_out")
-    if qs or ks or qos or kos:
+    if qs or ks or qos or kos or r.q_stride or r.k_stride or r.q_out_stride or r.k_out_stride:  # (strides are the tensors', whatever r says)
         r = l2a_rotary(r.axes, r.pairs, r.flags, qs, ks, qos, kos, r.freq)
     rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(r), q_at, k_at, _packed(pos, torch.int32, r.axes * tokens, dev, "pos"), qo_at, ko_at,
                         torch._C._cuda_getCurrentRawStream(dev))

@@ -63,3 +63,10 @@ def test_other_layouts_of_as_many_entries_are_refused(call, shape):
     for args in ((bad, k, q, k), (q, k, bad, k)):
         with pytest.raises(ValueError, match="must be"):
             call(*args)
+
+
+def test_strides_follow_the_tensors(call):
+    """What the struct says of strides is about C callers' tensors: with it, contiguous tensors would be read and written behind their ends."""
+    q, k = e(2, 6, 4, 128), e(2, 6, 2, 128)
+    for name in ("q_stride", "k_stride", "q_out_stride", "k_out_stride"):
+        assert call(q, k, q, k, **{name: 4096}) == (0, 0, 0, 0)
