@@ -358,7 +358,8 @@ int l2a_cache_weights(const l2a_params* p, const l2a_cache* c, const void* q, co
  *   weight_in   in  [pages, Hkv, page_size] float
  *   weight      out the same: rows 0 .. keep[b] - 1 are written.  May be weight_in
  *   kept_opt    out optional [B, Hkv, max_rows] int32: which row each of rows 0 .. keep[b] - 1 was before; entries behind are left as they were
- *   workspace   l2a_evict_workspace_bytes(p, c, max_rows) bytes
+ *   workspace   l2a_evict_workspace_bytes(p, c, max_rows) bytes: 4 for each of B Hkv max_rows rows, and where max_rows is larger than 8192 about 17 (rows
+ *               rounded up to multiples of 8192), so that sequences of very different lengths are better evicted from in calls of their own
  * Of p: B, Hkv and D count (the other fields must still be valid).  Rows in pages outside the pool are not moved.  Sequences that share pages must not
  * be evicted from in one call, nor may one of them while the other still needs them, nor may a page stand twice in a sequence's table.  Errors as for the other calls; L2A_ERR_SHAPE for max_rows.
  */

@@ -123,6 +123,12 @@ def layer_from_numpy(q, k, v, mask, W, dtype="bf16", flags=0, scale=None, qg=Non
     return Layer(p, up(q), up(k), up(v), m, up(qg), up(kg), up(vg), GuardedAllocator() if guard else None)
 
 
+# Rows that a call of an eviction selects among, those of all KV heads and sequences, each as long as the longest: its workspace takes 4 bytes of each, and about 17
+# where a sequence has more than 8192 (72 MB; 34 where rows are rounded up to twice as many).  That is four sequences of 114688 rows of 8 KV heads, more workgroups than
+# there are compute units.
+EVICT_ROWS = 1 << 22
+
+
 class PagedCache:
     """A paged KV cache for `p.B` sequences (p: make_params' sizes of the layer; a copy is kept as .p, whose T every step sets) and the bookkeeping around it: pages
     are handed out as sequences grow and taken back when they end.  The pool, the table and the steps' index arrays are on the GPU, what decides
@@ -244,7 +250,7 @@ class PagedCache:
     def evict(self, limit, recent: Optional[int] = None) -> np.ndarray:
         """Sequences with more than limit (one number, or one each) rows give rows up, in whole pages, down to the limit or as far as they can:
         every KV head those that received the least attention, never one of the last `recent` (default and least: the window W).  -> rows given
-        up by each sequence, whose pages are free."""
+        up by each sequence, whose pages are free.  Where there is much to select among, in several calls, of a workspace that stays small."""
         if self.weight is None:
             raise ValueError("the cache keeps no attention weights (decay)")
         self._check_not_captured()
@@ -261,16 +267,39 @@ class PagedCache:
         gone = rows - keep
         if not gone.any():
             return gone
-        self.p.T = 1
-        B.l2a_cache_evict(self.p, self.cache, self._upload(rows.astype(np.int32)), self._upload(keep.astype(np.int32)), int(rows.max()), self.weight, self.weight)
-        for b in np.nonzero(gone)[0]:
+        try:
+            for group in self._evict_groups(rows):
+                self._evict(group, rows, keep)
+        finally:
+            self.cache.tensors[4].copy_(torch.from_numpy(self.table))
+        return gone
+
+    def _evict_groups(self, rows: np.ndarray):
+        """The sequences of each call: all in one where that is small, else those with rows to give up, the longest first."""
+        if rows.size * self.p.Hkv * int(rows.max()) <= EVICT_ROWS:
+            return [np.arange(rows.size)]
+        left = [int(b) for b in np.argsort(-rows, kind="stable") if rows[b] > 0]
+        groups = []
+        while left:
+            n = max(EVICT_ROWS // (self.p.Hkv * int(rows[left[0]])), 1)
+            groups.append(np.array(left[:n]))
+            left = left[n:]
+        return groups
+
+    def _evict(self, group: np.ndarray, rows: np.ndarray, keep: np.ndarray):
+        p, cache = B.l2a_params.from_buffer_copy(self.p), self.cache
+        p.T = 1
+        if len(group) < p.B:
+            p.B = len(group)
+            k, v, ks, vs, _ = cache.tensors
+            cache = B.make_cache(k, v, self._upload(self.table[group]), ks, vs)
+        B.l2a_cache_evict(p, cache, self._upload(rows[group].astype(np.int32)), self._upload(keep[group].astype(np.int32)), int(rows[group].max()), self.weight, self.weight)
+        for b in group[rows[group] > 0]:
             first, last = keep[b] // self.page_size, rows[b] // self.page_size
             self.free.extend(int(x) for x in self.table[b, first:last])
             self.table[b] = np.concatenate([self.table[b, :first], self.table[b, last:], np.full(last - first, -1, dtype=np.int32)])
-        self.length = (self.length - gone).astype(np.int32)
-        self.evicted = self.evicted + gone
-        self.cache.tensors[4].copy_(torch.from_numpy(self.table))
-        return gone
+            self.length[b] -= rows[b] - keep[b]
+            self.evicted[b] += rows[b] - keep[b]
 
     def end(self, b: int):
         """Sequence b is over: its pages are free."""
