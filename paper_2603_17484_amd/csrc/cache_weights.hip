@@ -185,20 +185,16 @@ struct Raw16 {
         const char* const p = c.k + row * (kD * BITS / 8) + g * (4 * BITS);
 #pragma unroll
         for (int i = 0; i < BITS / 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + i * 16);
-        if constexpr (BITS < 16) exponent = c.ks[row * kRowScales + g];
+        exponent = c.ks[row * kRowScales + g];
     }
     __device__ __forceinline__ void get(bf16x8 (&k)[4]) const {
         constexpr int kSlots = 16 / BITS;  // slots of a load
 #pragma unroll
         for (int i = 0; i < BITS / 4; ++i) {
-            if constexpr (BITS == 16) {
-                k[i] = __builtin_bit_cast(bf16x8, x[i]);
-            } else {
-                u32x4 y[kSlots];
-                dequantise<BITS>(x[i], exponent_value(exponent), y);
+            u32x4 y[kSlots];
+            dequantise<BITS>(x[i], exponent_value(exponent), y);
 #pragma unroll
-                for (int j = 0; j < kSlots; ++j) k[i * kSlots + j] = __builtin_bit_cast(bf16x8, y[j]);
-            }
+            for (int j = 0; j < kSlots; ++j) k[i * kSlots + j] = __builtin_bit_cast(bf16x8, y[j]);
         }
     }
 };
