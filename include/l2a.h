@@ -373,7 +373,8 @@ int l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const int32_t* rows
  * axis 0, the next pairs[1] to axis 1, and so on; n is their sum.  Pair i is channels i and n + i, or 2 i and 2 i + 1 with
  * L2A_ROTARY_ADJACENT; channels from 2 n on are copied.  L2A_ROTARY_INVERSE turns back, which is the gradient's way too: dq = inverse(d q_out).
  * For the layer's inputs before l2a_attn_fwd, for new tokens before l2a_cache_write and l2a_attn_extend (B = 1, T = packed tokens), and for
- * the gradients behind l2a_attn_bwd.  bf16 or fp32, D = 64 or 128; angles are formed in fp64, results are rounded once.
+ * the gradients behind l2a_attn_bwd.  bf16 or fp32, D = 64 or 128; angles are formed in fp64 (off by less than
+ * 2^-23 of a turn where |freq| <= 1, at any position; in proportion to |freq| beyond), results are rounded once.
  *
  *   q      in  [B,T,Hq,D], k in [B,T,Hkv,D]; either may be NULL.  Heads of a token lie one behind the other, tokens q_stride (k_stride) elements apart
  *              over all B T, so that both may be parts of the rows of a fused projection; 0: contiguous

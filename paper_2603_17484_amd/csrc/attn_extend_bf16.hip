@@ -862,8 +862,7 @@ __device__ __forceinline__ bool few_rows(const ExtendArgs& a, char* lds, const T
 // do.  K goes straight from memory into its operand: a lane has 32 channels of a key, the part of a row that has one exponent, and the channels are
 // contracted in that order.  V becomes bf16 in shared memory.  Both are read alike: lane (n, g) key n of 16, quarter g of its row.
 // S^T = K Q^T leaves lane (n, g) with keys 4 g .. 4 g + 3 of either 16 for row n: eight slots of the weights as the next product's operand.
-// (64 sequences of 8K tokens of 32 / 8 heads 79 us for 87, 128 of 1K 61 for 70, one of 32K 17.9 for 19.2.  Two such tiles for up to 32 rows: 16 x 5 rows
-// behind 32K 61 for 55.)
+// (64 sequences of 8K tokens of 32 / 8 heads 79 us for 87, 128 of 1K 61 for 70, one of 32K 17.9 for 19.2.)
 struct RowSums16 {
     f32x4 o[8];  // channels 16 d + 4 g .. 16 d + 4 g + 3 of row n
     float m = kNone, l = 0.f;

@@ -28,7 +28,11 @@ constexpr int kPer = 8;                          // rows of a thread
 constexpr int kBlock = kSelectThreads * kPer;
 constexpr int kMostSegments = 64;                // workgroups of a KV head of a sequence
 constexpr int kBins = 2 * kSelectThreads;        // 11 bits; the last 10 leave half of them empty
-constexpr int kCandidates = 6144;                // rows of a bin in shared memory
+// Rows of a bin in shared memory.  A bin is a quarter of a power of two: half of 114688 log-normal weights (a tenth of them zero) with sigma 2, 1 and 0.5 leave 3300, 6200 and 10900 rows in
+// it.  Where they
+// do not fit, the last kernel goes through their list in memory three times, us of selection for these 33, 34 and 37, for 262144 rows 43, 43 and 49, for 2^20 75, 87 and 105.  What takes
+// long are equal weights at the border, whose counts are one word: all zero 252, 529 and 2030.
+constexpr int kCandidates = 6144;
 
 struct Counts {
     int bin, left;     // the bin of the first bits in which the last row that stays lies, and the how-manieth in it that is
@@ -429,7 +433,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(EvictArgs a)
             }
         };
         const int highest = kBins - 1 - 2 * (int)threadIdx.x;
-        const bool fits = in <= kCandidates;  // (else: many rows of nearly the same weight)
+        const bool fits = in <= kCandidates;
         bins[highest] = bins[highest - 1] = 0;
         if (fits) all([&](const u32x2& x, int at) __attribute__((always_inline)) { candidates[at] = x; });
         __syncthreads();

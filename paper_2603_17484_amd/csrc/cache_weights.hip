@@ -15,7 +15,8 @@
 // Nothing is added by atomics: the order of every sum is fixed.
 //
 // Measured (us): 64 tokens behind 8K of 32 / 8 heads in bf16 (831 MB) 170, 4.9 TB/s (a copy of 4 GiB: 4.8), in e4m3 93, in e2m1 57; one behind 32K 10, of which 6 are
-// the call's; 2048 behind 32K of 28 / 4 heads, half of them routed (248 GFLOP), 250: 10 packing, 235 the products (1.05 PFLOP/s; 8192 x 8192 matrices 1.22), 5 joining.
+// the call's; 2048 behind 32K of 28 / 4 heads, half of them routed (248 GFLOP), 250 a call (0.99 PFLOP/s; 8192 x 8192 matrices
+// 1.22); traced kernel by kernel 10 packing, 257 to 265 the products, 5 joining.
 #include "paged.hpp"
 #include "tiles.hpp"
 

@@ -4,11 +4,12 @@
 // Pair i is channels i and n + i (n pairs in all), or 2 i and 2 i + 1 with L2A_ROTARY_ADJACENT; channels from 2 n on are copied.
 //
 // The angle is found in 64 bits, in turns: positions have up to 31 bits, and 24-bit frequencies times them would leave no fraction in 32.
-// A turn's error stays below 2^-23 that way, at any position; cosine and sine are then 32-bit functions of the fraction.
+// Two products and a constant are off by 2.5 2^-53 of up to 2^28.4 |freq| turns: below 2^-23 of a turn, at any position, for frequencies up to 1, and in
+// proportion beyond.  Cosine and sine are then 32-bit functions of the fraction.
 //
 // Memory-bound: every row is read once and written once.  A workgroup finds the cosines and sines of its tokens once, for all heads, while
 // its first rows are on their way.  16384 tokens of 28 + 4 heads in bf16 (269 MB) 47 us, 5.7 TB/s (a copy of 4 GiB: 4.8; a part stays in the last-level
-// cache); 4094 of 32 + 8 in fp32 (168 MB) 35; 64 of 28 + 4 2.7, of which the launch is most.
+// cache); 4094 of 32 + 8 in fp32 (168 MB) 35; 64 of 28 + 4 3.2, of which the launch is most.
 #include "common.hpp"
 
 namespace l2a {
