@@ -267,6 +267,7 @@ class PagedCache:
         gone = rows - keep
         if not gone.any():
             return gone
+        self.length, self.evicted = self.length.copy(), self.evicted.copy()  # (who holds the old ones keeps them)
         try:
             for group in self._evict_groups(rows):
                 self._evict(group, rows, keep)

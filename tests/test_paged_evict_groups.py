@@ -66,6 +66,13 @@ def test_a_call_without_memory_leaves_its_sequences_as_they_were(calls, monkeypa
     assert sorted(cache.free + cache.table[cache.table >= 0].tolist()) == list(range(24))
 
 
+def test_lengths_that_were_taken_before_stay(calls):
+    cache = make()
+    length, evicted = cache.length, cache.evicted
+    cache.evict([16, 16, 0, 40])
+    assert length.tolist() == [96, 33, 10, 80] and evicted.tolist() == [0] * 4 and cache.length.tolist() == [16, 1, 10, 32]
+
+
 def test_params_of_the_step_stay(calls):
     cache = make()
     cache.begin_step([0, 7, 5, 0])
