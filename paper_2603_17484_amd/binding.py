@@ -302,21 +302,22 @@ def make_rotary(freq: torch.Tensor, pairs, adjacent: bool = False, inverse: bool
     return r
 
 
-def _token_rows(t: Optional[torch.Tensor], p: l2a_params, dtype, tokens: int, heads: int, D: int, device: int, what: str):
+def _token_rows(t: Optional[torch.Tensor], Bn: int, T: int, dtype, heads: int, D: int, device: int, what: str):
     """-> address and token stride in elements (0: contiguous) of a tensor [B, T, heads, D] or [B T, heads, D] whose heads lie one behind the other.  (Heads
     may be flattened into a token's row.  Other shapes with as many entries are other layouts, such as one with the heads before the tokens.)"""
     if t is None:
         return None, 0
-    if t.dtype == dtype and t.is_contiguous() and t.get_device() == device and tuple(t.shape) in (
-            (p.B, p.T, heads, D), (tokens, heads, D), (p.B, p.T, heads * D), (tokens, heads * D), (tokens * heads * D,)):
+    s, tokens = t.shape, Bn * T
+    if t.dtype == dtype and t.is_contiguous() and t.get_device() == device and (
+            s == (Bn, T, heads, D) or s == (tokens, heads, D) or s in ((Bn, T, heads * D), (tokens, heads * D), (tokens * heads * D,))):
         return t.data_ptr(), 0
-    ok = t.dtype == dtype and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, D) and t.shape[0] == (tokens if t.dim() == 3 else p.B)
-    ok = ok and (t.dim() == 3 or t.shape[1] == p.T) and t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == D)
+    ok = t.dtype == dtype and t.get_device() == device and t.dim() in (3, 4) and tuple(t.shape[-2:]) == (heads, D) and t.shape[0] == (tokens if t.dim() == 3 else Bn)
+    ok = ok and (t.dim() == 3 or t.shape[1] == T) and t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == D)
     if ok:
-        stride = heads * D if tokens == 1 else t.stride(-3) if t.dim() == 3 or p.T > 1 else t.stride(0)
-        ok = heads * D <= stride < 2 ** 31 and (t.dim() == 3 or p.B == 1 or p.T == 1 or t.stride(0) == p.T * stride)
+        stride = heads * D if tokens == 1 else t.stride(-3) if t.dim() == 3 or T > 1 else t.stride(0)
+        ok = heads * D <= stride < 2 ** 31 and (t.dim() == 3 or Bn == 1 or T == 1 or t.stride(0) == T * stride)
     if not ok:
-        raise ValueError(f"{what} must be [{p.B}, {p.T}, {heads}, {D}] or [{tokens}, {heads}, {D}] {dtype} on the current device, with one stride from "
+        raise ValueError(f"{what} must be [{Bn}, {T}, {heads}, {D}] or [{tokens}, {heads}, {D}] {dtype} on the current device, with one stride from "
                          f"token to token and the heads of a token one behind the other; got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
     return t.data_ptr(), stride
 
@@ -327,14 +328,14 @@ def l2a_rope(p: l2a_params, r: l2a_rotary, q, k, pos, q_out, k_out) -> None:
     dev = torch.cuda.current_device()
     if r.device != dev:
         raise ValueError("the frequencies must be on the current device, whose stream the call is enqueued on")
-    dtype, tokens, D, Hq, Hkv = torch_dtype(p), p.B * p.T, p.D, p.Hq, p.Hkv
-    q_at, qs = _token_rows(q, p, dtype, tokens, Hq, D, dev, "q")
-    k_at, ks = _token_rows(k, p, dtype, tokens, Hkv, D, dev, "k")
-    qo_at, qos = _token_rows(q_out, p, dtype, tokens, Hq, D, dev, "q_out")
-    ko_at, kos = _token_rows(k_out, p, dtype, tokens, Hkv, D, dev, "k_out")
+    dtype, Bn, T, D, Hq, Hkv = torch_dtype(p), p.B, p.T, p.D, p.Hq, p.Hkv
+    q_at, qs = _token_rows(q, Bn, T, dtype, Hq, D, dev, "q")
+    k_at, ks = _token_rows(k, Bn, T, dtype, Hkv, D, dev, "k")
+    qo_at, qos = _token_rows(q_out, Bn, T, dtype, Hq, D, dev, "q_out")
+    ko_at, kos = _token_rows(k_out, Bn, T, dtype, Hkv, D, dev, "k_out")
     if qs or ks or qos or kos or r.q_stride or r.k_stride or r.q_out_stride or r.k_out_stride:  # (strides are the tensors', whatever r says)
         r = l2a_rotary(r.axes, r.pairs, r.flags, qs, ks, qos, kos, r.freq)
-    rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(r), q_at, k_at, _packed(pos, torch.int32, r.axes * tokens, dev, "pos"), qo_at, ko_at,
+    rc = lib().l2a_rope(ctypes.byref(p), ctypes.byref(r), q_at, k_at, _packed(pos, torch.int32, r.axes * Bn * T, dev, "pos"), qo_at, ko_at,
                         torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         raise L2AError(rc, "l2a_rope")

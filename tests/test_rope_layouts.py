@@ -50,8 +50,7 @@ def test_layouts_that_are_taken(call):
     assert call(*parts, *parts) == (1024,) * 4
     assert call(*parts, q, k) == (1024, 1024, 0, 0)
     # one sequence's heads before the tokens is the same memory only where either is one
-    one = B.make_params(2, 1, 4, 2, 128, 4)
-    assert B._token_rows(e(2, 4, 1, 128).transpose(1, 2), one, torch.bfloat16, 2, 4, 128, -1, "q")[1] in (0, 512)
+    assert B._token_rows(e(2, 4, 1, 128).transpose(1, 2), 2, 1, torch.bfloat16, 4, 128, -1, "q")[1] in (0, 512)
 
 
 @pytest.mark.parametrize("shape", [(2, 4, 6, 128), (6, 2, 4, 128), (4, 2, 6, 128), (12, 128, 4), (2, 6, 128, 4), (6, 2, 512), (24, 256), (48, 128), (2, 3, 2, 4, 128)])
